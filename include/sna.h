@@ -286,6 +286,71 @@ sna_status_t sna_backward_static(const sna_plan_t* plan, const float* q, const f
  */
 sna_status_t sna_measure_fp32_fma_peak(double* tflops);
 
+/*
+ * ---- operators around the attention of a layer ---------------------------------------------------------------------
+ *
+ * What a layer computes next to the operator above: the norm of its queries and keys with their rotation by position, attention
+ * in 16 bits, and the dropout of its residual.  They need no plan.  Tensors carry their strides:
+ */
+typedef enum {
+    SNA_FLOAT32 = 0,
+    SNA_BFLOAT16 = 1,
+    SNA_FLOAT16 = 2
+} sna_dtype_t;
+
+/* A device tensor [B][H][nlat][nlon][C] whose channels are contiguous: element (b, h, i, j, c) is data[b * batch + h * head +
+ * i * lat + j * lon + c], strides in elements.  A packed or channels-last layout, or shared heads (stride 0 of an input), needs no copy. */
+typedef struct {
+    void* data;
+    int64_t batch, head, lat, lon;
+} sna_tensor_t;
+
+/*
+ * Norm per head and rotation by position, in one pass over queries and keys.  For a vector x of C channels at grid point (i, j):
+ *
+ *   n = x / sqrt(mean(x^2) + eps) * weight,     y = n with its pairs of channels turned by the angles of the point.
+ *
+ * Pair p of pairs_lat + pairs_lon holds the channels (2p, 2p + 1) if `interleaved`, else (p, p + pairs_lat + pairs_lon); channels
+ * that belong to no pair are not turned.  (a, b) becomes (a cos - b sin, a sin + b cos), with cos and sin read from lat_table[i][p]
+ * for p < pairs_lat and from lon_table[j][p - pairs_lat] for the others: the scores of two points then depend on their differences of
+ * latitude and longitude.  Tables are [nlat][pairs_lat][2] and [nlon][pairs_lon][2] (cos, sin), device, fp32.
+ *
+ * The backward pass takes x and dy and writes dx and dweight (summed in a fixed order: reproducible bit for bit).
+ * Sums are in fp32; results are rounded once.  y may be x, and dx may be dy (same strides); other overlaps are not allowed.
+ */
+typedef struct {
+    int nlat, nlon, H;
+    sna_tensor_t x;            /* input */
+    sna_tensor_t y;            /* forward: output */
+    sna_tensor_t dy, dx;       /* backward: gradient of the output, and of the input */
+    const float* weight;       /* [C], or NULL for ones */
+    float* dweight;            /* [C], backward; NULL if not wanted */
+    const float* lat_table;    /* may be NULL if pairs_lat = 0 */
+    const float* lon_table;
+    int pairs_lat, pairs_lon;
+} sna_rotate_t;
+
+/* parts: one or two tensors (queries and keys, whose grids and heads may differ), one launch for both.  C: a multiple of 4 between 4
+ * and 128.  Data pointers and strides must be multiples of 4 elements, tables 8-byte aligned.  A part of no points (nlat, nlon or H of
+ * zero) is not touched, but for its dweight, which is zero. */
+sna_status_t sna_norm_rotate_forward(const sna_rotate_t* parts, int n_parts, sna_dtype_t dtype, int B, int C, float eps,
+                                     int interleaved, void* cuda_stream);
+/* workspace: at least sna_norm_rotate_workspace_bytes(C), 16-byte aligned, private to the call until its work has finished; it may be
+ * NULL if no dweight is wanted. */
+size_t sna_norm_rotate_workspace_bytes(int C);
+sna_status_t sna_norm_rotate_backward(const sna_rotate_t* parts, int n_parts, sna_dtype_t dtype, int B, int C, float eps,
+                                      int interleaved, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
+ * Dropout into a residual: out[e] = residual[e] + (kept(e) ? x[e] / (1 - p) : 0), for e in [0, n); residual may be NULL (zero).
+ * kept(e): word e % 4 of the Philox 4x32 generator (ten rounds; Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", SC 2011)
+ * for the counter (e / 4, offset) and the key seed, both in 64 bits, is at least p 2^32 (rounded).  No mask is stored: the
+ * gradient of x for dout is the same call with x = dout and no residual.  rng: device, {seed, offset}, read by the kernel, so that a
+ * captured graph draws new numbers when they change.  0 <= p < 1.  out may be x or residual; pointers aligned to their elements.
+ */
+sna_status_t sna_dropout(const void* x, const void* residual, void* out, sna_dtype_t dtype, int64_t n, double p, const int64_t* rng,
+                         void* cuda_stream);
+
 /* Human-readable name of a status code (static string). */
 const char* sna_status_string(sna_status_t status);
 /* Detail of the most recent failure on the calling thread (static thread-local buffer; "" if none). */

@@ -16,6 +16,7 @@
 #include <vector>
 
 #include "sna_kernels.cuh"
+#include "sna_layer.cuh"
 #include "sna_plan.hpp"
 
 namespace {
@@ -38,6 +39,16 @@ sna_status_t cuda_fail(cudaError_t e, const char* what) {
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 }  // namespace
+
+namespace sna {
+sna_status_t fail(sna_status_t status, const char* fmt, ...) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
+    va_end(ap);
+    return status;
+}
+}  // namespace sna
 
 struct sna_plan {
     sna::HostPlan host;

@@ -11,6 +11,7 @@
 #include <atomic>
 
 #include "../../include/sna.h"
+#include "sna_torch.hpp"
 
 namespace {
 
@@ -31,8 +32,10 @@ struct Plan : torch::CustomClassHolder {
     }
 };
 
+}  // namespace
+
 // Raises sna.SnaError: as Python's own exception, the only kind that the autograd engine hands on as it is.
-void check(int status) {
+void sna_torch::check(int status) {
     if (status == SNA_OK) return;
     py::gil_scoped_acquire gil;
     const py::object type = py::module_::import("paper_2505_11157_b200.sna").attr("SnaError");
@@ -41,6 +44,10 @@ void check(int status) {
     e.persist();
     throw e;
 }
+
+namespace {
+
+using sna_torch::check;
 
 float* data(const at::Tensor& t) { return t.data_ptr<float>(); }
 void* current_stream() { return c10::cuda::getCurrentCUDAStream().stream(); }
@@ -104,4 +111,5 @@ PYBIND11_MODULE(_sna_torch, m) {
         .def(py::init([](uintptr_t h, int64_t a, int64_t b, int64_t c, int64_t d) { return c10::make_intrusive<Plan>(h, a, b, c, d); }))
         .def("close", &Plan::close);
     m.def("attention", &attention, py::call_guard<py::gil_scoped_release>());
+    sna_torch::bind_layer(m);
 }

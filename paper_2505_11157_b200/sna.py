@@ -40,6 +40,24 @@ if not os.path.exists(LIB_PATH):
 _lib = ctypes.CDLL(LIB_PATH)
 
 _vp, _i, _d, _sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_double, ctypes.c_size_t
+_f, _i64 = ctypes.c_float, ctypes.c_int64
+
+SNA_FLOAT32 = 0
+SNA_BFLOAT16 = 1
+SNA_FLOAT16 = 2
+
+
+class SnaTensor(ctypes.Structure):
+    """sna_tensor_t: a device tensor [B][H][nlat][nlon][C], strides in elements."""
+    _fields_ = [("data", _vp), ("batch", _i64), ("head", _i64), ("lat", _i64), ("lon", _i64)]
+
+
+class SnaRotate(ctypes.Structure):
+    """sna_rotate_t: one tensor of sna_norm_rotate_forward / _backward."""
+    _fields_ = [("nlat", _i), ("nlon", _i), ("H", _i), ("x", SnaTensor), ("y", SnaTensor), ("dy", SnaTensor), ("dx", SnaTensor),
+                ("weight", _vp), ("dweight", _vp), ("lat_table", _vp), ("lon_table", _vp), ("pairs_lat", _i), ("pairs_lon", _i)]
+
+
 _SIGNATURES = {
     "sna_plan_create": (_i, [_i, _i, _i, _i, _i, _i, _d, ctypes.POINTER(_vp)]),
     "sna_plan_create_host_only": (_i, [_i, _i, _i, _i, _i, _i, _d, ctypes.POINTER(_vp)]),
@@ -69,6 +87,10 @@ _SIGNATURES = {
     "sna_forward_tf32": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp]),
     "sna_backward_tf32": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _i, _i, _i, _vp]),
     "sna_backward_static": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i, _i, _i, _vp]),
+    "sna_norm_rotate_forward": (_i, [ctypes.POINTER(SnaRotate), _i, _i, _i, _i, _f, _i, _vp]),
+    "sna_norm_rotate_workspace_bytes": (_sz, [_i]),
+    "sna_norm_rotate_backward": (_i, [ctypes.POINTER(SnaRotate), _i, _i, _i, _i, _f, _i, _vp, _sz, _vp]),
+    "sna_dropout": (_i, [_vp, _vp, _vp, _i, _i64, _d, _vp, _vp]),
     "sna_measure_fp32_fma_peak": (_i, [ctypes.POINTER(ctypes.c_double)]),
     "sna_status_string": (ctypes.c_char_p, [_i]),
     "sna_last_error_message": (ctypes.c_char_p, []),
