@@ -351,6 +351,43 @@ sna_status_t sna_norm_rotate_backward(const sna_rotate_t* parts, int n_parts, sn
 sna_status_t sna_dropout(const void* x, const void* residual, void* out, sna_dtype_t dtype, int64_t n, double p, const int64_t* rng,
                          void* cuda_stream);
 
+/*
+ * Softmax attention of 16-bit tensors over all points of a grid, with a logarithmic weight per point:
+ *
+ *   s_ij = scale q_i . k_j + log_weights_j,   out_i = sum_j exp(s_ij) v_j / sum_j exp(s_ij),   lse_i = log sum_j exp(s_ij)
+ *
+ * With the logarithms of quadrature weights this is global spherical attention (Eq. s2_attention_discrete).  A point whose
+ * logarithmic weight is -1e30 or less is left out, whatever its k and v hold (infinities and NaN too); a row all of whose points are left
+ * out has out = 0, lse = -infinity and no gradient.  Hk key heads serve Hq = G Hk query heads, G each: head h reads key head h / G.
+ *
+ * q, out, dout, dq: [B][Hq][nlat_q][nlon_q][C]; k, v, dk, dv: [B][Hk][nlat_k][nlon_k][C]; bfloat16 or float16, C a multiple of 8 between
+ * 8 and 128.  Pointers and strides must be multiples of 8 elements, and a tensor's points in one line (lat = nlon * lon where both
+ * sizes are above one).  Sums, the softmax and its statistics are in fp32; softmax weights and their gradients are rounded to
+ * the tensors' type as operands of the second products, which accumulate in fp32; results are rounded once.  In float16 those operands
+ * carry powers of two, so that small probabilities and gradients keep their digits.  No atomics whose order could
+ * show: the same call gives the same bits.  Outputs must not overlap inputs.
+ */
+typedef struct {
+    int B, Hq, Hk, C;
+    int nlat_q, nlon_q, nlat_k, nlon_k;
+    sna_tensor_t q, k, v;
+    sna_tensor_t out;              /* forward: output; backward: input */
+    sna_tensor_t dout;             /* backward */
+    sna_tensor_t dq, dk, dv;       /* backward: outputs */
+    float* lse;                    /* [B][Hq][nlat_q][nlon_q]; forward: output, may be NULL; backward: input */
+    const float* log_weights;      /* [nlat_k][nlon_k], or [B] of them; NULL for zeros */
+    int64_t log_weights_batch;     /* stride of the batch, 0 if shared */
+    float scale;                   /* of the scores; 1 / sqrt(C) usually */
+} sna_attention_t;
+
+/* workspace: device, 256-byte aligned, private to the call until its work has finished; at least the bytes that the query gives for the same
+ * problem on the current device (0: it may be NULL).  The queries return 0 for invalid arguments. */
+size_t sna_attention_forward_workspace_bytes(const sna_attention_t* a, sna_dtype_t dtype);
+sna_status_t sna_attention_forward(const sna_attention_t* a, sna_dtype_t dtype, void* workspace, size_t workspace_bytes, void* cuda_stream);
+/* out and lse are those of the forward pass on the same q, k, v, weights and scale. */
+size_t sna_attention_backward_workspace_bytes(const sna_attention_t* a, sna_dtype_t dtype);
+sna_status_t sna_attention_backward(const sna_attention_t* a, sna_dtype_t dtype, void* workspace, size_t workspace_bytes, void* cuda_stream);
+
 /* Human-readable name of a status code (static string). */
 const char* sna_status_string(sna_status_t status);
 /* Detail of the most recent failure on the calling thread (static thread-local buffer; "" if none). */

@@ -1,0 +1,112 @@
+// C ABI of the 16-bit attention (declared in include/sna.h): checks of arguments and the choice of kernels.
+#include "sna_attend.cuh"
+
+namespace sna {
+namespace attend {
+namespace {
+
+bool multiple_of_8(const sna_tensor_t& t) { return ((uintptr_t)t.data & 15u) == 0 && ((t.batch | t.head | t.lat | t.lon) & 7) == 0; }
+
+// One stride for all points of a tensor; false if they do not lie in one line.
+bool view_of(const sna_tensor_t& t, int nlat, int nlon, View& view) {
+    view = View{t.data, t.batch, t.head, nlon > 1 ? t.lon : t.lat};
+    return nlat <= 1 || nlon <= 1 || t.lat == nlon * t.lon;
+}
+
+sna_status_t describe(const sna_attention_t* a, sna_dtype_t dtype, bool backward, Problem& p) {
+    if (a == nullptr) return fail(SNA_ERR_INVALID_ARG, "the problem is NULL");
+    if (dtype != SNA_BFLOAT16 && dtype != SNA_FLOAT16) return fail(SNA_ERR_UNSUPPORTED, "dtype %d unsupported (bfloat16 or float16)", (int)dtype);
+    if (a->B < 0 || a->Hq < 0 || a->Hk < 0 || a->nlat_q < 0 || a->nlon_q < 0 || a->nlat_k < 0 || a->nlon_k < 0) return fail(SNA_ERR_INVALID_ARG, "sizes must not be negative");
+    if (a->C < 8 || a->C > 128 || a->C % 8 != 0) return fail(SNA_ERR_UNSUPPORTED, "C=%d unsupported (a multiple of 8 between 8 and 128)", a->C);
+    if (a->Hk > 0 ? a->Hq % a->Hk != 0 : a->Hq != 0) return fail(SNA_ERR_INVALID_ARG, "Hq=%d must be a multiple of Hk=%d", a->Hq, a->Hk);
+    if (!(a->scale > -1e30f && a->scale < 1e30f)) return fail(SNA_ERR_INVALID_ARG, "scale must be finite");
+    const int64_t Nq = (int64_t)a->nlat_q * a->nlon_q, Nk = (int64_t)a->nlat_k * a->nlon_k, most = (int64_t)1 << 30;
+    if (Nq >= most || Nk >= most || (int64_t)a->Hq * Nq >= most || (int64_t)a->Hk * Nk >= most || (int64_t)a->B * a->Hq * Nq >= 64 * most || (int64_t)a->B * a->Hk * Nk >= 64 * most ||
+        (int64_t)a->B * a->Hq >= most)
+        return fail(SNA_ERR_UNSUPPORTED, "problem too large: heads * points must be less than 2^30, and 2^36 over the batch");
+    p = Problem{};
+    p.B = a->B; p.Hq = a->Hq; p.Hk = a->Hk; p.G = a->Hk > 0 ? a->Hq / a->Hk : 1; p.Nq = (int)Nq; p.Nk = (int)Nk; p.C = a->C;
+    p.scale = a->scale; p.scale_log2 = a->scale * LOG2E;
+    p.lse = a->lse; p.log_weights = a->log_weights; p.log_weights_batch = a->log_weights_batch;
+    if (((uintptr_t)a->lse | (uintptr_t)a->log_weights) & 3u) return fail(SNA_ERR_INVALID_ARG, "lse and log_weights must be 4-byte aligned");
+    struct { const sna_tensor_t& t; View& view; bool used, query; } tensors[] = {
+        {a->q, p.q, true, true},          {a->k, p.k, true, false},       {a->v, p.v, true, false},       {a->out, p.out, true, true},
+        {a->dout, p.dout, backward, true}, {a->dq, p.dq, backward, true}, {a->dk, p.dk, backward, false}, {a->dv, p.dv, backward, false}};
+    for (const auto& x : tensors) {
+        if (!x.used) continue;
+        if (!multiple_of_8(x.t)) return fail(SNA_ERR_INVALID_ARG, "data pointers and strides must be multiples of 8 elements");
+        if (!view_of(x.t, x.query ? a->nlat_q : a->nlat_k, x.query ? a->nlon_q : a->nlon_k, x.view)) return fail(SNA_ERR_INVALID_ARG, "the points of a tensor must lie in one line (lat = nlon * lon)");
+        const int64_t elements = (int64_t)a->B * (x.query ? a->Hq * Nq : a->Hk * Nk);
+        if (elements > 0 && x.t.data == nullptr) return fail(SNA_ERR_INVALID_ARG, "a tensor's data is NULL");
+    }
+    if (backward && rows_of(p) > 0 && a->lse == nullptr) return fail(SNA_ERR_INVALID_ARG, "lse must not be NULL");
+    return SNA_OK;
+}
+
+sna_status_t check_workspace(const void* workspace, size_t bytes, size_t need) {
+    if (need == 0) return SNA_OK;
+    if (workspace == nullptr || ((uintptr_t)workspace & 255u)) return fail(SNA_ERR_INVALID_ARG, "workspace must be non-NULL and 256-byte aligned");
+    if (bytes < need) return fail(SNA_ERR_WORKSPACE, "workspace too small: %zu < %zu bytes", bytes, need);
+    return SNA_OK;
+}
+
+size_t forward_bytes(const Problem& p, int splits) { return splits > 1 ? align256((size_t)splits * rows_of(p) * (1 + p.C) * sizeof(float)) : 0; }
+size_t backward_bytes(const Problem& p) { return 2 * align256((size_t)rows_of(p) * sizeof(float)) + align256((size_t)p.B * p.Hk * 2 * sizeof(uint32_t)); }
+
+}  // namespace
+}  // namespace attend
+}  // namespace sna
+
+using namespace sna::attend;
+
+extern "C" {
+
+size_t sna_attention_forward_workspace_bytes(const sna_attention_t* a, sna_dtype_t dtype) {
+    Problem p;
+    if (describe(a, dtype, false, p) != SNA_OK) return 0;
+    return forward_bytes(p, forward_splits(p, sna::sms_of_current_device()));
+}
+
+sna_status_t sna_attention_forward(const sna_attention_t* a, sna_dtype_t dtype, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    Problem p;
+    sna_status_t st = describe(a, dtype, false, p);
+    if (st != SNA_OK) return st;
+    if (rows_of(p) == 0) return SNA_OK;
+    const int sms = sna::sms_of_current_device();
+    if (sms == 0) return sna::fail(SNA_ERR_CUDA, "no CUDA device");
+    const int splits = forward_splits(p, sms);
+    st = check_workspace(workspace, workspace_bytes, forward_bytes(p, splits));
+    if (st != SNA_OK) return st;
+    const cudaError_t e = launch_forward(p, dtype, splits, static_cast<float*>(workspace), (cudaStream_t)cuda_stream);
+    if (e != cudaSuccess) return sna::fail(SNA_ERR_CUDA, "attention launch: %s", cudaGetErrorString(e));
+    return SNA_OK;
+}
+
+size_t sna_attention_backward_workspace_bytes(const sna_attention_t* a, sna_dtype_t dtype) {
+    Problem p;
+    if (describe(a, dtype, true, p) != SNA_OK) return 0;
+    return backward_bytes(p);
+}
+
+sna_status_t sna_attention_backward(const sna_attention_t* a, sna_dtype_t dtype, void* workspace, size_t workspace_bytes, void* cuda_stream) {
+    Problem p;
+    sna_status_t st = describe(a, dtype, true, p);
+    if (st != SNA_OK) return st;
+    const bool queries = rows_of(p) > 0, keys = (int64_t)p.B * p.Hk * p.Nk > 0;
+    if (!queries && !keys) return SNA_OK;
+    if (sna::sms_of_current_device() == 0) return sna::fail(SNA_ERR_CUDA, "no CUDA device");
+    st = check_workspace(workspace, workspace_bytes, backward_bytes(p));
+    if (st != SNA_OK) return st;
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    Stats s;
+    s.lse2 = static_cast<float*>(workspace);
+    s.D = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256((size_t)rows_of(p) * sizeof(float)));
+    s.norms = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + 2 * align256((size_t)rows_of(p) * sizeof(float)));
+    cudaError_t e = launch_statistics(p, s, dtype, stream);
+    if (e == cudaSuccess && queries) e = launch_backward_dq(p, s, dtype, stream);
+    if (e == cudaSuccess && keys) e = launch_backward_dkdv(p, s, dtype, stream);
+    if (e != cudaSuccess) return sna::fail(SNA_ERR_CUDA, "attention backward launch: %s", cudaGetErrorString(e));
+    return SNA_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,51 @@
+// What the 16-bit attention's kernels and their dispatch share.
+#pragma once
+#include "sna_layer.cuh"
+
+namespace sna {
+namespace attend {
+
+// Logarithmic weights that are not above this leave their point out (the lowest numbers of 32 and of 16 bits count as -infinity do).
+constexpr float EXCLUDED = -1e30f;
+constexpr float LOG2E = 1.4426950408889634f;
+constexpr float LN2 = 0.6931471805599453f;
+
+// [B][H][points][C]: strides in elements
+struct View {
+    void* data;
+    int64_t batch, head, point;
+};
+
+struct Problem {
+    View q, k, v, out, dout, dq, dk, dv;
+    float* lse;                     // [B][Hq][Nq], natural logarithm; may be null in the forward pass
+    const float* log_weights;       // [B or 1][Nk], or null
+    int64_t log_weights_batch;      // 0: shared
+    int B, Hq, Hk, G, Nq, Nk, C;    // G = Hq / Hk
+    float scale, scale_log2;
+};
+
+// Workspace of the backward pass: statistics per query, and the largest norms per key head (bits of floats)
+struct Stats {
+    float* lse2;                    // [B][Hq][Nq]: log2 of the sum of weights, +infinity for rows without any
+    float* D;                       // [B][Hq][Nq]
+    uint32_t* norms;                // [B][Hk][2]: of dout's rows, of v's rows (float16 only)
+};
+
+// Powers of two that keep float16 operands of the second products away from the numbers that its exponent has no room for: softmax
+// weights (at most 1) and, in the backward pass, probabilities are held times 2^SHIFT.
+template <typename T> constexpr float SHIFT = 0.f;
+template <> constexpr float SHIFT<__half> = 14.f;
+
+inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+__host__ __device__ inline int64_t rows_of(const Problem& p) { return (int64_t)p.B * p.Hq * p.Nq; }
+
+// mma.sync kernels (sna_kernels_attend.cu)
+int forward_splits(const Problem& p, int sms);
+cudaError_t launch_forward(const Problem& p, sna_dtype_t dtype, int splits, float* partials, cudaStream_t stream);
+cudaError_t launch_statistics(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream);
+cudaError_t launch_backward_dq(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream);
+cudaError_t launch_backward_dkdv(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream);
+
+}  // namespace attend
+}  // namespace sna

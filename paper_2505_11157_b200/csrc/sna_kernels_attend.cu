@@ -1,0 +1,724 @@
+// Softmax attention over all points with a logarithmic weight per point, 16-bit tensors: forward pass, its form for few queries, and the
+// backward pass that recomputes the probabilities.
+//
+//   s_ij = scale q_i.k_j + w_j,  p_ij = exp(s_ij - lse_i),  out_i = sum_j p_ij v_j,  lse_i = log sum_j exp(s_ij)
+//   t_ij = dout_i.v_j,  D_i = dout_i.out_i,  ds_ij = p_ij (t_ij - D_i)
+//   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i
+//
+// These are the kernels for any size, on mma.sync (m16n8k16): a warp owns 16 rows, scores stay in registers and become the next product's
+// operand there.  Products are accumulated in 32 bits, the softmax and all statistics are in 32 bits; p and ds are rounded to the tensors'
+// type as operands of the second products (to nearest, so that the roundings of a sum's terms cancel on average).
+//
+// A key head serves G query heads: their rows are stacked, so that the head's keys are read once for all of them, and so that its
+// gradients are summed within one block.  Few rows: a tile of 16 rows, the block's four warps sharing each 64 keys, and the keys split
+// over blocks whose partial results a second kernel joins.
+//
+// A point whose weight leaves it out is read as zeros, whatever it holds, and has a weight of exactly zero.  A row without any point has
+// out = 0, lse = -infinity, and no gradient.
+#include <algorithm>
+
+#include "sna_attend.cuh"
+
+namespace sna {
+namespace attend {
+namespace {
+
+constexpr int BN = 64;              // keys (or queries) per streamed block
+constexpr int WARPS = 4, THREADS = 32 * WARPS;
+
+__device__ __forceinline__ uint32_t s32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x)); return y; }
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool take) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldsm(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm_t(uint32_t (&r)[4], uint32_t addr) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+template <typename T> __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1);
+template <> __device__ __forceinline__ void mma<__nv_bfloat16>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <> __device__ __forceinline__ void mma<__half>(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+template <typename T> __device__ __forceinline__ uint32_t pack(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t pack<__nv_bfloat16>(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// A tile in shared memory: rows of CP 16-bit channels in pieces of 16 bytes, which are permuted within a row so that the eight rows of an
+// 8x8 matrix meet different banks.
+template <int CP> __device__ __forceinline__ uint32_t piece(int row, int c) {
+    constexpr int CH = CP / 8;
+    return (uint32_t)(row * CP * 2 + ((c ^ (CH >= 8 ? row & 7 : (row >> 1) & 3)) << 4));
+}
+// The A operand (16 rows x 16 channels) of rows row0 .. row0 + 15 at channel step ks
+template <int CP> __device__ __forceinline__ void load_a(uint32_t (&a)[4], uint32_t tile, int row0, int ks, int lane) {
+    ldsm(a, tile + piece<CP>(row0 + (lane & 15), ks * 2 + (lane >> 4)));
+}
+// B operands of 16 rows n0 .. n0 + 15 (as columns of the product) at channel step ks: b[0], b[1] for the first eight, b[2], b[3]
+template <int CP> __device__ __forceinline__ void load_b(uint32_t (&b)[4], uint32_t tile, int n0, int ks, int lane) {
+    ldsm(b, tile + piece<CP>(n0 + (lane & 7) + ((lane >> 4) << 3), ks * 2 + ((lane >> 3) & 1)));
+}
+// B operands for a sum over rows k0 .. k0 + 15 of 16 channels from 16 * n
+template <int CP> __device__ __forceinline__ void load_bt(uint32_t (&b)[4], uint32_t tile, int k0, int n, int lane) {
+    ldsm_t(b, tile + piece<CP>(k0 + (lane & 7) + (((lane >> 3) & 1) << 3), n * 2 + (lane >> 4)));
+}
+
+// rows [first, first + R) of a head's points (stride `point`); a row that is not there, or for which take(row in tile) is false, is zero
+template <int CP, typename T, typename Take>
+__device__ __forceinline__ void load_rows(uint32_t tile, const T* head, int64_t point, int first, int rows, int R, int C, Take take) {
+    constexpr int CH = CP / 8;
+    for (int e = threadIdx.x; e < R * CH; e += THREADS) {
+        const int r = e / CH, c = e - r * CH;
+        const bool there = first + r < rows && c * 8 < C && take(r);
+        copy16(tile + piece<CP>(r, c), there ? head + (int64_t)(first + r) * point + c * 8 : head, there);
+    }
+}
+// the same for the stacked rows of the query heads of a group: row = head in the group * Nq + query
+template <int CP, typename T>
+__device__ __forceinline__ void load_stacked(uint32_t tile, const T* group, int64_t head, int64_t point, int first, int rows, int Nq, int R, int C) {
+    constexpr int CH = CP / 8;
+    for (int e = threadIdx.x; e < R * CH; e += THREADS) {
+        const int r = e / CH, c = e - r * CH, row = first + r;
+        const bool there = row < rows && c * 8 < C;
+        const int g = there ? row / Nq : 0;
+        copy16(tile + piece<CP>(r, c), there ? group + g * head + (int64_t)(row - g * Nq) * point + c * 8 : group, there);
+    }
+}
+
+// log2 of a point's weight, -infinity if it is left out
+__device__ __forceinline__ float weight2(const float* weights, int n) {
+    if (weights == nullptr) return 0.f;
+    const float w = weights[n];
+    return w <= EXCLUDED ? -INFINITY : w * LOG2E;
+}
+
+// ---- forward ---------------------------------------------------------------------------------------------------------------
+
+template <int CP, int WM> constexpr int forward_smem() { return WM * 16 * CP * 2 + 4 * BN * CP * 2; }
+
+// WM warps along the rows, WK = 4 / WM along the keys of a block.  partials: null, or [splits][rows] statistics and [splits][rows][C] sums.
+template <typename T, int CP, int WM>
+__global__ void __launch_bounds__(THREADS) attend_forward_kernel(const __grid_constant__ Problem p, int tiles, int splits, float* partials) {
+    constexpr int WK = WARPS / WM, BM = 16 * WM, KW = BN / WK, NT = KW / 8, CN = CP / 8;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ float bias[4][BN];
+    const uint32_t tq = s32(smem), tkv = tq + BM * CP * 2;      // stages of (K, V)
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wm = warp % WM, wk = warp / WM;
+    const int split = blockIdx.x % splits, rest = blockIdx.x / splits, tile = rest % tiles, bh = rest / tiles;
+    const int b = bh / p.Hk, hk = bh - b * p.Hk;
+    const int rows = p.G * p.Nq, row0 = tile * BM;
+    const T* kh = static_cast<const T*>(p.k.data) + b * p.k.batch + hk * p.k.head;
+    const T* vh = static_cast<const T*>(p.v.data) + b * p.v.batch + hk * p.v.head;
+    const float* weights = p.log_weights == nullptr ? nullptr : p.log_weights + b * p.log_weights_batch;
+    const int blocks = (p.Nk + BN - 1) / BN;
+    const int first = (int)((int64_t)blocks * split / splits), last = (int)((int64_t)blocks * (split + 1) / splits);
+
+    auto load_bias = [&](int j) {
+        if (tid < BN) {
+            const int n = j * BN + tid;
+            bias[j & 3][tid] = j < last && n < p.Nk ? weight2(weights, n) : -INFINITY;
+        }
+    };
+    auto load_block = [&](int j) {
+        if (j < last) {
+            auto take = [&](int r) { return bias[j & 3][r] != -INFINITY; };
+            const uint32_t stage = tkv + (j & 1) * 2 * BN * CP * 2;
+            load_rows<CP>(stage, kh, p.k.point, j * BN, p.Nk, BN, p.C, take);
+            load_rows<CP>(stage + BN * CP * 2, vh, p.v.point, j * BN, p.Nk, BN, p.C, take);
+        }
+        commit();
+    };
+    load_stacked<CP>(tq, static_cast<const T*>(p.q.data) + b * p.q.batch + (int64_t)hk * p.G * p.q.head, p.q.head, p.q.point, row0, rows, p.Nq, BM, p.C);
+    load_bias(first);
+    load_bias(first + 1);
+    __syncthreads();
+    load_block(first);
+
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[CN][4];
+#pragma unroll
+    for (int n = 0; n < CN; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
+
+    for (int j = first; j < last; ++j) {
+        load_bias(j + 2);
+        load_block(j + 1);
+        wait_group<1>();
+        __syncthreads();
+        const uint32_t tk = tkv + (j & 1) * 2 * BN * CP * 2, tv = tk + BN * CP * 2;
+        const int key0 = wk * KW;
+        float s[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[n][i] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < CP / 16; ++ks) {
+            uint32_t a[4];
+            load_a<CP>(a, tq, wm * 16, ks, lane);
+#pragma unroll
+            for (int n = 0; n < NT; n += 2) {
+                uint32_t kb[4];
+                load_b<CP>(kb, tk, key0 + n * 8, ks, lane);
+                mma<T>(s[n], a, kb[0], kb[1]);
+                mma<T>(s[n + 1], a, kb[2], kb[3]);
+            }
+        }
+        float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float2 w = *reinterpret_cast<const float2*>(&bias[j & 3][key0 + n * 8 + (lane & 3) * 2]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[n][i] = fmaf(s[n][i], p.scale_log2, (i & 1) ? w.y : w.x);
+                top[i >> 1] = fmaxf(top[i >> 1], s[n][i]);
+            }
+        }
+        float base[2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 1));
+            top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
+            const float now = fmaxf(m[r], top[r]);
+            base[r] = now == -INFINITY ? 0.f : now;                 // (no point so far: every weight is exp2(-infinity))
+            const float correction = ex2(m[r] - base[r]);
+            m[r] = now;
+            l[r] *= correction;
+#pragma unroll
+            for (int n = 0; n < CN; ++n) { o[n][2 * r] *= correction; o[n][2 * r + 1] *= correction; }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[n][i] = ex2(s[n][i] - base[i >> 1] + SHIFT<T>);
+                l[i >> 1] += s[n][i];
+            }
+#pragma unroll
+        for (int ks = 0; ks < KW / 16; ++ks) {
+            const uint32_t a[4] = {pack<T>(s[2 * ks][0], s[2 * ks][1]), pack<T>(s[2 * ks][2], s[2 * ks][3]), pack<T>(s[2 * ks + 1][0], s[2 * ks + 1][1]),
+                                   pack<T>(s[2 * ks + 1][2], s[2 * ks + 1][3])};
+#pragma unroll
+            for (int n = 0; n < CN; n += 2) {
+                uint32_t vb[4];
+                load_bt<CP>(vb, tv, key0 + ks * 16, n / 2, lane);
+                mma<T>(o[n], a, vb[0], vb[1]);
+                mma<T>(o[n + 1], a, vb[2], vb[3]);
+            }
+        }
+        __syncthreads();        // before the stage is overwritten
+    }
+    wait_group<0>();
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);
+        l[r] += __shfl_xor_sync(0xffffffffu, l[r], 2);
+    }
+    if constexpr (WK > 1) {
+        // the warps' sums of the same rows are joined in the stages' memory: [warp][row][CP + 2]
+        __syncthreads();
+        float* join = reinterpret_cast<float*>(smem + BM * CP * 2);
+        constexpr int PITCH = CP + 4;
+        static_assert(WARPS * 16 * PITCH * 4 <= 4 * BN * CP * 2, "the join fits");
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            float* mine = join + (warp * 16 + (lane >> 2) + 8 * r) * PITCH;
+            if ((lane & 3) == 0) { mine[CP] = m[r]; mine[CP + 1] = l[r]; }
+#pragma unroll
+            for (int n = 0; n < CN; ++n) *reinterpret_cast<float2*>(mine + n * 8 + (lane & 3) * 2) = make_float2(o[n][2 * r], o[n][2 * r + 1]);
+        }
+        __syncthreads();
+        // warp w joins rows 4 w .. 4 w + 3
+        for (int r = warp * 4; r < warp * 4 + 4; ++r) {
+            float top = -INFINITY, total = 0.f;
+            for (int w = 0; w < WARPS; ++w) top = fmaxf(top, join[(w * 16 + r) * PITCH + CP]);
+            const float base = top == -INFINITY ? 0.f : top;
+            float factor[WARPS];
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) {
+                factor[w] = ex2(join[(w * 16 + r) * PITCH + CP] - base);
+                total += factor[w] * join[(w * 16 + r) * PITCH + CP + 1];
+            }
+            const int row = row0 + r;
+            if (row >= rows) continue;
+            const int g = row / p.Nq;
+            const int64_t at = ((int64_t)b * p.Hq + hk * p.G + g) * p.Nq + (row - g * p.Nq);
+            const float inverse = total == 0.f ? 0.f : 1.f / total;
+            const float lse2 = total == 0.f ? -INFINITY : top + log2f(total) - SHIFT<T>;
+            for (int c = lane; c < p.C; c += 32) {
+                float sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < WARPS; ++w) sum += factor[w] * join[(w * 16 + r) * PITCH + c];
+                if (partials != nullptr) partials[(int64_t)splits * rows_of(p) + ((int64_t)split * rows_of(p) + at) * p.C + c] = sum * inverse;
+                else static_cast<T*>(p.out.data)[b * p.out.batch + (int64_t)(hk * p.G + g) * p.out.head + (int64_t)(row - g * p.Nq) * p.out.point + c] = from_float<T>(sum * inverse);
+            }
+            if (lane == 0) {
+                if (partials != nullptr) partials[(int64_t)split * rows_of(p) + at] = lse2;
+                else if (p.lse != nullptr) p.lse[at] = lse2 * LN2;
+            }
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            const int row = row0 + wm * 16 + (lane >> 2) + 8 * r;
+            if (row >= rows) continue;
+            const int g = row / p.Nq;
+            const int64_t at = ((int64_t)b * p.Hq + hk * p.G + g) * p.Nq + (row - g * p.Nq);
+            const float inverse = l[r] == 0.f ? 0.f : 1.f / l[r];
+            const float lse2 = l[r] == 0.f ? -INFINITY : m[r] + log2f(l[r]) - SHIFT<T>;
+            T* out = static_cast<T*>(p.out.data) + b * p.out.batch + (int64_t)(hk * p.G + g) * p.out.head + (int64_t)(row - g * p.Nq) * p.out.point;
+#pragma unroll
+            for (int n = 0; n < CN; ++n) {
+                const int c = n * 8 + (lane & 3) * 2;
+                if (c >= p.C) continue;
+                const float x = o[n][2 * r] * inverse, y = o[n][2 * r + 1] * inverse;
+                if (partials != nullptr) *reinterpret_cast<float2*>(partials + (int64_t)splits * rows_of(p) + ((int64_t)split * rows_of(p) + at) * p.C + c) = make_float2(x, y);
+                else *reinterpret_cast<uint32_t*>(out + c) = pack<T>(x, y);
+            }
+            if ((lane & 3) == 0) {
+                if (partials != nullptr) partials[(int64_t)split * rows_of(p) + at] = lse2;
+                else if (p.lse != nullptr) p.lse[at] = lse2 * LN2;
+            }
+        }
+    }
+}
+
+// Joins the splits' results of a row: out = sum_s 2^(lse2_s - lse2) out_s.  One block of 128 threads per row; warp w takes the splits w, w + 4, ...
+template <typename T>
+__global__ void __launch_bounds__(THREADS) attend_join_kernel(const __grid_constant__ Problem p, int splits, const float* partials) {
+    __shared__ float sums[WARPS][128];
+    __shared__ float totals[WARPS];
+    const int64_t rows = rows_of(p), at = blockIdx.x;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    float top = -INFINITY;
+    for (int s = lane; s < splits; s += 32) top = fmaxf(top, partials[s * rows + at]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum[4] = {0.f, 0.f, 0.f, 0.f}, total = 0.f;
+    const float* values = partials + (int64_t)splits * rows;
+    for (int s = warp; s < splits; s += WARPS) {
+        const float w = ex2(partials[s * rows + at] - base);
+        total += w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (lane + 32 * i < p.C) sum[i] = fmaf(w, values[(s * rows + at) * p.C + lane + 32 * i], sum[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sums[warp][lane + 32 * i] = sum[i];
+    if (lane == 0) totals[warp] = total;
+    __syncthreads();
+    total = totals[0] + totals[1] + totals[2] + totals[3];
+    const int c = threadIdx.x, i = (int)(at % p.Nq);
+    const int64_t bh = at / p.Nq, b = bh / p.Hq, h = bh - b * p.Hq;
+    if (c < p.C) {
+        const float x = sums[0][c] + sums[1][c] + sums[2][c] + sums[3][c];
+        static_cast<T*>(p.out.data)[b * p.out.batch + h * p.out.head + i * p.out.point + c] = from_float<T>(total == 0.f ? 0.f : x / total);
+    }
+    if (c == 0 && p.lse != nullptr) p.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
+}
+
+// ---- backward: statistics -----------------------------------------------------------------------------------------------------
+
+// Per query: D = dout . out, and log2 of the sum of weights.  float16: also the largest norm of a row of dout and of v per key head, which bound
+// |t - D| <= 2 |dout| |v| (the blocks beyond the queries' take v's rows).  A maximum does not depend on the order of its atomics.  Four lanes per row.
+template <typename T>
+__global__ void __launch_bounds__(256) attend_statistics_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats s, int64_t query_blocks) {
+    constexpr bool SCALED = SHIFT<T> != 0.f;
+    const int part = threadIdx.x & 3;
+    const bool queries = blockIdx.x < query_blocks;
+    const int64_t row = ((int64_t)blockIdx.x - (queries ? 0 : query_blocks)) * 64 + (threadIdx.x >> 2);
+    const int64_t rows = queries ? rows_of(p) : (int64_t)p.B * p.Hk * p.Nk;
+    float square = 0.f, dot = 0.f;
+    int64_t bk = 0;
+    bool there = row < rows;
+    if (there) {
+        const int N = queries ? p.Nq : p.Nk, H = queries ? p.Hq : p.Hk;
+        const int64_t bh = row / N, n = row - bh * N, b = bh / H, h = bh - b * H;
+        bk = queries ? b * p.Hk + h / p.G : bh;
+        if (!queries && p.log_weights != nullptr && p.log_weights[b * p.log_weights_batch + n] <= EXCLUDED) there = false;
+        const View& x = queries ? p.dout : p.v;
+        const T* px = static_cast<const T*>(x.data) + b * x.batch + h * x.head + n * x.point;
+        const T* py = queries ? static_cast<const T*>(p.out.data) + b * p.out.batch + h * p.out.head + n * p.out.point : px;
+        if (there)
+            for (int c = part * 8; c < p.C; c += 32) {
+                const Pack<T, 8> a = *reinterpret_cast<const Pack<T, 8>*>(px + c), o = *reinterpret_cast<const Pack<T, 8>*>(py + c);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float f = to_float(a.v[i]);
+                    dot = fmaf(f, to_float(o.v[i]), dot);
+                    if (SCALED) square = fmaf(f, f, square);
+                }
+            }
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o <<= 1) {
+        dot += __shfl_xor_sync(0xffffffffu, dot, o);
+        if (SCALED) square += __shfl_xor_sync(0xffffffffu, square, o);
+    }
+    if (there && part == 0) {
+        if (queries) {
+            const float lse = p.lse[row];
+            s.D[row] = lse == -INFINITY ? 0.f : dot;
+            s.lse2[row] = lse == -INFINITY ? INFINITY : lse * LOG2E - SHIFT<T>;
+        }
+        if (SCALED) atomicMax(s.norms + bk * 2 + (queries ? 0 : 1), __float_as_uint(sqrtf(square)));
+    }
+}
+
+// The power of two that ds is held times.  The probabilities in it are already held times 2^SHIFT; with |t - D| <= bound the products stay below 2^15.
+template <typename T>
+__device__ __forceinline__ float ds_scale(const Stats& s, int bk) {
+    if (SHIFT<T> == 0.f) return 1.f;
+    const float bound = 2.f * __uint_as_float(s.norms[bk * 2]) * __uint_as_float(s.norms[bk * 2 + 1]);
+    if (!(bound > 0.f && bound < INFINITY)) return 1.f;
+    return exp2f(fminf(fmaxf(-ceilf(log2f(bound)), -100.f), 100.f));
+}
+
+// ---- backward: dq -------------------------------------------------------------------------------------------------------------
+
+template <int CP> constexpr int dq_smem() { return 2 * 64 * CP * 2 + 4 * BN * CP * 2; }
+
+// A block owns 64 stacked rows (16 per warp) and walks all keys.
+template <typename T, int CP>
+__global__ void __launch_bounds__(THREADS) attend_dq_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats st, int tiles) {
+    constexpr int BM = 64, NT = BN / 8, CN = CP / 8;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ float bias[4][BN];
+    const uint32_t tq = s32(smem), ty = tq + BM * CP * 2, tkv = ty + BM * CP * 2;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tile = blockIdx.x % tiles, bh = blockIdx.x / tiles, b = bh / p.Hk, hk = bh - b * p.Hk;
+    const int rows = p.G * p.Nq, row0 = tile * BM;
+    const T* kh = static_cast<const T*>(p.k.data) + b * p.k.batch + hk * p.k.head;
+    const T* vh = static_cast<const T*>(p.v.data) + b * p.v.batch + hk * p.v.head;
+    const float* weights = p.log_weights == nullptr ? nullptr : p.log_weights + b * p.log_weights_batch;
+    const int last = (p.Nk + BN - 1) / BN;
+    auto load_bias = [&](int j) {
+        if (tid < BN) {
+            const int n = j * BN + tid;
+            bias[j & 3][tid] = j < last && n < p.Nk ? weight2(weights, n) : -INFINITY;
+        }
+    };
+    auto load_block = [&](int j) {
+        if (j < last) {
+            auto take = [&](int r) { return bias[j & 3][r] != -INFINITY; };
+            const uint32_t stage = tkv + (j & 1) * 2 * BN * CP * 2;
+            load_rows<CP>(stage, kh, p.k.point, j * BN, p.Nk, BN, p.C, take);
+            load_rows<CP>(stage + BN * CP * 2, vh, p.v.point, j * BN, p.Nk, BN, p.C, take);
+        }
+        commit();
+    };
+    load_stacked<CP>(tq, static_cast<const T*>(p.q.data) + b * p.q.batch + (int64_t)hk * p.G * p.q.head, p.q.head, p.q.point, row0, rows, p.Nq, BM, p.C);
+    load_stacked<CP>(ty, static_cast<const T*>(p.dout.data) + b * p.dout.batch + (int64_t)hk * p.G * p.dout.head, p.dout.head, p.dout.point, row0, rows, p.Nq, BM, p.C);
+    load_bias(0);
+    load_bias(1);
+    __syncthreads();
+    load_block(0);
+
+    const int64_t first_row = ((int64_t)b * p.Hq + hk * p.G) * p.Nq;        // (stacked rows lie one after the other in the statistics)
+    float lse2[2], D[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int row = row0 + warp * 16 + (lane >> 2) + 8 * r;
+        lse2[r] = row < rows ? st.lse2[first_row + row] : INFINITY;
+        D[r] = row < rows ? st.D[first_row + row] : 0.f;
+    }
+    const float factor = ds_scale<T>(st, bh);
+    float dq[CN][4];
+#pragma unroll
+    for (int n = 0; n < CN; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dq[n][i] = 0.f;
+
+    for (int j = 0; j < last; ++j) {
+        load_bias(j + 2);
+        load_block(j + 1);
+        wait_group<1>();
+        __syncthreads();
+        const uint32_t tk = tkv + (j & 1) * 2 * BN * CP * 2, tv = tk + BN * CP * 2;
+        float s[NT][4], t[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { s[n][i] = 0.f; t[n][i] = 0.f; }
+#pragma unroll
+        for (int ks = 0; ks < CP / 16; ++ks) {
+            uint32_t a[4], y[4];
+            load_a<CP>(a, tq, warp * 16, ks, lane);
+            load_a<CP>(y, ty, warp * 16, ks, lane);
+#pragma unroll
+            for (int n = 0; n < NT; n += 2) {
+                uint32_t kb[4], vb[4];
+                load_b<CP>(kb, tk, n * 8, ks, lane);
+                mma<T>(s[n], a, kb[0], kb[1]);
+                mma<T>(s[n + 1], a, kb[2], kb[3]);
+                load_b<CP>(vb, tv, n * 8, ks, lane);
+                mma<T>(t[n], y, vb[0], vb[1]);
+                mma<T>(t[n + 1], y, vb[2], vb[3]);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float2 w = *reinterpret_cast<const float2*>(&bias[j & 3][n * 8 + (lane & 3) * 2]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float pr = ex2(fmaf(s[n][i], p.scale_log2, (i & 1) ? w.y : w.x) - lse2[i >> 1]);
+                s[n][i] = pr * ((t[n][i] - D[i >> 1]) * factor);
+            }
+        }
+#pragma unroll
+        for (int ks = 0; ks < BN / 16; ++ks) {
+            const uint32_t a[4] = {pack<T>(s[2 * ks][0], s[2 * ks][1]), pack<T>(s[2 * ks][2], s[2 * ks][3]), pack<T>(s[2 * ks + 1][0], s[2 * ks + 1][1]),
+                                   pack<T>(s[2 * ks + 1][2], s[2 * ks + 1][3])};
+#pragma unroll
+            for (int n = 0; n < CN; n += 2) {
+                uint32_t kb[4];
+                load_bt<CP>(kb, tk, ks * 16, n / 2, lane);
+                mma<T>(dq[n], a, kb[0], kb[1]);
+                mma<T>(dq[n + 1], a, kb[2], kb[3]);
+            }
+        }
+        __syncthreads();
+    }
+    wait_group<0>();
+    const float back = p.scale * ex2(-SHIFT<T>) / factor;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int row = row0 + warp * 16 + (lane >> 2) + 8 * r;
+        if (row >= rows) continue;
+        const int g = row / p.Nq;
+        T* out = static_cast<T*>(p.dq.data) + b * p.dq.batch + (int64_t)(hk * p.G + g) * p.dq.head + (int64_t)(row - g * p.Nq) * p.dq.point;
+#pragma unroll
+        for (int n = 0; n < CN; ++n) {
+            const int c = n * 8 + (lane & 3) * 2;
+            if (c < p.C) *reinterpret_cast<uint32_t*>(out + c) = pack<T>(dq[n][2 * r] * back, dq[n][2 * r + 1] * back);
+        }
+    }
+}
+
+// ---- backward: dk, dv -----------------------------------------------------------------------------------------------------------
+
+// Streamed queries per block: 64, or 32 for wide heads, whose two sums take 128 registers
+template <int CP> constexpr int DKDV_QUERIES = CP > 64 ? 32 : 64;
+template <int CP> constexpr int dkdv_smem() { return 2 * 64 * CP * 2 + 4 * DKDV_QUERIES<CP> * CP * 2; }
+
+// A block owns 64 keys (16 per warp) and walks the stacked queries of its group.
+template <typename T, int CP>
+__global__ void __launch_bounds__(THREADS) attend_dkdv_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats st, int tiles) {
+    constexpr int BM = 64, QB = DKDV_QUERIES<CP>, NT = QB / 8, CN = CP / 8;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ float2 stats[2][QB];         // lse2, D
+    const uint32_t tk = s32(smem), tv = tk + BM * CP * 2, tqy = tv + BM * CP * 2;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int tile = blockIdx.x % tiles, bh = blockIdx.x / tiles, b = bh / p.Hk, hk = bh - b * p.Hk;
+    const int rows = p.G * p.Nq, key0 = tile * BM;
+    const T* qg = static_cast<const T*>(p.q.data) + b * p.q.batch + (int64_t)hk * p.G * p.q.head;
+    const T* yg = static_cast<const T*>(p.dout.data) + b * p.dout.batch + (int64_t)hk * p.G * p.dout.head;
+    const float* weights = p.log_weights == nullptr ? nullptr : p.log_weights + b * p.log_weights_batch;
+    const int64_t first_row = ((int64_t)b * p.Hq + hk * p.G) * p.Nq;
+    const int last = (rows + QB - 1) / QB;
+    auto load_block = [&](int j) {
+        if (j < last) {
+            const uint32_t stage = tqy + (j & 1) * 2 * QB * CP * 2;
+            load_stacked<CP>(stage, qg, p.q.head, p.q.point, j * QB, rows, p.Nq, QB, p.C);
+            load_stacked<CP>(stage + QB * CP * 2, yg, p.dout.head, p.dout.point, j * QB, rows, p.Nq, QB, p.C);
+            if (tid < QB) {
+                const int row = j * QB + tid;
+                stats[j & 1][tid] = row < rows ? make_float2(st.lse2[first_row + row], st.D[first_row + row]) : make_float2(INFINITY, 0.f);
+            }
+        }
+        commit();
+    };
+    auto take = [&](int r) { return weight2(weights, min(key0 + r, p.Nk - 1)) != -INFINITY; };
+    load_rows<CP>(tk, static_cast<const T*>(p.k.data) + b * p.k.batch + hk * p.k.head, p.k.point, key0, p.Nk, BM, p.C, take);
+    load_rows<CP>(tv, static_cast<const T*>(p.v.data) + b * p.v.batch + hk * p.v.head, p.v.point, key0, p.Nk, BM, p.C, take);
+    load_block(0);
+    float w2[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int n = key0 + warp * 16 + (lane >> 2) + 8 * r;
+        w2[r] = n < p.Nk ? weight2(weights, n) : -INFINITY;
+    }
+    const float factor = ds_scale<T>(st, bh);
+    float dk[CN][4], dv[CN][4];
+#pragma unroll
+    for (int n = 0; n < CN; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { dk[n][i] = 0.f; dv[n][i] = 0.f; }
+
+    for (int j = 0; j < last; ++j) {
+        load_block(j + 1);
+        wait_group<1>();
+        __syncthreads();
+        const uint32_t tq = tqy + (j & 1) * 2 * QB * CP * 2, ty = tq + QB * CP * 2;
+        float s[NT][4], t[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { s[n][i] = 0.f; t[n][i] = 0.f; }
+#pragma unroll
+        for (int ks = 0; ks < CP / 16; ++ks) {
+            uint32_t a[4], y[4];
+            load_a<CP>(a, tk, warp * 16, ks, lane);
+            load_a<CP>(y, tv, warp * 16, ks, lane);
+#pragma unroll
+            for (int n = 0; n < NT; n += 2) {
+                uint32_t qb[4], yb[4];
+                load_b<CP>(qb, tq, n * 8, ks, lane);
+                mma<T>(s[n], a, qb[0], qb[1]);
+                mma<T>(s[n + 1], a, qb[2], qb[3]);
+                load_b<CP>(yb, ty, n * 8, ks, lane);
+                mma<T>(t[n], y, yb[0], yb[1]);
+                mma<T>(t[n + 1], y, yb[2], yb[3]);
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float4 w = *reinterpret_cast<const float4*>(&stats[j & 1][n * 8 + (lane & 3) * 2]);       // lse2, D of two queries
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                s[n][i] = ex2(fmaf(s[n][i], p.scale_log2, w2[i >> 1]) - ((i & 1) ? w.z : w.x));
+                t[n][i] = s[n][i] * ((t[n][i] - ((i & 1) ? w.w : w.y)) * factor);
+            }
+        }
+#pragma unroll
+        for (int ks = 0; ks < QB / 16; ++ks) {
+            const uint32_t a[4] = {pack<T>(s[2 * ks][0], s[2 * ks][1]), pack<T>(s[2 * ks][2], s[2 * ks][3]), pack<T>(s[2 * ks + 1][0], s[2 * ks + 1][1]),
+                                   pack<T>(s[2 * ks + 1][2], s[2 * ks + 1][3])};
+            const uint32_t d[4] = {pack<T>(t[2 * ks][0], t[2 * ks][1]), pack<T>(t[2 * ks][2], t[2 * ks][3]), pack<T>(t[2 * ks + 1][0], t[2 * ks + 1][1]),
+                                   pack<T>(t[2 * ks + 1][2], t[2 * ks + 1][3])};
+#pragma unroll
+            for (int n = 0; n < CN; n += 2) {
+                uint32_t yb[4], qb[4];
+                load_bt<CP>(yb, ty, ks * 16, n / 2, lane);
+                mma<T>(dv[n], a, yb[0], yb[1]);
+                mma<T>(dv[n + 1], a, yb[2], yb[3]);
+                load_bt<CP>(qb, tq, ks * 16, n / 2, lane);
+                mma<T>(dk[n], d, qb[0], qb[1]);
+                mma<T>(dk[n + 1], d, qb[2], qb[3]);
+            }
+        }
+        __syncthreads();
+    }
+    wait_group<0>();
+    const float unshift = ex2(-SHIFT<T>), back = p.scale * unshift / factor;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int n_key = key0 + warp * 16 + (lane >> 2) + 8 * r;
+        if (n_key >= p.Nk) continue;
+        T* k_out = static_cast<T*>(p.dk.data) + b * p.dk.batch + hk * p.dk.head + (int64_t)n_key * p.dk.point;
+        T* v_out = static_cast<T*>(p.dv.data) + b * p.dv.batch + hk * p.dv.head + (int64_t)n_key * p.dv.point;
+#pragma unroll
+        for (int n = 0; n < CN; ++n) {
+            const int c = n * 8 + (lane & 3) * 2;
+            if (c >= p.C) continue;
+            *reinterpret_cast<uint32_t*>(k_out + c) = pack<T>(dk[n][2 * r] * back, dk[n][2 * r + 1] * back);
+            *reinterpret_cast<uint32_t*>(v_out + c) = pack<T>(dv[n][2 * r] * unshift, dv[n][2 * r + 1] * unshift);
+        }
+    }
+}
+
+// ---- launches -------------------------------------------------------------------------------------------------------------------
+
+template <typename K>
+cudaError_t allow(K kernel, int bytes) {       // (48 KB hold the static arrays too)
+    return bytes > 40 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) : cudaSuccess;
+}
+bool few_rows(const Problem& p) { return p.G * (int64_t)p.Nq <= 16; }
+int forward_tiles(const Problem& p) { return (int)(((int64_t)p.G * p.Nq + (few_rows(p) ? 15 : 63)) / (few_rows(p) ? 16 : 64)); }
+
+template <typename T, int CP, int WM>
+cudaError_t forward_as(const Problem& p, int splits, float* partials, cudaStream_t stream) {
+    const int tiles = forward_tiles(p);
+    cudaError_t e = allow(attend_forward_kernel<T, CP, WM>, forward_smem<CP, WM>());
+    if (e != cudaSuccess) return e;
+    attend_forward_kernel<T, CP, WM><<<(unsigned)((int64_t)p.B * p.Hk * tiles * splits), THREADS, forward_smem<CP, WM>(), stream>>>(p, tiles, splits, splits > 1 ? partials : nullptr);
+    e = cudaGetLastError();
+    if (e != cudaSuccess || splits == 1) return e;
+    attend_join_kernel<T><<<(unsigned)rows_of(p), THREADS, 0, stream>>>(p, splits, partials);
+    return cudaGetLastError();
+}
+template <typename T, int CP>
+cudaError_t dq_as(const Problem& p, const Stats& s, cudaStream_t stream) {
+    const int tiles = (int)(((int64_t)p.G * p.Nq + 63) / 64);
+    cudaError_t e = allow(attend_dq_kernel<T, CP>, dq_smem<CP>());
+    if (e != cudaSuccess) return e;
+    attend_dq_kernel<T, CP><<<(unsigned)((int64_t)p.B * p.Hk * tiles), THREADS, dq_smem<CP>(), stream>>>(p, s, tiles);
+    return cudaGetLastError();
+}
+template <typename T, int CP>
+cudaError_t dkdv_as(const Problem& p, const Stats& s, cudaStream_t stream) {
+    const int tiles = (p.Nk + 63) / 64;
+    cudaError_t e = allow(attend_dkdv_kernel<T, CP>, dkdv_smem<CP>());
+    if (e != cudaSuccess) return e;
+    attend_dkdv_kernel<T, CP><<<(unsigned)((int64_t)p.B * p.Hk * tiles), THREADS, dkdv_smem<CP>(), stream>>>(p, s, tiles);
+    return cudaGetLastError();
+}
+template <typename F>
+cudaError_t by_width(int C, F f) {
+    return C <= 32 ? f(std::integral_constant<int, 32>()) : C <= 64 ? f(std::integral_constant<int, 64>()) : f(std::integral_constant<int, 128>());
+}
+
+}  // namespace
+
+// Blocks that share the keys of a tile: until the GPU has four blocks per SM, with at least four blocks of 64 keys each.
+int forward_splits(const Problem& p, int sms) {
+    const int64_t tiles = (int64_t)p.B * p.Hk * forward_tiles(p);
+    const int64_t blocks = (p.Nk + BN - 1) / BN;
+    if (tiles == 0 || blocks == 0 || tiles >= 2 * sms) return 1;
+    return (int)std::max<int64_t>(1, std::min(blocks / 4, 4 * sms / tiles));
+}
+
+cudaError_t launch_forward(const Problem& p, sna_dtype_t dtype, int splits, float* partials, cudaStream_t stream) {
+    return by_width(p.C, [&](auto width) {
+        constexpr int CP = decltype(width)::value;
+        if (dtype == SNA_BFLOAT16) return few_rows(p) ? forward_as<__nv_bfloat16, CP, 1>(p, splits, partials, stream) : forward_as<__nv_bfloat16, CP, 4>(p, splits, partials, stream);
+        return few_rows(p) ? forward_as<__half, CP, 1>(p, splits, partials, stream) : forward_as<__half, CP, 4>(p, splits, partials, stream);
+    });
+}
+
+cudaError_t launch_statistics(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream) {
+    const int64_t query_blocks = (rows_of(p) + 63) / 64, key_blocks = ((int64_t)p.B * p.Hk * p.Nk + 63) / 64;
+    if (dtype == SNA_BFLOAT16) {
+        if (query_blocks == 0) return cudaSuccess;
+        attend_statistics_kernel<__nv_bfloat16><<<(unsigned)query_blocks, 256, 0, stream>>>(p, s, query_blocks);
+    } else {
+        const cudaError_t e = cudaMemsetAsync(s.norms, 0, (size_t)p.B * p.Hk * 2 * sizeof(uint32_t), stream);
+        if (e != cudaSuccess) return e;
+        attend_statistics_kernel<__half><<<(unsigned)(query_blocks + key_blocks), 256, 0, stream>>>(p, s, query_blocks);
+    }
+    return cudaGetLastError();
+}
+
+cudaError_t launch_backward_dq(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream) {
+    return by_width(p.C, [&](auto width) {
+        constexpr int CP = decltype(width)::value;
+        return dtype == SNA_BFLOAT16 ? dq_as<__nv_bfloat16, CP>(p, s, stream) : dq_as<__half, CP>(p, s, stream);
+    });
+}
+
+cudaError_t launch_backward_dkdv(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream) {
+    return by_width(p.C, [&](auto width) {
+        constexpr int CP = decltype(width)::value;
+        return dtype == SNA_BFLOAT16 ? dkdv_as<__nv_bfloat16, CP>(p, s, stream) : dkdv_as<__half, CP>(p, s, stream);
+    });
+}
+
+}  // namespace attend
+}  // namespace sna

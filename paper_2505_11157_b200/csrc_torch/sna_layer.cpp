@@ -197,6 +197,128 @@ std::tuple<at::Tensor, at::Tensor> qk_norm_rotate(const at::Tensor& q, const at:
     return {out[0], out[1]};
 }
 
+// ---- attention ------------------------------------------------------------------------------------------------------------
+
+// Points in one line, 16-byte pieces: the tensor itself if it is so, else a contiguous copy.
+bool in_line(const at::Tensor& t) { return in_place(t, 8) && (t.size(2) <= 1 || t.size(3) <= 1 || t.stride(2) == t.size(3) * t.stride(3)); }
+at::Tensor attendable(const at::Tensor& t) {
+    if (in_line(t)) return t;
+    const at::Tensor c = t.contiguous();
+    return in_line(c) ? c : c.clone();
+}
+at::Tensor attention_result_like(const at::Tensor& t) {
+    at::Tensor r = at::empty_like(t);
+    return in_line(r) ? r : at::empty_like(t, at::MemoryFormat::Contiguous);
+}
+
+struct AttentionInputs {
+    at::Tensor q, k, v, log_weights;
+    double scale;
+};
+
+void check_attention(const AttentionInputs& in) {
+    const at::Tensor& q = in.q;
+    TORCH_CHECK_VALUE(q.dim() == 5, "q must be [B, H, nlat, nlon, C], got ", q.sizes());
+    TORCH_CHECK_VALUE(q.is_cuda() && q.layout() == at::kStrided, "q must be a dense CUDA tensor");
+    TORCH_CHECK_VALUE(q.scalar_type() == at::kBFloat16 || q.scalar_type() == at::kHalf, "q must be bfloat16 or float16, got ", q.scalar_type());
+    check_like(in.k, "k", q, "q");
+    check_like(in.v, "v", q, "q");
+    TORCH_CHECK_VALUE(in.k.dim() == 5 && in.k.size(0) == q.size(0) && in.k.size(4) == q.size(4), "k must be [B, H, nlat, nlon, C] with B = ", q.size(0), " and C = ", q.size(4),
+                      ", got ", in.k.sizes());
+    TORCH_CHECK_VALUE(in.v.sizes() == in.k.sizes(), "v has shape ", in.v.sizes(), ", expected ", in.k.sizes());
+    for (const at::Tensor* t : {&in.q, &in.k})
+        for (int i = 0; i < 4; ++i) TORCH_CHECK_VALUE(t->size(i) < (1 << 30), "a tensor is too large: ", t->sizes());
+    TORCH_CHECK_VALUE(in.k.size(1) > 0 ? q.size(1) % in.k.size(1) == 0 : q.size(1) == 0, "q's heads (", q.size(1), ") must be a multiple of k's (", in.k.size(1), ")");
+    if (!in.log_weights.defined()) return;
+    const at::Tensor& w = in.log_weights;
+    check_cuda(w, "log_weights", q, "q");
+    const int64_t points = in.k.size(2) * in.k.size(3);
+    TORCH_CHECK_VALUE(w.scalar_type() == at::kFloat, "log_weights must be float32, got ", w.scalar_type());
+    TORCH_CHECK_VALUE((w.dim() == 1 || (w.dim() == 2 && (w.size(0) == q.size(0) || w.size(0) == 1))) && w.size(-1) == points, "log_weights must be [", points, "] or [", q.size(0), ", ",
+                      points, "], got ", w.sizes());
+    TORCH_CHECK_VALUE(!w.requires_grad(), "log_weights: no gradient of the weights is computed");
+}
+
+sna_attention_t described(const AttentionInputs& in) {
+    sna_attention_t a{};
+    a.B = (int)in.q.size(0); a.Hq = (int)in.q.size(1); a.Hk = (int)in.k.size(1); a.C = (int)in.q.size(4);
+    a.nlat_q = (int)in.q.size(2); a.nlon_q = (int)in.q.size(3); a.nlat_k = (int)in.k.size(2); a.nlon_k = (int)in.k.size(3);
+    a.q = described(in.q); a.k = described(in.k); a.v = described(in.v);
+    if (in.log_weights.defined()) {
+        a.log_weights = in.log_weights.const_data_ptr<float>();
+        a.log_weights_batch = in.log_weights.dim() == 2 && in.log_weights.size(0) > 1 ? in.log_weights.stride(0) : 0;
+    }
+    a.scale = (float)in.scale;
+    return a;
+}
+
+// (the inputs become what the kernels read)
+std::tuple<at::Tensor, at::Tensor> attention_forward(AttentionInputs& in) {
+    const c10::cuda::CUDAGuard guard(in.q.device());
+    for (at::Tensor* t : {&in.q, &in.k, &in.v}) *t = attendable(*t);
+    if (in.log_weights.defined() && in.log_weights.size(-1) > 1 && in.log_weights.stride(-1) != 1) in.log_weights = in.log_weights.contiguous();
+    at::Tensor out = attention_result_like(in.q), lse = at::empty(in.q.sizes().slice(0, 4), in.q.options().dtype(at::kFloat));
+    const sna_dtype_t dtype = dtype_of(in.q, "q");
+    sna_attention_t a = described(in);
+    a.out = described(out);
+    a.lse = lse.data_ptr<float>();
+    const size_t bytes = sna_attention_forward_workspace_bytes(&a, dtype);
+    at::Tensor workspace;
+    if (bytes > 0) workspace = at::empty({(int64_t)bytes}, in.q.options().dtype(at::kByte));
+    check(sna_attention_forward(&a, dtype, bytes ? workspace.data_ptr() : nullptr, bytes, stream_of(in.q)));
+    return {out, lse};
+}
+
+class WeightedAttention : public torch::autograd::Function<WeightedAttention> {
+public:
+    static variable_list forward(AutogradContext* ctx, at::Tensor q, at::Tensor k, at::Tensor v, std::optional<at::Tensor> log_weights, double scale) {
+        AttentionInputs in{q, k, v, or_undefined(log_weights), scale};
+        auto [out, lse] = attention_forward(in);
+        ctx->save_for_backward({in.q, in.k, in.v, in.log_weights, out, lse});
+        ctx->saved_data["scale"] = scale;
+        ctx->mark_non_differentiable({lse});
+        return {out, lse};
+    }
+    static variable_list backward(AutogradContext* ctx, variable_list grads) {
+        check_once_differentiable("weighted_attention");
+        const auto saved = ctx->get_saved_variables();
+        AttentionInputs in{saved[0], saved[1], saved[2], saved[3], ctx->saved_data["scale"].toDouble()};
+        // (what hooks on saved tensors return is checked like arguments)
+        check_attention(in);
+        const at::Tensor& lse = saved[5];
+        check_like(saved[4], "out", in.q, "q");
+        TORCH_CHECK_VALUE(saved[4].sizes() == in.q.sizes(), "out has shape ", saved[4].sizes(), ", expected ", in.q.sizes());
+        TORCH_CHECK_VALUE(grads[0].sizes() == in.q.sizes() && grads[0].device() == in.q.device(), "the gradient has shape ", grads[0].sizes(), ", expected ", in.q.sizes());
+        check_cuda(lse, "lse", in.q, "q");
+        TORCH_CHECK_VALUE(lse.scalar_type() == at::kFloat && lse.sizes() == in.q.sizes().slice(0, 4) && lse.is_contiguous(), "lse must be float32 and contiguous, of shape ",
+                          in.q.sizes().slice(0, 4));
+        const c10::cuda::CUDAGuard guard(in.q.device());
+        for (at::Tensor* t : {&in.q, &in.k, &in.v}) *t = attendable(*t);
+        const at::Tensor out = attendable(saved[4]), dout = attendable(grads[0].to(in.q.scalar_type()));
+        at::Tensor dq = attention_result_like(in.q), dk = attention_result_like(in.k), dv = attention_result_like(in.v);
+        const sna_dtype_t dtype = dtype_of(in.q, "q");
+        sna_attention_t a = described(in);
+        a.out = described(out); a.dout = described(dout);
+        a.dq = described(dq); a.dk = described(dk); a.dv = described(dv);
+        a.lse = const_cast<float*>(lse.const_data_ptr<float>());
+        const size_t bytes = sna_attention_backward_workspace_bytes(&a, dtype);
+        at::Tensor workspace;
+        if (bytes > 0) workspace = at::empty({(int64_t)bytes}, in.q.options().dtype(at::kByte));
+        check(sna_attention_backward(&a, dtype, bytes ? workspace.data_ptr() : nullptr, bytes, stream_of(in.q)));
+        return {dq, dk, dv, Variable(), Variable()};
+    }
+};
+
+std::tuple<at::Tensor, at::Tensor> weighted_attention(const at::Tensor& q, const at::Tensor& k, const at::Tensor& v, const std::optional<at::Tensor>& log_weights, double scale) {
+    AttentionInputs in{q, k, v, or_undefined(log_weights), scale};
+    check_attention(in);
+    if (wants_grad({&q, &k, &v})) {
+        const variable_list r = WeightedAttention::apply(q, k, v, log_weights, scale);
+        return {r[0], r[1]};
+    }
+    return attention_forward(in);
+}
+
 // ---- dropout --------------------------------------------------------------------------------------------------------------
 
 at::Tensor dropout_into(const at::Tensor& x, const at::Tensor& residual, const at::Tensor& state, double p) {
@@ -252,6 +374,7 @@ at::Tensor residual_dropout(const at::Tensor& x, const at::Tensor& state, double
 namespace sna_torch {
 void bind_layer(py::module_& m) {
     m.def("qk_norm_rotate", &qk_norm_rotate, py::call_guard<py::gil_scoped_release>());
+    m.def("weighted_attention", &weighted_attention, py::call_guard<py::gil_scoped_release>());
     m.def("residual_dropout", &residual_dropout, py::call_guard<py::gil_scoped_release>());
 }
 }  // namespace sna_torch

@@ -63,6 +63,28 @@ def qk_norm_rotate(q, k, q_weight=None, k_weight=None, q_rotation=None, k_rotati
     return _sna_torch.qk_norm_rotate(q, k, q_weight, k_weight, q_lat, q_lon, k_lat, k_lon, eps, interleaved)
 
 
+def weighted_attention(q, k, v, log_weights=None, scale: float | None = None, return_lse: bool = False):
+    """Softmax attention of 16-bit tensors over all points of a grid: out_i = sum_j p_ij v_j, p_ij ~ exp(scale q_i.k_j + log_weights_j).
+
+    q [B, Hq, nlat, nlon, C], k and v [B, Hk, nlat', nlon', C], bfloat16 or float16, C a multiple of 8 up to 128, Hq a multiple of Hk:
+    query head h reads key head h // (Hq // Hk).  ``log_weights``: float32, [nlat' * nlon'] or one such row per batch; with the logarithms of
+    quadrature weights (:func:`log_quadrature_weights`) this is global spherical attention.  A point at -1e30 or below (-inf, the lowest number of any
+    type) is left out, whatever k and v hold there; a row without points gives zeros, and no gradient.  ``scale``: 1 / sqrt(C) if None.
+    Returns out, or with ``return_lse`` (out, lse): the logarithm of each row's sum, float32 [B, Hq, nlat, nlon], not differentiable.
+    Differentiable in q, k and v: the backward pass keeps out and lse and recomputes the probabilities."""
+    _check_plain(q, k, v, log_weights)
+    if scale is None:
+        scale = q.shape[-1] ** -0.5 if q.dim() and q.shape[-1] else 1.0
+    out, lse = _sna_torch.weighted_attention(q, k, v, log_weights, scale)
+    return (out, lse) if return_lse else out
+
+
+def log_quadrature_weights(plan: "sna.Plan", device="cuda") -> torch.Tensor:
+    """The logarithm of the quadrature weight of every point of a plan's input grid, float32 [nlat_in * nlon_in] (-inf for weight zero)."""
+    weights = torch.from_numpy(plan.quad_weights())
+    return weights.log().float().repeat_interleave(plan.nlon_in).to(device)
+
+
 def residual_dropout(x, state, p: float, residual=None):
     """residual + dropout(x): each value of x is kept with probability 1 - p and then divided by it, else dropped; no mask is stored.
 

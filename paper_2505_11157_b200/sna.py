@@ -52,6 +52,13 @@ class SnaTensor(ctypes.Structure):
     _fields_ = [("data", _vp), ("batch", _i64), ("head", _i64), ("lat", _i64), ("lon", _i64)]
 
 
+class SnaAttention(ctypes.Structure):
+    """sna_attention_t: a problem of sna_attention_forward / _backward."""
+    _fields_ = ([(n, _i) for n in ("B", "Hq", "Hk", "C", "nlat_q", "nlon_q", "nlat_k", "nlon_k")]
+                + [(n, SnaTensor) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
+                + [("lse", _vp), ("log_weights", _vp), ("log_weights_batch", _i64), ("scale", _f)])
+
+
 class SnaRotate(ctypes.Structure):
     """sna_rotate_t: one tensor of sna_norm_rotate_forward / _backward."""
     _fields_ = [("nlat", _i), ("nlon", _i), ("H", _i), ("x", SnaTensor), ("y", SnaTensor), ("dy", SnaTensor), ("dx", SnaTensor),
@@ -90,6 +97,10 @@ _SIGNATURES = {
     "sna_norm_rotate_forward": (_i, [ctypes.POINTER(SnaRotate), _i, _i, _i, _i, _f, _i, _vp]),
     "sna_norm_rotate_workspace_bytes": (_sz, [_i]),
     "sna_norm_rotate_backward": (_i, [ctypes.POINTER(SnaRotate), _i, _i, _i, _i, _f, _i, _vp, _sz, _vp]),
+    "sna_attention_forward_workspace_bytes": (_sz, [ctypes.POINTER(SnaAttention), _i]),
+    "sna_attention_forward": (_i, [ctypes.POINTER(SnaAttention), _i, _vp, _sz, _vp]),
+    "sna_attention_backward_workspace_bytes": (_sz, [ctypes.POINTER(SnaAttention), _i]),
+    "sna_attention_backward": (_i, [ctypes.POINTER(SnaAttention), _i, _vp, _sz, _vp]),
     "sna_dropout": (_i, [_vp, _vp, _vp, _i, _i64, _d, _vp, _vp]),
     "sna_measure_fp32_fma_peak": (_i, [ctypes.POINTER(ctypes.c_double)]),
     "sna_status_string": (ctypes.c_char_p, [_i]),
