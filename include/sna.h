@@ -380,6 +380,10 @@ typedef struct {
     float scale;                   /* of the scores; 1 / sqrt(C) usually */
 } sna_attention_t;
 
+/* Waits for the current device to finish and reports whether a kernel of sna_attention_* there gave up on one of its bounded waits since the
+ * last check (SNA_ERR_CUDA; its outputs would be incomplete), as sna_plan_check does for a plan.  Not expected to happen. */
+sna_status_t sna_layer_check(void);
+
 /* workspace: device, 256-byte aligned, private to the call until its work has finished; at least the bytes that the query gives for the same
  * problem on the current device (0: it may be NULL).  The queries return 0 for invalid arguments. */
 size_t sna_attention_forward_workspace_bytes(const sna_attention_t* a, sna_dtype_t dtype);

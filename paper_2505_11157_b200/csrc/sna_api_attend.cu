@@ -1,4 +1,6 @@
 // C ABI of the 16-bit attention (declared in include/sna.h): checks of arguments and the choice of kernels.
+#include <algorithm>
+
 #include "sna_attend.cuh"
 
 namespace sna {
@@ -50,6 +52,14 @@ sna_status_t check_workspace(const void* workspace, size_t bytes, size_t need) {
     return SNA_OK;
 }
 
+// The tcgen05 kernels take tiles of 128 (forward: two of them) rows and blocks of 128 points.
+bool on_tensor_memory(const Problem& p) { return p.Nq > 64 && p.Nk >= 128; }
+int splits_of(const Problem& p, int sms) {
+    if (!on_tensor_memory(p)) return forward_splits(p, sms);
+    const int64_t tiles = (int64_t)p.B * p.Hq * ((p.Nq + 255) / 256), blocks = (p.Nk + 127) / 128;
+    return tiles >= sms ? 1 : (int)std::max<int64_t>(1, std::min(blocks / 2, sms / tiles));
+}
+
 size_t forward_bytes(const Problem& p, int splits) { return splits > 1 ? align256((size_t)splits * rows_of(p) * (1 + p.C) * sizeof(float)) : 0; }
 size_t backward_bytes(const Problem& p) { return 2 * align256((size_t)rows_of(p) * sizeof(float)) + align256((size_t)p.B * p.Hk * 2 * sizeof(uint32_t)); }
 
@@ -64,7 +74,7 @@ extern "C" {
 size_t sna_attention_forward_workspace_bytes(const sna_attention_t* a, sna_dtype_t dtype) {
     Problem p;
     if (describe(a, dtype, false, p) != SNA_OK) return 0;
-    return forward_bytes(p, forward_splits(p, sna::sms_of_current_device()));
+    return forward_bytes(p, splits_of(p, sna::sms_of_current_device()));
 }
 
 sna_status_t sna_attention_forward(const sna_attention_t* a, sna_dtype_t dtype, void* workspace, size_t workspace_bytes, void* cuda_stream) {
@@ -74,10 +84,14 @@ sna_status_t sna_attention_forward(const sna_attention_t* a, sna_dtype_t dtype, 
     if (rows_of(p) == 0) return SNA_OK;
     const int sms = sna::sms_of_current_device();
     if (sms == 0) return sna::fail(SNA_ERR_CUDA, "no CUDA device");
-    const int splits = forward_splits(p, sms);
+    const int splits = splits_of(p, sms);
     st = check_workspace(workspace, workspace_bytes, forward_bytes(p, splits));
     if (st != SNA_OK) return st;
-    const cudaError_t e = launch_forward(p, dtype, splits, static_cast<float*>(workspace), (cudaStream_t)cuda_stream);
+    cudaStream_t stream = (cudaStream_t)cuda_stream;
+    float* partials = static_cast<float*>(workspace);
+    cudaError_t e = cudaSuccess;
+    if (!on_tensor_memory(p) || !forward_tc(p, dtype, splits, partials, stream, e)) e = launch_forward(p, dtype, splits, partials, stream);
+    if (e == cudaSuccess && splits > 1) e = launch_join(p, dtype, splits, partials, stream);
     if (e != cudaSuccess) return sna::fail(SNA_ERR_CUDA, "attention launch: %s", cudaGetErrorString(e));
     return SNA_OK;
 }
@@ -103,9 +117,18 @@ sna_status_t sna_attention_backward(const sna_attention_t* a, sna_dtype_t dtype,
     s.D = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256((size_t)rows_of(p) * sizeof(float)));
     s.norms = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + 2 * align256((size_t)rows_of(p) * sizeof(float)));
     cudaError_t e = launch_statistics(p, s, dtype, stream);
-    if (e == cudaSuccess && queries) e = launch_backward_dq(p, s, dtype, stream);
-    if (e == cudaSuccess && keys) e = launch_backward_dkdv(p, s, dtype, stream);
+    const bool on_tc = on_tensor_memory(p);
+    if (e == cudaSuccess && queries && (!on_tc || !backward_dq_tc(p, s, dtype, stream, e))) e = launch_backward_dq(p, s, dtype, stream);
+    if (e == cudaSuccess && keys && (!on_tc || !backward_dkdv_tc(p, s, dtype, stream, e))) e = launch_backward_dkdv(p, s, dtype, stream);
     if (e != cudaSuccess) return sna::fail(SNA_ERR_CUDA, "attention backward launch: %s", cudaGetErrorString(e));
+    return SNA_OK;
+}
+
+sna_status_t sna_layer_check(void) {
+    int status = 0;
+    const cudaError_t e = read_status(&status);
+    if (e != cudaSuccess) return sna::fail(SNA_ERR_CUDA, "reading the status word: %s", cudaGetErrorString(e));
+    if (status != 0) return sna::fail(SNA_ERR_CUDA, "a kernel gave up on a bounded wait; its outputs are incomplete");
     return SNA_OK;
 }
 

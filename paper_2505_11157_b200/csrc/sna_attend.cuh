@@ -37,11 +37,29 @@ struct Stats {
 template <typename T> constexpr float SHIFT = 0.f;
 template <> constexpr float SHIFT<__half> = 14.f;
 
+#ifdef __CUDACC__
+// The power of two that ds is held times.  The probabilities in it are already held times 2^SHIFT; with |t - D| <= bound the products stay below 2^15.
+template <typename T>
+__device__ __forceinline__ float ds_scale(const Stats& s, int bk) {
+    if (SHIFT<T> == 0.f) return 1.f;
+    const float bound = 2.f * __uint_as_float(s.norms[bk * 2]) * __uint_as_float(s.norms[bk * 2 + 1]);
+    if (!(bound > 0.f && bound < INFINITY)) return 1.f;
+    return exp2f(fminf(fmaxf(-ceilf(log2f(bound)), -100.f), 100.f));
+}
+#endif
+
 inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 __host__ __device__ inline int64_t rows_of(const Problem& p) { return (int64_t)p.B * p.Hq * p.Nq; }
 
+// tcgen05 kernels (sna_kernels_attend_tc.cu).  False: the driver refuses a map of one of the tensors (heads that share memory, say).
+bool forward_tc(const Problem& p, sna_dtype_t dtype, int splits, float* partials, cudaStream_t stream, cudaError_t& e);
+bool backward_dq_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream, cudaError_t& e);
+bool backward_dkdv_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream, cudaError_t& e);
+cudaError_t read_status(int* status);
+
 // mma.sync kernels (sna_kernels_attend.cu)
 int forward_splits(const Problem& p, int sms);
+cudaError_t launch_join(const Problem& p, sna_dtype_t dtype, int splits, const float* partials, cudaStream_t stream);
 cudaError_t launch_forward(const Problem& p, sna_dtype_t dtype, int splits, float* partials, cudaStream_t stream);
 cudaError_t launch_statistics(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream);
 cudaError_t launch_backward_dq(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream);

@@ -112,12 +112,13 @@ __device__ __forceinline__ float weight2(const float* weights, int n) {
 
 template <int CP, int WM> constexpr int forward_smem() { return WM * 16 * CP * 2 + 4 * BN * CP * 2; }
 
-// WM warps along the rows, WK = 4 / WM along the keys of a block.  partials: null, or [splits][rows] statistics and [splits][rows][C] sums.
+// WM warps along the rows, WK = 4 / WM along the keys of a block.  partials: null, or sums [splits][rows][C] (first, so that vectors stay aligned) and statistics
+// [splits][rows].
 template <typename T, int CP, int WM>
 __global__ void __launch_bounds__(THREADS) attend_forward_kernel(const __grid_constant__ Problem p, int tiles, int splits, float* partials) {
     constexpr int WK = WARPS / WM, BM = 16 * WM, KW = BN / WK, NT = KW / 8, CN = CP / 8;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ float bias[4][BN];
+    __shared__ __align__(16) float bias[4][BN];
     const uint32_t tq = s32(smem), tkv = tq + BM * CP * 2;      // stages of (K, V)
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wm = warp % WM, wk = warp / WM;
     const int split = blockIdx.x % splits, rest = blockIdx.x / splits, tile = rest % tiles, bh = rest / tiles;
@@ -265,11 +266,11 @@ __global__ void __launch_bounds__(THREADS) attend_forward_kernel(const __grid_co
                 float sum = 0.f;
 #pragma unroll
                 for (int w = 0; w < WARPS; ++w) sum += factor[w] * join[(w * 16 + r) * PITCH + c];
-                if (partials != nullptr) partials[(int64_t)splits * rows_of(p) + ((int64_t)split * rows_of(p) + at) * p.C + c] = sum * inverse;
+                if (partials != nullptr) partials[((int64_t)split * rows_of(p) + at) * p.C + c] = sum * inverse;
                 else static_cast<T*>(p.out.data)[b * p.out.batch + (int64_t)(hk * p.G + g) * p.out.head + (int64_t)(row - g * p.Nq) * p.out.point + c] = from_float<T>(sum * inverse);
             }
             if (lane == 0) {
-                if (partials != nullptr) partials[(int64_t)split * rows_of(p) + at] = lse2;
+                if (partials != nullptr) partials[splits * rows_of(p) * p.C + split * rows_of(p) + at] = lse2;
                 else if (p.lse != nullptr) p.lse[at] = lse2 * LN2;
             }
         }
@@ -288,11 +289,11 @@ __global__ void __launch_bounds__(THREADS) attend_forward_kernel(const __grid_co
                 const int c = n * 8 + (lane & 3) * 2;
                 if (c >= p.C) continue;
                 const float x = o[n][2 * r] * inverse, y = o[n][2 * r + 1] * inverse;
-                if (partials != nullptr) *reinterpret_cast<float2*>(partials + (int64_t)splits * rows_of(p) + ((int64_t)split * rows_of(p) + at) * p.C + c) = make_float2(x, y);
+                if (partials != nullptr) *reinterpret_cast<float2*>(partials + ((int64_t)split * rows_of(p) + at) * p.C + c) = make_float2(x, y);
                 else *reinterpret_cast<uint32_t*>(out + c) = pack<T>(x, y);
             }
             if ((lane & 3) == 0) {
-                if (partials != nullptr) partials[(int64_t)split * rows_of(p) + at] = lse2;
+                if (partials != nullptr) partials[splits * rows_of(p) * p.C + split * rows_of(p) + at] = lse2;
                 else if (p.lse != nullptr) p.lse[at] = lse2 * LN2;
             }
         }
@@ -306,19 +307,19 @@ __global__ void __launch_bounds__(THREADS) attend_join_kernel(const __grid_const
     __shared__ float totals[WARPS];
     const int64_t rows = rows_of(p), at = blockIdx.x;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const float* statistics = partials + splits * rows * p.C;
     float top = -INFINITY;
-    for (int s = lane; s < splits; s += 32) top = fmaxf(top, partials[s * rows + at]);
+    for (int s = lane; s < splits; s += 32) top = fmaxf(top, statistics[s * rows + at]);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const float base = top == -INFINITY ? 0.f : top;
     float sum[4] = {0.f, 0.f, 0.f, 0.f}, total = 0.f;
-    const float* values = partials + (int64_t)splits * rows;
     for (int s = warp; s < splits; s += WARPS) {
-        const float w = ex2(partials[s * rows + at] - base);
+        const float w = ex2(statistics[s * rows + at] - base);
         total += w;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (lane + 32 * i < p.C) sum[i] = fmaf(w, values[(s * rows + at) * p.C + lane + 32 * i], sum[i]);
+            if (lane + 32 * i < p.C) sum[i] = fmaf(w, partials[(s * rows + at) * p.C + lane + 32 * i], sum[i]);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) sums[warp][lane + 32 * i] = sum[i];
@@ -382,15 +383,6 @@ __global__ void __launch_bounds__(256) attend_statistics_kernel(const __grid_con
     }
 }
 
-// The power of two that ds is held times.  The probabilities in it are already held times 2^SHIFT; with |t - D| <= bound the products stay below 2^15.
-template <typename T>
-__device__ __forceinline__ float ds_scale(const Stats& s, int bk) {
-    if (SHIFT<T> == 0.f) return 1.f;
-    const float bound = 2.f * __uint_as_float(s.norms[bk * 2]) * __uint_as_float(s.norms[bk * 2 + 1]);
-    if (!(bound > 0.f && bound < INFINITY)) return 1.f;
-    return exp2f(fminf(fmaxf(-ceilf(log2f(bound)), -100.f), 100.f));
-}
-
 // ---- backward: dq -------------------------------------------------------------------------------------------------------------
 
 template <int CP> constexpr int dq_smem() { return 2 * 64 * CP * 2 + 4 * BN * CP * 2; }
@@ -400,7 +392,7 @@ template <typename T, int CP>
 __global__ void __launch_bounds__(THREADS) attend_dq_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats st, int tiles) {
     constexpr int BM = 64, NT = BN / 8, CN = CP / 8;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ float bias[4][BN];
+    __shared__ __align__(16) float bias[4][BN];
     const uint32_t tq = s32(smem), ty = tq + BM * CP * 2, tkv = ty + BM * CP * 2;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int tile = blockIdx.x % tiles, bh = blockIdx.x / tiles, b = bh / p.Hk, hk = bh - b * p.Hk;
@@ -523,7 +515,7 @@ template <typename T, int CP>
 __global__ void __launch_bounds__(THREADS) attend_dkdv_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats st, int tiles) {
     constexpr int BM = 64, QB = DKDV_QUERIES<CP>, NT = QB / 8, CN = CP / 8;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ float2 stats[2][QB];         // lse2, D
+    __shared__ __align__(16) float2 stats[2][QB];         // lse2, D
     const uint32_t tk = s32(smem), tv = tk + BM * CP * 2, tqy = tv + BM * CP * 2;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int tile = blockIdx.x % tiles, bh = blockIdx.x / tiles, b = bh / p.Hk, hk = bh - b * p.Hk;
@@ -649,9 +641,6 @@ cudaError_t forward_as(const Problem& p, int splits, float* partials, cudaStream
     cudaError_t e = allow(attend_forward_kernel<T, CP, WM>, forward_smem<CP, WM>());
     if (e != cudaSuccess) return e;
     attend_forward_kernel<T, CP, WM><<<(unsigned)((int64_t)p.B * p.Hk * tiles * splits), THREADS, forward_smem<CP, WM>(), stream>>>(p, tiles, splits, splits > 1 ? partials : nullptr);
-    e = cudaGetLastError();
-    if (e != cudaSuccess || splits == 1) return e;
-    attend_join_kernel<T><<<(unsigned)rows_of(p), THREADS, 0, stream>>>(p, splits, partials);
     return cudaGetLastError();
 }
 template <typename T, int CP>
@@ -683,6 +672,12 @@ int forward_splits(const Problem& p, int sms) {
     const int64_t blocks = (p.Nk + BN - 1) / BN;
     if (tiles == 0 || blocks == 0 || tiles >= 2 * sms) return 1;
     return (int)std::max<int64_t>(1, std::min(blocks / 4, 4 * sms / tiles));
+}
+
+cudaError_t launch_join(const Problem& p, sna_dtype_t dtype, int splits, const float* partials, cudaStream_t stream) {
+    if (dtype == SNA_BFLOAT16) attend_join_kernel<__nv_bfloat16><<<(unsigned)rows_of(p), THREADS, 0, stream>>>(p, splits, partials);
+    else attend_join_kernel<__half><<<(unsigned)rows_of(p), THREADS, 0, stream>>>(p, splits, partials);
+    return cudaGetLastError();
 }
 
 cudaError_t launch_forward(const Problem& p, sna_dtype_t dtype, int splits, float* partials, cudaStream_t stream) {

@@ -1,0 +1,745 @@
+// The 16-bit attention's kernels for many rows, on tcgen05 / TMEM / TMA (formulas: sna_kernels_attend.cu).
+//
+// Specialised warps run side by side, coupled by mbarriers only.  A thread of the element-wise warps owns a whole row of a tile, so that
+// maxima and sums of a row need no exchange; operands of the second products go back to TMEM as 16-bit pairs.
+//
+// Every accumulator has one issuing thread and all sums are taken in a fixed order: results are reproducible bit for bit.  Every wait is
+// bounded; one that runs out sets the device's status word (sna_layer_check), and the block leaves after another bounded wait for the copies
+// and MMAs that it has under way.
+#include <type_traits>
+
+#include "sna_attend_tc.cuh"
+
+namespace sna {
+namespace attend {
+namespace {
+
+__device__ int g_status;        // non-zero: a bounded wait has run out since the last check
+
+constexpr int TILE = 128;       // rows of a tile, points of a block
+constexpr int SLAB = TILE * 128;        // bytes of 128 points x 64 channels
+
+__device__ __forceinline__ bool all_lanes(bool ok) { return __all_sync(0xffffffffu, ok); }
+
+// ---- forward ---------------------------------------------------------------------------------------------------------------
+//
+// A block owns two tiles of 128 queries of one head and walks the keys in blocks of 128:
+//   warp 8   TMA: q once, then k and v blocks into rings of stages
+//   warp 9   MMAs: S_t = Q_t K^T of the next block after O_t += P_t V of this one, tile after tile: while one tile's products run, the other
+//            tile's softmax does (S and P share TMEM columns; MMAs of one thread are executed in order)
+//   warp 10  weights of the next block's points to shared memory; zeroes k and v rows of points left out
+//   warps 0-3 and 4-7  softmax of tile 0 and 1, thread = row: S from TMEM, P back over it.  The row's reference moves (and O is scaled in TMEM)
+//            only when its maximum has grown by 2^8: then the sums are still far from overflow, and most blocks skip the correction.
+constexpr int FWD_THREADS = 384;
+
+template <int D> struct Forward {
+    static constexpr int SLABS = D / 64, STAGES = D == 64 ? 4 : 2, TILE_BYTES = SLABS * SLAB;
+    static constexpr int OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + STAGES * TILE_BYTES;
+    static constexpr size_t SMEM = OFF_V + STAGES * TILE_BYTES + 1024;
+    static constexpr int BIAS_SLOTS = 8;        // a slot is written again when the softmax of four blocks later is under way at the earliest
+    enum { Q_FULL = 0, K_FULL = 2, V_FULL = K_FULL + STAGES, K_FREE = V_FULL + STAGES, V_FREE = K_FREE + STAGES, K_READY = V_FREE + STAGES,
+           V_READY = K_READY + STAGES, W_READY = V_READY + STAGES, S_FULL = W_READY + BIAS_SLOTS, P_READY = S_FULL + 2, O_DONE = P_READY + 2, DRAIN = O_DONE + 2, COUNT };
+};
+
+// Rounded to float16, weights up to 2^8 times the reference's must stay finite: 2^(8 + 7) < 65504.
+template <typename T> constexpr float FORWARD_SHIFT = 0.f;
+template <> constexpr float FORWARD_SHIFT<__half> = 7.f;
+constexpr float GROWTH = 8.f;
+
+template <typename T, int D, bool WEIGHTS>
+__global__ void __launch_bounds__(FWD_THREADS, 1)
+attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                         const __grid_constant__ CUtensorMap map_v, int tiles, int splits, float* partials) {
+    using F = Forward<D>;
+    extern __shared__ unsigned char raw[];
+    unsigned char* base = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+    __shared__ unsigned long long bars[F::COUNT];
+    __shared__ __align__(16) float bias[WEIGHTS ? F::BIAS_SLOTS : 1][TILE];
+    __shared__ uint32_t tmem_s;
+    __shared__ int fail_s;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int split = blockIdx.x % splits, rest = blockIdx.x / splits, tile = rest % tiles, bh = rest / tiles;
+    const int b = bh / p.Hq, h = bh - b * p.Hq, hk = h / p.G;
+    const int row0 = tile * 2 * TILE, halves = row0 + TILE < p.Nq ? 2 : 1;
+    const int blocks = (p.Nk + TILE - 1) / TILE;
+    const int first = (int)((int64_t)blocks * split / splits), count = (int)((int64_t)blocks * (split + 1) / splits) - first;
+    const int steps = (p.C + 15) / 16, slabs = (p.C + 63) / 64;
+    auto bar = [&](int i) { return s32(&bars[i]); };
+
+    if (tid == 0) {
+        for (int i = 0; i < F::COUNT; ++i) mb_init(bar(i), i >= F::P_READY && i < F::P_READY + 2 ? 128 : 1);
+        fail_s = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s32(&tmem_s)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tm_before();
+    __syncthreads();
+    tm_after();
+    const uint32_t tm = tmem_s;
+    bool ok = true;
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (warp == 8 && elect_one()) {
+            // ---------------------------------------------------------------- TMA
+            for (int t = 0; t < halves; ++t) {
+                mb_expect(bar(F::Q_FULL + t), slabs * SLAB);
+                for (int s = 0; s < slabs; ++s) tma_load(s32(base) + t * F::TILE_BYTES + s * SLAB, &map_q, s * 64, row0 + t * TILE, h, b, bar(F::Q_FULL + t));
+            }
+            int it = 0;
+            for (; it < count && ok; ++it) {
+                const int st = it % F::STAGES, turn = it / F::STAGES;
+                if (turn > 0) ok = mb_wait(bar(F::K_FREE + st), (turn - 1) & 1, ok);
+                if (!ok) break;
+                mb_expect(bar(F::K_FULL + st), slabs * SLAB);
+                for (int s = 0; s < slabs; ++s) tma_load(s32(base) + F::OFF_K + st * F::TILE_BYTES + s * SLAB, &map_k, s * 64, (first + it) * TILE, hk, b, bar(F::K_FULL + st));
+                if (turn > 0) ok = mb_wait(bar(F::V_FREE + st), (turn - 1) & 1, ok);
+                if (!ok) break;
+                mb_expect(bar(F::V_FULL + st), slabs * SLAB);
+                for (int s = 0; s < slabs; ++s) tma_load(s32(base) + F::OFF_V + st * F::TILE_BYTES + s * SLAB, &map_v, s * 64, (first + it) * TILE, hk, b, bar(F::V_FULL + st));
+            }
+            // the copies under way (all there already if all went well)
+            for (int t = 0; t < halves; ++t) mb_wait(bar(F::Q_FULL + t), 0, true);
+            for (int back = 0; back <= F::STAGES && back <= it; ++back) {
+                const int i = it - back, st = i % F::STAGES, turn = i / F::STAGES;
+                if (i >= count) continue;
+                mb_wait(bar(F::K_FULL + st), turn & 1, i < it || !ok);
+                if (i < it) mb_wait(bar(F::V_FULL + st), turn & 1, true);
+            }
+        } else if (warp == 9 && elect_one()) {
+            // ---------------------------------------------------------------- MMAs
+            const uint32_t ids = idesc<T>(TILE, false), ido = idesc<T>(steps * 16, true);
+            auto scores = [&](int t, int st) {
+                for (int ks = 0; ks < steps; ++ks)
+                    mma_ss(tm + t * TILE, desc_channels(s32(base) + t * F::TILE_BYTES + (ks >> 2) * SLAB + (ks & 3) * 32),
+                           desc_channels(s32(base) + F::OFF_K + st * F::TILE_BYTES + (ks >> 2) * SLAB + (ks & 3) * 32), ids, ks > 0);
+                mma_commit(bar(F::S_FULL + t));
+            };
+            if (count > 0) {
+                ok = mb_wait(bar((WEIGHTS ? F::K_READY : F::K_FULL) + 0), 0, ok);
+                for (int t = 0; t < halves && ok; ++t) {
+                    ok = mb_wait(bar(F::Q_FULL + t), 0, ok);
+                    if (ok) scores(t, 0);
+                }
+                mma_commit(bar(F::K_FREE));
+            }
+            for (int it = 0; it < count && ok; ++it) {
+                const int st = it % F::STAGES, next = (it + 1) % F::STAGES;
+                ok = mb_wait(bar((WEIGHTS ? F::V_READY : F::V_FULL) + st), (it / F::STAGES) & 1, ok);
+                for (int t = 0; t < halves && ok; ++t) {
+                    ok = mb_wait(bar(F::P_READY + t), it & 1, ok);
+                    if (!ok) break;
+                    tm_after();
+#pragma unroll
+                    for (int kk = 0; kk < TILE / 16; ++kk)
+                        mma_ts(tm + 256 + t * D, tm + t * TILE + kk * 8, desc_points(s32(base) + F::OFF_V + st * F::TILE_BYTES + kk * 2048, SLAB), ido, it > 0 || kk > 0);
+                    mma_commit(bar(F::O_DONE + t));
+                    if (it + 1 < count) {
+                        if (t == 0) ok = mb_wait(bar((WEIGHTS ? F::K_READY : F::K_FULL) + next), ((it + 1) / F::STAGES) & 1, ok);
+                        if (ok) scores(t, next);
+                    }
+                }
+                mma_commit(bar(F::V_FREE + st));
+                if (it + 1 < count) mma_commit(bar(F::K_FREE + next));
+            }
+            mma_commit(bar(F::DRAIN));
+            mb_wait(bar(F::DRAIN), 0, true);
+        } else if (WEIGHTS && warp == 10) {
+            // ---------------------------------------------------------------- weights
+            const float* weights = p.log_weights == nullptr ? nullptr : p.log_weights + b * p.log_weights_batch;
+            float w[4];
+            auto fetch = [&](int it) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int n = (first + it) * TILE + i * 32 + lane;
+                    w[i] = n < p.Nk ? weight2(weights, n) : -INFINITY;
+                }
+            };
+            if (count > 0) fetch(0);
+            for (int it = 0; it < count && ok; ++it) {
+                const int st = it % F::STAGES, slot = it % F::BIAS_SLOTS;
+                const uint32_t phase = (it / F::STAGES) & 1;
+                uint32_t gone[4], any = 0;
+                float now[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    now[i] = w[i];
+                    gone[i] = __ballot_sync(0xffffffffu, w[i] == -INFINITY && (first + it) * TILE + i * 32 + lane < p.Nk);
+                    any |= gone[i];
+                }
+                if (it + 1 < count) fetch(it + 1);
+                ok = all_lanes(mb_wait(bar(F::K_FULL + st), phase, ok));
+                if (!ok) break;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) bias[slot][i * 32 + lane] = now[i];
+                if (any)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) zero_rows(base + F::OFF_K + st * F::TILE_BYTES, slabs, SLAB, i, gone[i], lane);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) { mb_arrive(bar(F::W_READY + slot)); mb_arrive(bar(F::K_READY + st)); }
+                ok = all_lanes(mb_wait(bar(F::V_FULL + st), phase, ok));
+                if (!ok) break;
+                if (any)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) zero_rows(base + F::OFF_V + st * F::TILE_BYTES, slabs, SLAB, i, gone[i], lane);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mb_arrive(bar(F::V_READY + st));
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        const int t = warp >> 2;
+        if (t < halves) {
+            // ------------------------------------------------------------ softmax
+            const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+            const uint32_t ts = tm + t * TILE + lanes, to = tm + 256 + t * D + lanes;
+            const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2);
+            float ref = -INFINITY, l = 0.f;
+            for (int it = 0; it < count && ok; ++it) {
+                uint32_t s[TILE];
+                ok = all_lanes(mb_wait(bar(F::S_FULL + t), it & 1, ok));
+                if (WEIGHTS) ok = all_lanes(mb_wait(bar(F::W_READY + it % F::BIAS_SLOTS), (it / F::BIAS_SLOTS) & 1, ok)) && ok;
+                if (!ok) break;
+                tm_after();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tm_ld32(s + 32 * c, ts + 32 * c);
+                tm_ld_wait();
+                if (WEIGHTS) {
+                    const float4* w = reinterpret_cast<const float4*>(bias[WEIGHTS ? it % F::BIAS_SLOTS : 0]);
+#pragma unroll
+                    for (int i = 0; i < TILE / 4; ++i) {
+                        const float4 wi = w[i];
+                        float x[4];
+                        unpack2(fma2(pack2(__uint_as_float(s[4 * i]), __uint_as_float(s[4 * i + 1])), scale2, pack2(wi.x, wi.y)), x[0], x[1]);
+                        unpack2(fma2(pack2(__uint_as_float(s[4 * i + 2]), __uint_as_float(s[4 * i + 3])), scale2, pack2(wi.z, wi.w)), x[2], x[3]);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) s[4 * i + k] = __float_as_uint(x[k]);
+                    }
+                } else if ((first + it + 1) * TILE > p.Nk) {
+                    const int there = p.Nk - (first + it) * TILE;       // (the scale is positive)
+#pragma unroll
+                    for (int i = 0; i < TILE; ++i)
+                        if (i >= there) s[i] = 0xff800000u;
+                }
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int i = 0; i < TILE; i += 8)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], fmaxf(__uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1])));
+                float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                if (!WEIGHTS) now *= p.scale_log2;
+                const bool grown = now > ref + GROWTH;       // (also the first finite maximum: the reference is -infinity until then)
+                if (__any_sync(0xffffffffu, grown)) {
+                    const float to_ref = grown ? now : ref;
+                    const float factor = grown ? ex2(ref - now) : 1.f;
+                    l *= factor;
+                    ref = to_ref;
+                    if (it > 0) {
+                        ok = all_lanes(mb_wait(bar(F::O_DONE + t), (it - 1) & 1, ok));
+                        if (!ok) break;
+                        tm_after();
+                        const uint64_t factor2 = pack2(factor, factor);
+                        for (int c = 0; c < steps * 16; c += 32) {
+                            uint32_t o[32];
+                            tm_ld32(o, to + c);
+                            tm_ld_wait();
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                float x, y;
+                                unpack2(mul2(pack2(__uint_as_float(o[i]), __uint_as_float(o[i + 1])), factor2), x, y);
+                                o[i] = __float_as_uint(x); o[i + 1] = __float_as_uint(y);
+                            }
+                            tm_st32(to + c, o);
+                        }
+                    }
+                }
+                const float off = FORWARD_SHIFT<T> - (ref == -INFINITY ? 0.f : ref);
+                const uint64_t off2 = pack2(off, off);
+                uint64_t sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t pr[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const uint64_t x2 = pack2(__uint_as_float(s[64 * c + 2 * i]), __uint_as_float(s[64 * c + 2 * i + 1]));
+                        float x, y;
+                        unpack2(WEIGHTS ? add2(x2, off2) : fma2(x2, scale2, off2), x, y);
+                        x = ex2(x); y = ex2(y);
+                        sum2[i & 1] = add2(sum2[i & 1], pack2(x, y));
+                        pr[i] = pack16<T>(x, y);
+                    }
+                    tm_st32(ts + 32 * c, pr);
+                }
+                float a0, a1, a2, a3;
+                unpack2(sum2[0], a0, a1);
+                unpack2(sum2[1], a2, a3);
+                l += (a0 + a1) + (a2 + a3);
+                tm_st_wait();
+                tm_before();
+                mb_arrive(bar(F::P_READY + t));
+            }
+            if (ok && count > 0) ok = all_lanes(mb_wait(bar(F::O_DONE + t), (count - 1) & 1, ok));
+            if (ok) {
+                tm_after();
+                const int row = row0 + t * TILE + (warp & 3) * 32 + lane;
+                const int64_t at = ((int64_t)b * p.Hq + h) * p.Nq + row;
+                const bool there = row < p.Nq;
+                const float inverse = l == 0.f ? 0.f : 1.f / l;
+                if (there) {
+                    const float lse2 = l == 0.f ? -INFINITY : ref + log2f(l) - FORWARD_SHIFT<T>;
+                    if (splits > 1) partials[splits * rows_of(p) * p.C + split * rows_of(p) + at] = lse2;
+                    else if (p.lse != nullptr) p.lse[at] = lse2 * LN2;
+                }
+                for (int c = 0; c < p.C; c += 32) {
+                    uint32_t o[32];
+                    if (count > 0) {
+                        tm_ld32(o, to + c);
+                        tm_ld_wait();
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) o[i] = 0;
+                    }
+                    if (!there) continue;
+                    if (splits > 1) {
+                        float* out = partials + ((int64_t)split * rows_of(p) + at) * p.C + c;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4)
+                            if (c + i < p.C)
+                                *reinterpret_cast<float4*>(out + i) = make_float4(__uint_as_float(o[i]) * inverse, __uint_as_float(o[i + 1]) * inverse,
+                                                                                  __uint_as_float(o[i + 2]) * inverse, __uint_as_float(o[i + 3]) * inverse);
+                    } else {
+                        T* out = static_cast<T*>(p.out.data) + b * p.out.batch + h * p.out.head + row * p.out.point + c;
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8)
+                            if (c + i < p.C) {
+                                uint32_t x[4];
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) x[k] = pack16<T>(__uint_as_float(o[i + 2 * k]) * inverse, __uint_as_float(o[i + 2 * k + 1]) * inverse);
+                                *reinterpret_cast<uint4*>(out + i) = make_uint4(x[0], x[1], x[2], x[3]);
+                            }
+                    }
+                }
+            }
+        }
+    }
+    if (!ok) atomicExch(&fail_s, 1);
+    tm_before();
+    __syncthreads();
+    if (fail_s && tid == 0) atomicExch(&g_status, 1);
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "r"(512));
+}
+
+// ---- backward -----------------------------------------------------------------------------------------------------------------
+//
+// dq and dk, dv are the same walk with the sides exchanged.  A block owns 128 rows x (queries: dq; keys: dk, dv) with their operands A1 (q or k) and
+// A2 (dout or v), and walks the other side's points in blocks of 64, B1 (k or q) and B2 (v or dout):
+//   S = A1 B1^T, T = A2 B2^T;  p = exp(S - lse), ds = p (T - D);  acc1 += ds B1 (dq or dk);  dk, dv: acc2 += p B2 (dv)
+//   warp 8   TMA of the blocks
+//   warp 9   MMAs: acc of block j, then S and T of block j + 2 into the TMEM that block j has left
+//   warp 10  dq: weights of the block's points, rows of points left out zeroed; dk, dv: lse and D of the block's queries
+//   warps 0-3 and 4-7  element-wise, blocks of even and of odd number; thread = row; ds and p go back over T and S
+// Blocks of 64 points need two buffers of S and T to keep both sides busy: 256 of the 512 columns.  An MMA of 64 columns that reads its
+// A operand from shared memory is bound by that (6 KB at 128 bytes per clock: 48 cycles instead of 32), so A1 and A2 are kept in TMEM; only for dk, dv of wide
+// heads, whose two sums take the other 256 columns, are they in shared memory.
+constexpr int BWD_THREADS = 384, BLOCK = 64, BSLAB = BLOCK * 128;
+
+template <int D, bool DKDV> struct Backward {
+    static constexpr bool A_IN_TMEM = D == 64 || !DKDV;
+    static constexpr int SLABS = D / 64, STAGES = D == 64 ? 8 : A_IN_TMEM ? 6 : 4, STAGE_BYTES = 2 * SLABS * BSLAB, A_BYTES = A_IN_TMEM ? 0 : 2 * SLABS * SLAB;
+    static constexpr size_t SMEM = A_BYTES + STAGES * STAGE_BYTES + 1024;
+    static constexpr int SLOTS = 8;         // at least the stages: a slot is written again when its block's stage is, or later
+    // TMEM columns: buffers of (S, T), sums, operands
+    static constexpr int T_BUF = 0, T_ACC = 256, T_A = T_ACC + (DKDV ? 2 : 1) * D;
+    static_assert(T_A + (A_IN_TMEM ? D : 0) <= 512, "TMEM");
+    enum { A_FULL = 0, A_READY = 1, FULL = 2, READY = FULL + STAGES, FREE = READY + STAGES, W_READY = FREE + STAGES, ST_FULL = W_READY + SLOTS, PD_READY = ST_FULL + 2,
+           ACC_DONE = PD_READY + 2, COUNT };
+};
+
+template <typename T, int D, bool DKDV, bool WEIGHTS>
+__global__ void __launch_bounds__(BWD_THREADS, 1)
+attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats stats, const __grid_constant__ CUtensorMap map_a1, const __grid_constant__ CUtensorMap map_a2,
+                          const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_b2, int tiles) {
+    using K = Backward<D, DKDV>;
+    constexpr bool COLUMNS = DKDV || WEIGHTS;           // something is read per streamed point
+    constexpr bool CLEARED = !DKDV && WEIGHTS;          // streamed points may be left out
+    extern __shared__ unsigned char raw[];
+    unsigned char* base = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
+    __shared__ unsigned long long bars[K::COUNT];
+    __shared__ __align__(16) float column[COLUMNS ? K::SLOTS : 1][DKDV ? 2 : 1][BLOCK];        // dq: weights; dk, dv: -lse, -D
+    __shared__ uint32_t tmem_s;
+    __shared__ int fail_s;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int tile = blockIdx.x % tiles, bh = blockIdx.x / tiles;
+    const int heads = DKDV ? p.Hk : p.Hq, b = bh / heads, head = bh - b * heads, hk = DKDV ? head : head / p.G;
+    const int row0 = tile * TILE, N = DKDV ? p.Nk : p.Nq, M = DKDV ? p.Nq : p.Nk;       // rows, streamed points
+    const int per_head = (M + BLOCK - 1) / BLOCK, count = DKDV ? p.G * per_head : per_head;
+    const int steps = (p.C + 15) / 16, slabs = (p.C + 63) / 64;
+    const float* weights = p.log_weights == nullptr ? nullptr : p.log_weights + b * p.log_weights_batch;
+    auto bar = [&](int i) { return s32(&bars[i]); };
+    auto stage = [&](int st) { return s32(base) + K::A_BYTES + st * K::STAGE_BYTES; };
+
+    if (tid == 0) {
+        for (int i = 0; i < K::COUNT; ++i) mb_init(bar(i), i == K::A_READY && K::A_IN_TMEM ? 256 : i >= K::PD_READY && i < K::PD_READY + 2 ? 128 : 1);
+        fail_s = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s32(&tmem_s)), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    tm_before();
+    __syncthreads();
+    tm_after();
+    const uint32_t tm = tmem_s;
+    bool ok = true;
+
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (warp == 8 && elect_one()) {
+            // ---------------------------------------------------------------- TMA
+            if (!K::A_IN_TMEM) {
+                mb_expect(bar(K::A_FULL), 2 * slabs * SLAB);
+                for (int s = 0; s < slabs; ++s) {
+                    tma_load(s32(base) + s * SLAB, &map_a1, s * 64, row0, head, b, bar(K::A_FULL));
+                    tma_load(s32(base) + (K::SLABS + s) * SLAB, &map_a2, s * 64, row0, head, b, bar(K::A_FULL));
+                }
+            }
+            int it = 0;
+            for (; it < count; ++it) {
+                const int st = it % K::STAGES, turn = it / K::STAGES;
+                if (turn > 0) ok = mb_wait(bar(K::FREE + st), (turn - 1) & 1, ok);
+                if (!ok) break;
+                const int g = DKDV ? it / per_head : 0, point = (it - g * per_head) * BLOCK, h = DKDV ? head * p.G + g : hk;
+                mb_expect(bar(K::FULL + st), 2 * slabs * BSLAB);
+                for (int s = 0; s < slabs; ++s) {
+                    tma_load(stage(st) + s * BSLAB, &map_b1, s * 64, point, h, b, bar(K::FULL + st));
+                    tma_load(stage(st) + (K::SLABS + s) * BSLAB, &map_b2, s * 64, point, h, b, bar(K::FULL + st));
+                }
+            }
+            // the copies under way (all there already if all went well)
+            if (!K::A_IN_TMEM) mb_wait(bar(K::A_FULL), 0, true);
+            for (int i = max(0, it - K::STAGES); i < it; ++i) mb_wait(bar(K::FULL + i % K::STAGES), (i / K::STAGES) & 1, true);
+        } else if (warp == 9 && elect_one()) {
+            // ---------------------------------------------------------------- MMAs
+            const uint32_t ids = idesc<T>(BLOCK, false), ido = idesc<T>(steps * 16, true);
+            auto ready = [&](int it) { return mb_wait(bar((CLEARED ? K::READY : K::FULL) + it % K::STAGES), (it / K::STAGES) & 1, ok); };
+            auto first = [&](int it) {
+                const uint32_t at = stage(it % K::STAGES), to = tm + K::T_BUF + (it & 1) * 2 * BLOCK;
+#pragma unroll
+                for (int which = 0; which < 2; ++which)
+                    for (int ks = 0; ks < steps; ++ks) {
+                        const uint64_t bd = desc_channels(at + (which * K::SLABS + (ks >> 2)) * BSLAB + (ks & 3) * 32);
+                        if (K::A_IN_TMEM) mma_ts(to + which * BLOCK, tm + K::T_A + which * (D / 2) + ks * 8, bd, ids, ks > 0);
+                        else mma_ss(to + which * BLOCK, desc_channels(s32(base) + (which * K::SLABS + (ks >> 2)) * SLAB + (ks & 3) * 32), bd, ids, ks > 0);
+                    }
+                mma_commit(bar(K::ST_FULL + (it & 1)));
+            };
+            ok = mb_wait(bar(K::A_IN_TMEM || (DKDV && WEIGHTS) ? K::A_READY : K::A_FULL), 0, ok);
+            tm_after();
+            for (int it = 0; it < 2 && it < count && ok; ++it) {
+                ok = ready(it);
+                if (ok) first(it);
+            }
+            for (int it = 0; it < count && ok; ++it) {
+                const uint32_t at = stage(it % K::STAGES), from = tm + K::T_BUF + (it & 1) * 2 * BLOCK;
+                ok = mb_wait(bar(K::PD_READY + (it & 1)), (it >> 1) & 1, ok);
+                if (!ok) break;
+                tm_after();
+#pragma unroll
+                for (int kk = 0; kk < BLOCK / 16; ++kk) {
+                    mma_ts(tm + K::T_ACC, from + BLOCK + kk * 8, desc_points(at + kk * 2048, BSLAB), ido, it > 0 || kk > 0);
+                    if (DKDV) mma_ts(tm + K::T_ACC + D, from + kk * 8, desc_points(at + K::SLABS * BSLAB + kk * 2048, BSLAB), ido, it > 0 || kk > 0);
+                }
+                mma_commit(bar(K::FREE + it % K::STAGES));
+                if (it + 2 < count) {
+                    ok = ready(it + 2);
+                    if (ok) first(it + 2);
+                }
+            }
+            mma_commit(bar(K::ACC_DONE));
+            mb_wait(bar(K::ACC_DONE), 0, true);
+        } else if (COLUMNS && warp == 10) {
+            // ---------------------------------------------------------------- what is read per streamed point
+            if (!K::A_IN_TMEM && WEIGHTS) {
+                ok = all_lanes(mb_wait(bar(K::A_FULL), 0, ok));
+                for (int r = 0; r < 4 && ok; ++r) {
+                    const int n = row0 + r * 32 + lane;
+                    const uint32_t gone = __ballot_sync(0xffffffffu, n < p.Nk && weight2(weights, n) == -INFINITY);
+                    for (int which = 0; which < 2; ++which) zero_rows(base + which * K::SLABS * SLAB, slabs, SLAB, r, gone, lane);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mb_arrive(bar(K::A_READY));
+            }
+            float x[2], y[2];
+            auto fetch = [&](int it) {
+                const int g = DKDV ? it / per_head : 0;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int n = (it - g * per_head) * BLOCK + i * 32 + lane;
+                    if (DKDV) {
+                        const int64_t at = ((int64_t)b * p.Hq + head * p.G + g) * p.Nq + n;
+                        x[i] = n < M ? -stats.lse2[at] : -INFINITY;
+                        y[i] = n < M ? -stats.D[at] : 0.f;
+                    } else {
+                        x[i] = n < M ? weight2(weights, n) : -INFINITY;
+                        y[i] = 0.f;
+                    }
+                }
+            };
+            fetch(0);
+            for (int it = 0; it < count && ok; ++it) {
+                const int st = it % K::STAGES, slot = it % K::SLOTS;
+                float now[2], also[2];
+                uint32_t gone[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    now[i] = x[i]; also[i] = y[i];
+                    gone[i] = CLEARED ? __ballot_sync(0xffffffffu, x[i] == -INFINITY && it * BLOCK + i * 32 + lane < M) : 0;
+                }
+                if (it + 1 < count) fetch(it + 1);
+                ok = all_lanes(mb_wait(bar(K::FULL + st), (it / K::STAGES) & 1, ok));       // (then the slot's last readers are done, too)
+                if (!ok) break;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    column[slot][0][i * 32 + lane] = now[i];
+                    if (DKDV) column[slot][DKDV ? 1 : 0][i * 32 + lane] = also[i];
+                }
+                if (CLEARED) {
+                    if (gone[0] | gone[1])
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            for (int which = 0; which < 2; ++which)
+                                zero_rows(base + K::A_BYTES + st * K::STAGE_BYTES + which * K::SLABS * BSLAB, slabs, BSLAB, i, gone[i], lane);
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                }
+                __syncwarp();
+                if (lane == 0) {
+                    mb_arrive(bar(K::W_READY + slot));
+                    if (CLEARED) mb_arrive(bar(K::READY + st));
+                }
+            }
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        const int group = warp >> 2, row = row0 + (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        const bool there = row < N;
+        // ---------------------------------------------------------------- operands: group 0 those of S, group 1 those of T
+        float w = 0.f;          // dk, dv: the row's weight
+        if (DKDV && WEIGHTS) w = there ? weight2(weights, row) : -INFINITY;
+        if (K::A_IN_TMEM) {
+            const View& v = DKDV ? (group == 0 ? p.k : p.v) : (group == 0 ? p.q : p.dout);
+            const uint4* from = reinterpret_cast<const uint4*>(static_cast<const T*>(v.data) + b * v.batch + head * v.head + (there ? row : 0) * v.point);
+            const bool take = there && w != -INFINITY;
+#pragma unroll
+            for (int half = 0; half < D / 64; ++half) {
+                uint32_t x[32];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const uint4 q = take && half * 64 + i * 8 < p.C ? from[half * 8 + i] : make_uint4(0, 0, 0, 0);
+                    x[4 * i] = q.x; x[4 * i + 1] = q.y; x[4 * i + 2] = q.z; x[4 * i + 3] = q.w;
+                }
+                tm_st32(tm + K::T_A + group * (D / 2) + half * 32 + lanes, x);
+            }
+            tm_st_wait();
+            tm_before();
+            mb_arrive(bar(K::A_READY));
+        }
+        const float factor = ds_scale<T>(stats, b * p.Hk + hk);
+        float neg_lse = 0.f, neg_D = 0.f;       // dq: the row's
+        if (!DKDV && there) {
+            const int64_t at = ((int64_t)b * p.Hq + head) * p.Nq + row;
+            neg_lse = -stats.lse2[at];
+            neg_D = -stats.D[at];
+        }
+        const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), row_x = DKDV ? pack2(w, w) : pack2(neg_lse, neg_lse), row_D = pack2(neg_D, neg_D), factor2 = pack2(factor, factor);
+        for (int it = group; it < count && ok; it += 2) {
+            const uint32_t from = tm + K::T_BUF + group * 2 * BLOCK + lanes;
+            uint32_t s[BLOCK], t[BLOCK];
+            ok = all_lanes(mb_wait(bar(K::ST_FULL + group), (it >> 1) & 1, ok));
+            if (COLUMNS) ok = all_lanes(mb_wait(bar(K::W_READY + it % K::SLOTS), (it / K::SLOTS) & 1, ok)) && ok;
+            if (!ok) break;
+            tm_after();
+            tm_ld32(s, from);
+            tm_ld32(s + 32, from + 32);
+            tm_ld32(t, from + BLOCK);
+            tm_ld32(t + 32, from + BLOCK + 32);
+            tm_ld_wait();
+            if (!COLUMNS && (it + 1) * BLOCK > M) {
+                // points that are not there: zero rows, whose probability must not overflow (the scale is positive)
+                const int left = M - it * BLOCK;
+#pragma unroll
+                for (int i = 0; i < BLOCK; ++i)
+                    if (i >= left) s[i] = 0xff800000u;
+            }
+            const float4* c0 = reinterpret_cast<const float4*>(column[COLUMNS ? it % K::SLOTS : 0][0]);
+            const float4* c1 = reinterpret_cast<const float4*>(column[COLUMNS ? it % K::SLOTS : 0][DKDV ? 1 : 0]);
+            uint32_t pr[DKDV ? 32 : 1], ds[32];
+#pragma unroll
+            for (int i = 0; i < BLOCK / 4; ++i) {
+                float4 cx, cd;
+                if (COLUMNS) cx = c0[i];
+                if (DKDV) cd = c1[i];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const uint64_t s2 = pack2(__uint_as_float(s[4 * i + 2 * k]), __uint_as_float(s[4 * i + 2 * k + 1]));
+                    const uint64_t t2 = pack2(__uint_as_float(t[4 * i + 2 * k]), __uint_as_float(t[4 * i + 2 * k + 1]));
+                    uint64_t x2;
+                    if (COLUMNS) {
+                        x2 = fma2(s2, scale2, k == 0 ? pack2(cx.x, cx.y) : pack2(cx.z, cx.w));
+                        if (!DKDV || WEIGHTS) x2 = add2(x2, row_x);
+                    } else {
+                        x2 = fma2(s2, scale2, row_x);
+                    }
+                    float e0, e1;
+                    unpack2(x2, e0, e1);
+                    e0 = ex2(e0); e1 = ex2(e1);
+                    uint64_t d2 = add2(t2, DKDV ? (k == 0 ? pack2(cd.x, cd.y) : pack2(cd.z, cd.w)) : row_D);
+                    if (SHIFT<T> != 0.f) d2 = mul2(d2, factor2);
+                    float d0, d1;
+                    unpack2(mul2(d2, pack2(e0, e1)), d0, d1);
+                    if (DKDV) pr[DKDV ? 2 * i + k : 0] = pack16<T>(e0, e1);
+                    ds[2 * i + k] = pack16<T>(d0, d1);
+                }
+            }
+            if constexpr (DKDV) tm_st32(from, pr);
+            tm_st32(from + BLOCK, ds);
+            tm_st_wait();
+            tm_before();
+            mb_arrive(bar(K::PD_READY + group));
+        }
+        // ---------------------------------------------------------------- results: dq by halves of the channels, or dk by group 0 and dv by group 1
+        ok = all_lanes(mb_wait(bar(K::ACC_DONE), 0, ok)) && ok;
+        if (ok) {
+            tm_after();
+            const float unshift = ex2(-SHIFT<T>), back = DKDV && group == 1 ? unshift : p.scale * unshift / factor;
+            const View& v = DKDV ? (group == 0 ? p.dk : p.dv) : p.dq;
+            T* out = static_cast<T*>(v.data) + b * v.batch + head * v.head + (int64_t)row * v.point;
+            for (int c = DKDV ? 0 : group * 32; c < p.C; c += DKDV ? 32 : 64) {
+                uint32_t o[32];
+                tm_ld32(o, tm + K::T_ACC + (DKDV ? group * D : 0) + c + lanes);
+                tm_ld_wait();
+                if (!there) continue;
+#pragma unroll
+                for (int i = 0; i < 32; i += 8)
+                    if (c + i < p.C) {
+                        uint32_t x[4];
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) x[k] = pack16<T>(__uint_as_float(o[i + 2 * k]) * back, __uint_as_float(o[i + 2 * k + 1]) * back);
+                        *reinterpret_cast<uint4*>(out + c + i) = make_uint4(x[0], x[1], x[2], x[3]);
+                    }
+            }
+        }
+    }
+    if (!ok) atomicExch(&fail_s, 1);
+    tm_before();
+    __syncthreads();
+    if (fail_s && tid == 0) atomicExch(&g_status, 1);
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "r"(512));
+}
+
+using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
+                            CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+Encode encoder() {
+    static const Encode fn = [] {
+        void* symbol = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &symbol, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) symbol = nullptr;
+        return reinterpret_cast<Encode>(symbol);
+    }();
+    return fn;
+}
+
+template <typename K>
+cudaError_t allow(K kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); }
+
+template <typename T, int D, bool WEIGHTS>
+cudaError_t forward_as(const Problem& p, const CUtensorMap (&maps)[3], int splits, float* partials, cudaStream_t stream) {
+    const int tiles = (p.Nq + 2 * TILE - 1) / (2 * TILE);
+    const auto kernel = attend_forward_tc_kernel<T, D, WEIGHTS>;
+    const cudaError_t e = allow(kernel, Forward<D>::SMEM);
+    if (e != cudaSuccess) return e;
+    kernel<<<(unsigned)((int64_t)p.B * p.Hq * tiles * splits), FWD_THREADS, Forward<D>::SMEM, stream>>>(p, maps[0], maps[1], maps[2], tiles, splits, partials);
+    return cudaGetLastError();
+}
+
+template <typename T, int D, bool DKDV, bool WEIGHTS>
+cudaError_t backward_as(const Problem& p, const Stats& s, const CUtensorMap (&maps)[4], cudaStream_t stream) {
+    const int tiles = ((DKDV ? p.Nk : p.Nq) + TILE - 1) / TILE;
+    const auto kernel = attend_backward_tc_kernel<T, D, DKDV, WEIGHTS>;
+    const cudaError_t e = allow(kernel, Backward<D, DKDV>::SMEM);
+    if (e != cudaSuccess) return e;
+    kernel<<<(unsigned)((int64_t)p.B * (DKDV ? p.Hk : p.Hq) * tiles), BWD_THREADS, Backward<D, DKDV>::SMEM, stream>>>(p, s, maps[0], maps[1], maps[2], maps[3], tiles);
+    return cudaGetLastError();
+}
+template <bool DKDV>
+bool backward_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream, cudaError_t& e) {
+    CUtensorMap maps[4];        // A1, A2 (boxes of a tile), B1, B2 (of a block)
+    const int q_rows = DKDV ? BLOCK : TILE, k_rows = DKDV ? TILE : BLOCK, q_at = DKDV ? 2 : 0, k_at = 2 - q_at;
+    if (!make_map(&maps[q_at], p.q, dtype, p.C, p.Nq, p.Hq, p.B, q_rows) || !make_map(&maps[q_at + 1], p.dout, dtype, p.C, p.Nq, p.Hq, p.B, q_rows) ||
+        !make_map(&maps[k_at], p.k, dtype, p.C, p.Nk, p.Hk, p.B, k_rows) || !make_map(&maps[k_at + 1], p.v, dtype, p.C, p.Nk, p.Hk, p.B, k_rows))
+        return false;
+    const bool weights = p.log_weights != nullptr || !(p.scale > 0.f);
+    auto run = [&](auto t, auto width) {
+        using T = decltype(t);
+        constexpr int D = decltype(width)::value;
+        return weights ? backward_as<T, D, DKDV, true>(p, s, maps, stream) : backward_as<T, D, DKDV, false>(p, s, maps, stream);
+    };
+    using W64 = std::integral_constant<int, 64>;
+    using W128 = std::integral_constant<int, 128>;
+    if (dtype == SNA_BFLOAT16) e = p.C <= 64 ? run(__nv_bfloat16(), W64()) : run(__nv_bfloat16(), W128());
+    else e = p.C <= 64 ? run(__half(), W64()) : run(__half(), W128());
+    return true;
+}
+
+}  // namespace
+
+bool backward_dq_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream, cudaError_t& e) { return backward_tc<false>(p, s, dtype, stream, e); }
+bool backward_dkdv_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream, cudaError_t& e) { return backward_tc<true>(p, s, dtype, stream, e); }
+
+bool make_map(CUtensorMap* map, const View& v, sna_dtype_t dtype, int C, int N, int H, int B, int rows) {
+    const Encode fn = encoder();
+    if (fn == nullptr) return false;
+    // (a dimension of one is never stepped over: any stride that the driver accepts will do)
+    auto bytes = [](int64_t stride, int size) { return (cuuint64_t)(size > 1 ? stride * 2 : 16); };
+    const cuuint64_t dims[4] = {(cuuint64_t)C, (cuuint64_t)N, (cuuint64_t)H, (cuuint64_t)B};
+    const cuuint64_t strides[3] = {bytes(v.point, N), bytes(v.head, H), bytes(v.batch, B)};
+    const cuuint32_t box[4] = {64, (cuuint32_t)rows, 1, 1}, steps[4] = {1, 1, 1, 1};
+    return fn(map, dtype == SNA_BFLOAT16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, v.data, dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool forward_tc(const Problem& p, sna_dtype_t dtype, int splits, float* partials, cudaStream_t stream, cudaError_t& e) {
+    CUtensorMap maps[3];
+    if (!make_map(&maps[0], p.q, dtype, p.C, p.Nq, p.Hq, p.B, TILE) || !make_map(&maps[1], p.k, dtype, p.C, p.Nk, p.Hk, p.B, TILE) ||
+        !make_map(&maps[2], p.v, dtype, p.C, p.Nk, p.Hk, p.B, TILE))
+        return false;
+    const bool weights = p.log_weights != nullptr || !(p.scale > 0.f);
+    auto run = [&](auto t, auto width) {
+        using T = decltype(t);
+        constexpr int D = decltype(width)::value;
+        return weights ? forward_as<T, D, true>(p, maps, splits, partials, stream) : forward_as<T, D, false>(p, maps, splits, partials, stream);
+    };
+    using W64 = std::integral_constant<int, 64>;
+    using W128 = std::integral_constant<int, 128>;
+    if (dtype == SNA_BFLOAT16) e = p.C <= 64 ? run(__nv_bfloat16(), W64()) : run(__nv_bfloat16(), W128());
+    else e = p.C <= 64 ? run(__half(), W64()) : run(__half(), W128());
+    return true;
+}
+
+cudaError_t read_status(int* status) {
+    cudaError_t e = cudaDeviceSynchronize();
+    if (e == cudaSuccess) e = cudaMemcpyFromSymbol(status, g_status, sizeof(int));
+    const int zero = 0;
+    if (e == cudaSuccess && *status != 0) e = cudaMemcpyToSymbol(g_status, &zero, sizeof(int));
+    return e;
+}
+
+}  // namespace attend
+}  // namespace sna

@@ -101,6 +101,7 @@ _SIGNATURES = {
     "sna_attention_forward": (_i, [ctypes.POINTER(SnaAttention), _i, _vp, _sz, _vp]),
     "sna_attention_backward_workspace_bytes": (_sz, [ctypes.POINTER(SnaAttention), _i]),
     "sna_attention_backward": (_i, [ctypes.POINTER(SnaAttention), _i, _vp, _sz, _vp]),
+    "sna_layer_check": (_i, []),
     "sna_dropout": (_i, [_vp, _vp, _vp, _i, _i64, _d, _vp, _vp]),
     "sna_measure_fp32_fma_peak": (_i, [ctypes.POINTER(ctypes.c_double)]),
     "sna_status_string": (ctypes.c_char_p, [_i]),
@@ -184,6 +185,11 @@ def sna_plan_destroy(plan: int):
 def sna_plan_check(plan: int):
     """Synchronise and raise if a kernel of this plan gave up on a bounded wait."""
     _check(_lib.sna_plan_check(plan))
+
+
+def sna_layer_check():
+    """Synchronise and raise if a kernel of the 16-bit attention gave up on a bounded wait on the current device."""
+    _check(_lib.sna_layer_check())
 
 
 def sna_plan_get_nnz(plan: int) -> int:

@@ -320,3 +320,8 @@ def test_refusals():
     out = call(q, k, v)
     with pytest.raises(RuntimeError, match="differentiable once"):
         torch.autograd.grad(out.sum(), q, create_graph=True)
+
+
+def test_no_kernel_gave_up_on_a_wait():
+    """Last in this file: every bounded wait of the calls above came to its end."""
+    sna.sna_layer_check()
