@@ -52,8 +52,9 @@ sna_status_t check_workspace(const void* workspace, size_t bytes, size_t need) {
     return SNA_OK;
 }
 
-// The tcgen05 kernels take tiles of 128 (forward: two of them) rows and blocks of 128 points.
-bool on_tensor_memory(const Problem& p) { return p.Nq > 64 && p.Nk >= 128; }
+// The tcgen05 kernels take tiles of 128 (forward: two of them) rows and blocks of 128 points.  They find a row's maximum before the scores are scaled, and
+// hold weights divided by the scale: it has to be positive, and not so small that a point left out could be taken for one with a low weight.
+bool on_tensor_memory(const Problem& p) { return p.Nq > 64 && p.Nk >= 128 && p.scale >= 0x1p-20f && p.scale <= 0x1p20f; }
 int splits_of(const Problem& p, int sms) {
     if (!on_tensor_memory(p)) return forward_splits(p, sms);
     const int64_t tiles = (int64_t)p.B * p.Hq * ((p.Nq + 255) / 256), blocks = (p.Nk + 127) / 128;

@@ -38,24 +38,37 @@ __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, i
 // Shared-memory operands: rows (points) of 128 bytes (64 channels), groups of 8 rows 1024 bytes apart, 128-byte swizzle; a second slab holds
 // the channels from 64.  The same tile serves a sum over channels (K-major: a step of 16 channels is 32 bytes further) and, as a B operand
 // whose columns are channels, a sum over points (MN-major: a step of 16 points is 2048 bytes further, the next 64 channels a slab).
-__device__ __forceinline__ uint64_t desc_channels(uint32_t addr) {
-    return (uint64_t)((addr >> 4) & 0x3fff) | ((uint64_t)1 << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+// A descriptor is held as its low half, which addresses (in units of 16 bytes) move along; the high half is the same for all of these tiles.
+constexpr uint32_t DESC_HIGH = (1024 >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_channels(uint32_t addr) { return (addr >> 4) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_points(uint32_t addr, uint32_t slab) { return (addr >> 4) | ((slab >> 4) << 16); }
+// Rows of 16 bytes without a swizzle, 8 rows 256 bytes apart, and a second half of a step's 16 channels 128 bytes further: one step of extra channels
+// beside a tile, that add a number per point to the scores (the number in three bfloat16 parts against ones: 24 bits).
+constexpr uint32_t DESC_EXTRA_HIGH = (256 >> 4) | (1u << 14);
+__device__ __forceinline__ uint32_t desc_extra(uint32_t addr) { return (addr >> 4) | ((128u >> 4) << 16); }
+__device__ __forceinline__ int extra_at(int row) { return (row >> 3) * 256 + (row & 7) * 16; }
+constexpr uint32_t EXTRA_ONES_0 = 0x3f803f80u, EXTRA_ONES_1 = 0x00003f80u;
+constexpr uint32_t EXTRA_OUT = 0x0000ff61u;        // -2.99e38: times a scale of 2^-20 or more, below any finite score of a point that takes part
+__device__ __forceinline__ uint2 extra_parts(float x) {
+    const __nv_bfloat16 hi = __float2bfloat16_rn(x);
+    const float rest = x - __bfloat162float(hi);
+    const __nv_bfloat16 mid = __float2bfloat16_rn(rest), lo = __float2bfloat16_rn(rest - __bfloat162float(mid));
+    return make_uint2((uint32_t)__bfloat16_as_ushort(hi) | ((uint32_t)__bfloat16_as_ushort(mid) << 16), __bfloat16_as_ushort(lo));
 }
-__device__ __forceinline__ uint64_t desc_points(uint32_t addr, uint32_t slab) {
-    return (uint64_t)((addr >> 4) & 0x3fff) | ((uint64_t)(slab >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-}
+
 // fp32 accumulator, both operands T, 128 rows, n columns
 template <typename T> __device__ __forceinline__ uint32_t idesc(int n, bool b_is_points) {
     const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
     return (1u << 4) | (type << 7) | (type << 10) | ((b_is_points ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, {%5, %5, %5, %5}, p;\n\t}\n"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(0u) : "memory");
+template <uint32_t HIGH = DESC_HIGH>
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}\n" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "n"(HIGH) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t acc) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}\n"
-                 ::"r"(d), "r"(a_tmem), "l"(b), "r"(idesc), "r"(acc), "r"(0u) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}\n" ::"r"(d), "r"(a_tmem), "r"(b), "r"(idesc), "r"(acc), "n"(DESC_HIGH) : "memory");
 }
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -85,6 +98,28 @@ __device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("m
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
 __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+
+// 2^x for two numbers of at most 2^6 on the FMA pipe, beside the special-function unit that ex2 uses: x = n + f with |f| <= 1/2 (Cody and Waite),
+// 2^f by the polynomial of degree 4 with the least relative error there (2.6e-6: 2^-18.5, found by iterated least squares), n added to the exponent.  Numbers below -126 count as -126; NaN and
+// infinities are not kept: the caller has to see to them.
+__device__ __forceinline__ void exp2_by_fma(uint64_t x2, float& y0, float& y1) {
+    float x0, x1;
+    unpack2(x2, x0, x1);
+    x2 = pack2(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
+    const uint64_t round2 = pack2(12582912.f, 12582912.f), back2 = pack2(-12582912.f, -12582912.f), minus2 = pack2(-1.f, -1.f);
+    const uint64_t t2 = add2(x2, round2), f2 = fma2(add2(t2, back2), minus2, x2);
+    uint64_t p2 = pack2(0.009570102f, 0.009570102f);
+    p2 = fma2(p2, f2, pack2(0.055917863f, 0.055917863f));
+    p2 = fma2(p2, f2, pack2(0.24024744f, 0.24024744f));
+    p2 = fma2(p2, f2, pack2(0.6931218f, 0.6931218f));
+    p2 = fma2(p2, f2, pack2(0.9999993f, 0.9999993f));
+    float t0, t1, p0, p1;
+    unpack2(t2, t0, t1);
+    unpack2(p2, p0, p1);
+    y0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
+    y1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
+}
+__device__ __forceinline__ float max_or_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
 
 template <typename T> __device__ __forceinline__ uint32_t pack16(float lo, float hi);
 template <> __device__ __forceinline__ uint32_t pack16<__nv_bfloat16>(float lo, float hi) {

@@ -379,7 +379,19 @@ __global__ void __launch_bounds__(256) attend_statistics_kernel(const __grid_con
             s.D[row] = lse == -INFINITY ? 0.f : dot;
             s.lse2[row] = lse == -INFINITY ? INFINITY : lse * LOG2E - SHIFT<T>;
         }
-        if (SCALED) atomicMax(s.norms + bk * 2 + (queries ? 0 : 1), __float_as_uint(sqrtf(square)));
+    }
+    if (SCALED) {
+        // one atomic per block where its rows belong to one key head (contended ones, one per row, took ten times as long as the rest)
+        __shared__ uint32_t most;
+        __shared__ int64_t head;
+        if (threadIdx.x == 0) { most = 0; head = bk; }
+        __syncthreads();
+        if (there && part == 0) {
+            if (bk == head) atomicMax(&most, __float_as_uint(sqrtf(square)));
+            else atomicMax(s.norms + bk * 2 + (queries ? 0 : 1), __float_as_uint(sqrtf(square)));
+        }
+        __syncthreads();
+        if (threadIdx.x == 0 && most != 0) atomicMax(s.norms + head * 2 + (queries ? 0 : 1), most);
     }
 }
 

@@ -20,31 +20,44 @@ constexpr int TILE = 128;       // rows of a tile, points of a block
 constexpr int SLAB = TILE * 128;        // bytes of 128 points x 64 channels
 
 __device__ __forceinline__ bool all_lanes(bool ok) { return __all_sync(0xffffffffu, ok); }
+// One arrival per warp, for what its lanes have read from or written to TMEM.  (32 arrivals on one barrier are carried out one after the other.)
+__device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
+    tm_before();
+    __syncwarp();
+    if (lane == 0) mb_arrive(bar);
+}
 
 // ---- forward ---------------------------------------------------------------------------------------------------------------
 //
 // A block owns two tiles of 128 queries of one head and walks the keys in blocks of 128:
-//   warp 8   TMA: q once, then k and v blocks into rings of stages
-//   warp 9   MMAs: S_t = Q_t K^T of the next block after O_t += P_t V of this one, tile after tile: while one tile's products run, the other
-//            tile's softmax does (S and P share TMEM columns; MMAs of one thread are executed in order)
-//   warp 10  weights of the next block's points to shared memory; zeroes k and v rows of points left out
-//   warps 0-3 and 4-7  softmax of tile 0 and 1, thread = row: S from TMEM, P back over it.  The row's reference moves (and O is scaled in TMEM)
-//            only when its maximum has grown by 2^8: then the sums are still far from overflow, and most blocks skip the correction.
+//   warp 8       TMA: q once, then k and v blocks into rings of stages
+//   warps 9, 11  MMAs of tile 0 and 1: S = Q K^T of the next block, O += P V of this one, in halves of 64 points as P gets ready
+//   warp 10      weights of the next block's points; zeroes k and v rows of points left out
+//   warps 0-3 and 4-7  softmax of tile 0 and 1, thread = row: S from TMEM, P back.  The row's reference moves (and O is scaled in TMEM)
+//                only when its maximum has grown by 2^8: then the sums are still far from overflow, and most blocks skip the correction.
+// Narrow heads leave TMEM columns for P beside S: S of the next block is then computed during this block's softmax.  Wide ones keep P
+// in S's columns; while one tile's products run, the other tile's softmax does.
+// A point's weight is one more step of the first product: its parts against ones.  (Added per element, with the weights read from shared memory, it
+// cost 40 % of the time: 64x128, B = 2, eight heads of 128, 683 us against 486 without weights.)
 constexpr int FWD_THREADS = 384;
 
 template <int D> struct Forward {
-    static constexpr int SLABS = D / 64, STAGES = D == 64 ? 4 : 2, TILE_BYTES = SLABS * SLAB;
-    static constexpr int OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + STAGES * TILE_BYTES;
-    static constexpr size_t SMEM = OFF_V + STAGES * TILE_BYTES + 1024;
-    static constexpr int BIAS_SLOTS = 8;        // a slot is written again when the softmax of four blocks later is under way at the earliest
+    static constexpr bool P_APART = D == 64;
+    static constexpr int SLABS = D / 64, STAGES = D == 64 ? 4 : 2, TILE_BYTES = SLABS * SLAB, EXTRA_BYTES = TILE * 32;
+    static constexpr int OFF_K = 2 * TILE_BYTES, OFF_V = OFF_K + STAGES * TILE_BYTES, OFF_ONES = OFF_V + STAGES * TILE_BYTES, OFF_W = OFF_ONES + EXTRA_BYTES;
+    static constexpr size_t SMEM = OFF_W + STAGES * EXTRA_BYTES + 1024;
+    // TMEM columns
+    static constexpr int T_P = P_APART ? 256 : 0, P_STEP = P_APART ? 64 : 128, T_O = P_APART ? 384 : 256;
     enum { Q_FULL = 0, K_FULL = 2, V_FULL = K_FULL + STAGES, K_FREE = V_FULL + STAGES, V_FREE = K_FREE + STAGES, K_READY = V_FREE + STAGES,
-           V_READY = K_READY + STAGES, W_READY = V_READY + STAGES, S_FULL = W_READY + BIAS_SLOTS, P_READY = S_FULL + 2, O_DONE = P_READY + 2, DRAIN = O_DONE + 2, COUNT };
+           V_READY = K_READY + STAGES, S_FULL = V_READY + STAGES, S_FREE = S_FULL + 2, P_READY = S_FREE + 2 /* [tile][half] */, O_DONE = P_READY + 4, DRAIN = O_DONE + 2, COUNT = DRAIN + 2 };
 };
 
 // Rounded to float16, weights up to 2^8 times the reference's must stay finite: 2^(8 + 7) < 65504.
 template <typename T> constexpr float FORWARD_SHIFT = 0.f;
 template <> constexpr float FORWARD_SHIFT<__half> = 7.f;
 constexpr float GROWTH = 8.f;
+constexpr int BY_FMA = 4;               // one pair of this many takes its exponentials on the FMA pipe
+constexpr float NOTHING = -1e31f;       // scores below belong to points left out
 
 template <typename T, int D, bool WEIGHTS>
 __global__ void __launch_bounds__(FWD_THREADS, 1)
@@ -54,7 +67,6 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
     extern __shared__ unsigned char raw[];
     unsigned char* base = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     __shared__ unsigned long long bars[F::COUNT];
-    __shared__ __align__(16) float bias[WEIGHTS ? F::BIAS_SLOTS : 1][TILE];
     __shared__ uint32_t tmem_s;
     __shared__ int fail_s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -67,13 +79,21 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
     auto bar = [&](int i) { return s32(&bars[i]); };
 
     if (tid == 0) {
-        for (int i = 0; i < F::COUNT; ++i) mb_init(bar(i), i >= F::P_READY && i < F::P_READY + 2 ? 128 : 1);
+        for (int i = 0; i < F::COUNT; ++i)
+            mb_init(bar(i), i >= F::S_FREE && i < F::O_DONE ? 4 : i >= F::K_FREE && i < F::K_READY ? halves : 1);
         fail_s = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s32(&tmem_s)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (WEIGHTS) {
+        // the ones, and zeros behind the weights' parts
+        for (int e = tid; e < F::EXTRA_BYTES / 16; e += FWD_THREADS)
+            *reinterpret_cast<uint4*>(base + F::OFF_ONES + e * 16) = (e & 8) ? make_uint4(0, 0, 0, 0) : make_uint4(EXTRA_ONES_0, EXTRA_ONES_1, 0, 0);
+        for (int e = tid; e < F::STAGES * F::EXTRA_BYTES / 16; e += FWD_THREADS) *reinterpret_cast<uint4*>(base + F::OFF_W + e * 16) = make_uint4(0, 0, 0, 0);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     tm_before();
     __syncthreads();
@@ -109,78 +129,94 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
                 mb_wait(bar(F::K_FULL + st), turn & 1, i < it || !ok);
                 if (i < it) mb_wait(bar(F::V_FULL + st), turn & 1, true);
             }
-        } else if (warp == 9 && elect_one()) {
+        } else if ((warp == 9 || (F::P_APART && warp == 11 && halves == 2)) && elect_one()) {
             // ---------------------------------------------------------------- MMAs
-            const uint32_t ids = idesc<T>(TILE, false), ido = idesc<T>(steps * 16, true);
-            auto scores = [&](int t, int st) {
-                for (int ks = 0; ks < steps; ++ks)
-                    mma_ss(tm + t * TILE, desc_channels(s32(base) + t * F::TILE_BYTES + (ks >> 2) * SLAB + (ks & 3) * 32),
-                           desc_channels(s32(base) + F::OFF_K + st * F::TILE_BYTES + (ks >> 2) * SLAB + (ks & 3) * 32), ids, ks > 0);
+            const uint32_t ids = idesc<T>(TILE, false), idw = idesc<__nv_bfloat16>(TILE, false), ido = idesc<T>(steps * 16, true);
+            const uint32_t dq = desc_channels(s32(base)), dk = desc_channels(s32(base) + F::OFF_K), dv = desc_points(s32(base) + F::OFF_V, SLAB);
+            const uint32_t dones = desc_extra(s32(base) + F::OFF_ONES), dw = desc_extra(s32(base) + F::OFF_W);
+            auto scores = [&](int t, int it) {
+                const int st = it % F::STAGES;
+                if (!mb_wait(bar((WEIGHTS ? F::K_READY : F::K_FULL) + st), (it / F::STAGES) & 1, true)) return false;
+                const uint32_t to = tm + t * TILE, a = dq + t * (F::TILE_BYTES >> 4), k = dk + st * (F::TILE_BYTES >> 4);
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+                    if (ks < steps) mma_ss(to, a + (ks >> 2) * (SLAB >> 4) + (ks & 3) * 2, k + (ks >> 2) * (SLAB >> 4) + (ks & 3) * 2, ids, ks > 0);
+                if (WEIGHTS) mma_ss<DESC_EXTRA_HIGH>(to, dones, dw + st * (F::EXTRA_BYTES >> 4), idw, 1);
                 mma_commit(bar(F::S_FULL + t));
+                mma_commit(bar(F::K_FREE + st));
+                return true;
             };
-            if (count > 0) {
-                ok = mb_wait(bar((WEIGHTS ? F::K_READY : F::K_FULL) + 0), 0, ok);
-                for (int t = 0; t < halves && ok; ++t) {
-                    ok = mb_wait(bar(F::Q_FULL + t), 0, ok);
-                    if (ok) scores(t, 0);
-                }
-                mma_commit(bar(F::K_FREE));
-            }
-            for (int it = 0; it < count && ok; ++it) {
-                const int st = it % F::STAGES, next = (it + 1) % F::STAGES;
-                ok = mb_wait(bar((WEIGHTS ? F::V_READY : F::V_FULL) + st), (it / F::STAGES) & 1, ok);
-                for (int t = 0; t < halves && ok; ++t) {
-                    ok = mb_wait(bar(F::P_READY + t), it & 1, ok);
-                    if (!ok) break;
+            auto values = [&](int t, int it) {
+                const int st = it % F::STAGES;
+                if (!mb_wait(bar((WEIGHTS ? F::V_READY : F::V_FULL) + st), (it / F::STAGES) & 1, true)) return false;
+                const uint32_t to = tm + F::T_O + t * D, a = tm + F::T_P + t * F::P_STEP, v = dv + st * (F::TILE_BYTES >> 4);
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    if (!mb_wait(bar(F::P_READY + 2 * t + half), it & 1, true)) return false;
                     tm_after();
 #pragma unroll
-                    for (int kk = 0; kk < TILE / 16; ++kk)
-                        mma_ts(tm + 256 + t * D, tm + t * TILE + kk * 8, desc_points(s32(base) + F::OFF_V + st * F::TILE_BYTES + kk * 2048, SLAB), ido, it > 0 || kk > 0);
-                    mma_commit(bar(F::O_DONE + t));
-                    if (it + 1 < count) {
-                        if (t == 0) ok = mb_wait(bar((WEIGHTS ? F::K_READY : F::K_FULL) + next), ((it + 1) / F::STAGES) & 1, ok);
-                        if (ok) scores(t, next);
-                    }
+                    for (int kk = 4 * half; kk < 4 * half + 4; ++kk) mma_ts(to, a + kk * 8, v + kk * (2048 >> 4), ido, it > 0 || kk > 0);
                 }
+                mma_commit(bar(F::O_DONE + t));
                 mma_commit(bar(F::V_FREE + st));
-                if (it + 1 < count) mma_commit(bar(F::K_FREE + next));
+                return true;
+            };
+            if constexpr (F::P_APART) {
+                const int t = warp == 9 ? 0 : 1;
+                ok = mb_wait(bar(F::Q_FULL + t), 0, true) && (count == 0 || scores(t, 0));
+                for (int it = 0; it < count && ok; ++it) {
+                    if (it + 1 < count) {
+                        ok = mb_wait(bar(F::S_FREE + t), it & 1, true);
+                        if (!ok) break;
+                        tm_after();
+                        ok = scores(t, it + 1);
+                    }
+                    ok = ok && values(t, it);
+                }
+            } else {
+                // (one thread for both tiles: with one each, the two softmaxes drift into step and wait together; 64x128, B = 2, eight heads of 128: 708 us)
+                for (int t = 0; t < halves && ok; ++t) ok = mb_wait(bar(F::Q_FULL + t), 0, true) && (count == 0 || scores(t, 0));
+                for (int it = 0; it < count && ok; ++it)
+                    for (int t = 0; t < halves && ok; ++t) ok = values(t, it) && (it + 1 >= count || scores(t, it + 1));
             }
-            mma_commit(bar(F::DRAIN));
-            mb_wait(bar(F::DRAIN), 0, true);
+            mma_commit(bar(F::DRAIN + (warp == 9 ? 0 : 1)));
+            mb_wait(bar(F::DRAIN + (warp == 9 ? 0 : 1)), 0, true);
         } else if (WEIGHTS && warp == 10) {
             // ---------------------------------------------------------------- weights
             const float* weights = p.log_weights == nullptr ? nullptr : p.log_weights + b * p.log_weights_batch;
+            const float unscale = 1.f / p.scale;
             float w[4];
             auto fetch = [&](int it) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int n = (first + it) * TILE + i * 32 + lane;
-                    w[i] = n < p.Nk ? weight2(weights, n) : -INFINITY;
+                    w[i] = n >= p.Nk ? -INFINITY : weights == nullptr ? 0.f : weights[n];
                 }
             };
             if (count > 0) fetch(0);
             for (int it = 0; it < count && ok; ++it) {
-                const int st = it % F::STAGES, slot = it % F::BIAS_SLOTS;
+                const int st = it % F::STAGES;
                 const uint32_t phase = (it / F::STAGES) & 1;
                 uint32_t gone[4], any = 0;
-                float now[4];
+                uint2 parts[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    now[i] = w[i];
-                    gone[i] = __ballot_sync(0xffffffffu, w[i] == -INFINITY && (first + it) * TILE + i * 32 + lane < p.Nk);
+                    const bool out = w[i] <= EXCLUDED;
+                    gone[i] = __ballot_sync(0xffffffffu, out && (first + it) * TILE + i * 32 + lane < p.Nk);
                     any |= gone[i];
+                    parts[i] = out ? make_uint2(EXTRA_OUT, 0) : extra_parts(w[i] * unscale);
                 }
                 if (it + 1 < count) fetch(it + 1);
-                ok = all_lanes(mb_wait(bar(F::K_FULL + st), phase, ok));
+                ok = all_lanes(mb_wait(bar(F::K_FULL + st), phase, ok));        // (the stage's last scores are done, too)
                 if (!ok) break;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) bias[slot][i * 32 + lane] = now[i];
+                for (int i = 0; i < 4; ++i) *reinterpret_cast<uint2*>(base + F::OFF_W + st * F::EXTRA_BYTES + extra_at(i * 32 + lane)) = parts[i];
                 if (any)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) zero_rows(base + F::OFF_K + st * F::TILE_BYTES, slabs, SLAB, i, gone[i], lane);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) { mb_arrive(bar(F::W_READY + slot)); mb_arrive(bar(F::K_READY + st)); }
+                if (lane == 0) mb_arrive(bar(F::K_READY + st));
                 ok = all_lanes(mb_wait(bar(F::V_FULL + st), phase, ok));
                 if (!ok) break;
                 if (any)
@@ -197,30 +233,21 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
         if (t < halves) {
             // ------------------------------------------------------------ softmax
             const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
-            const uint32_t ts = tm + t * TILE + lanes, to = tm + 256 + t * D + lanes;
+            const uint32_t ts = tm + t * TILE + lanes, tp = tm + F::T_P + t * F::P_STEP + lanes, to = tm + F::T_O + t * D + lanes;
             const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2);
             float ref = -INFINITY, l = 0.f;
             for (int it = 0; it < count && ok; ++it) {
                 uint32_t s[TILE];
                 ok = all_lanes(mb_wait(bar(F::S_FULL + t), it & 1, ok));
-                if (WEIGHTS) ok = all_lanes(mb_wait(bar(F::W_READY + it % F::BIAS_SLOTS), (it / F::BIAS_SLOTS) & 1, ok)) && ok;
                 if (!ok) break;
                 tm_after();
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tm_ld32(s + 32 * c, ts + 32 * c);
                 tm_ld_wait();
-                if (WEIGHTS) {
-                    const float4* w = reinterpret_cast<const float4*>(bias[WEIGHTS ? it % F::BIAS_SLOTS : 0]);
-#pragma unroll
-                    for (int i = 0; i < TILE / 4; ++i) {
-                        const float4 wi = w[i];
-                        float x[4];
-                        unpack2(fma2(pack2(__uint_as_float(s[4 * i]), __uint_as_float(s[4 * i + 1])), scale2, pack2(wi.x, wi.y)), x[0], x[1]);
-                        unpack2(fma2(pack2(__uint_as_float(s[4 * i + 2]), __uint_as_float(s[4 * i + 3])), scale2, pack2(wi.z, wi.w)), x[2], x[3]);
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) s[4 * i + k] = __float_as_uint(x[k]);
-                    }
-                } else if ((first + it + 1) * TILE > p.Nk) {
+                if (F::P_APART) {
+                    warp_arrive(bar(F::S_FREE + t), lane);
+                }
+                if (!WEIGHTS && (first + it + 1) * TILE > p.Nk) {
                     const int there = p.Nk - (first + it) * TILE;       // (the scale is positive)
 #pragma unroll
                     for (int i = 0; i < TILE; ++i)
@@ -230,15 +257,15 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
 #pragma unroll
                 for (int i = 0; i < TILE; i += 8)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) top[k] = fmaxf(top[k], fmaxf(__uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1])));
-                float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-                if (!WEIGHTS) now *= p.scale_log2;
+                    for (int k = 0; k < 4; ++k) top[k] = max_or_nan(top[k], max_or_nan(__uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1])));
+                float now = max_or_nan(max_or_nan(top[0], top[1]), max_or_nan(top[2], top[3])) * p.scale_log2;
+                if (WEIGHTS && now < NOTHING) now = -INFINITY;
+                if (!(now < INFINITY)) ref = NAN;            // a score that is NaN or infinite makes its row NaN, from here on
                 const bool grown = now > ref + GROWTH;       // (also the first finite maximum: the reference is -infinity until then)
                 if (__any_sync(0xffffffffu, grown)) {
-                    const float to_ref = grown ? now : ref;
                     const float factor = grown ? ex2(ref - now) : 1.f;
                     l *= factor;
-                    ref = to_ref;
+                    ref = grown ? now : ref;
                     if (it > 0) {
                         ok = all_lanes(mb_wait(bar(F::O_DONE + t), (it - 1) & 1, ok));
                         if (!ok) break;
@@ -262,26 +289,33 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
                 const uint64_t off2 = pack2(off, off);
                 uint64_t sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
+                for (int half = 0; half < 2; ++half) {
                     uint32_t pr[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
-                        const uint64_t x2 = pack2(__uint_as_float(s[64 * c + 2 * i]), __uint_as_float(s[64 * c + 2 * i + 1]));
+                        const uint64_t x2 = fma2(pack2(__uint_as_float(s[64 * half + 2 * i]), __uint_as_float(s[64 * half + 2 * i + 1])), scale2, off2);
                         float x, y;
-                        unpack2(WEIGHTS ? add2(x2, off2) : fma2(x2, scale2, off2), x, y);
-                        x = ex2(x); y = ex2(y);
+                        if (i % BY_FMA == BY_FMA - 1) {
+                            exp2_by_fma(x2, x, y);
+                        } else {
+                            unpack2(x2, x, y);
+                            x = ex2(x); y = ex2(y);
+                        }
                         sum2[i & 1] = add2(sum2[i & 1], pack2(x, y));
                         pr[i] = pack16<T>(x, y);
                     }
-                    tm_st32(ts + 32 * c, pr);
+                    if (F::P_APART && half == 0 && it > 0) {
+                        ok = all_lanes(mb_wait(bar(F::O_DONE + t), (it - 1) & 1, ok));      // the last block's P has been read
+                        if (!ok) break;
+                    }
+                    tm_st32(tp + 32 * half, pr);
+                    tm_st_wait();
+                    warp_arrive(bar(F::P_READY + 2 * t + half), lane);
                 }
                 float a0, a1, a2, a3;
                 unpack2(sum2[0], a0, a1);
                 unpack2(sum2[1], a2, a3);
                 l += (a0 + a1) + (a2 + a3);
-                tm_st_wait();
-                tm_before();
-                mb_arrive(bar(F::P_READY + t));
             }
             if (ok && count > 0) ok = all_lanes(mb_wait(bar(F::O_DONE + t), (count - 1) & 1, ok));
             if (ok) {
@@ -289,9 +323,9 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
                 const int row = row0 + t * TILE + (warp & 3) * 32 + lane;
                 const int64_t at = ((int64_t)b * p.Hq + h) * p.Nq + row;
                 const bool there = row < p.Nq;
-                const float inverse = l == 0.f ? 0.f : 1.f / l;
+                const float inverse = ref == -INFINITY ? 0.f : 1.f / l;
                 if (there) {
-                    const float lse2 = l == 0.f ? -INFINITY : ref + log2f(l) - FORWARD_SHIFT<T>;
+                    const float lse2 = ref == -INFINITY ? -INFINITY : ref + log2f(l) - FORWARD_SHIFT<T>;
                     if (splits > 1) partials[splits * rows_of(p) * p.C + split * rows_of(p) + at] = lse2;
                     else if (p.lse != nullptr) p.lse[at] = lse2 * LN2;
                 }
@@ -340,9 +374,10 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
 // A2 (dout or v), and walks the other side's points in blocks of 64, B1 (k or q) and B2 (v or dout):
 //   S = A1 B1^T, T = A2 B2^T;  p = exp(S - lse), ds = p (T - D);  acc1 += ds B1 (dq or dk);  dk, dv: acc2 += p B2 (dv)
 //   warp 8   TMA of the blocks
-//   warp 9   MMAs: acc of block j, then S and T of block j + 2 into the TMEM that block j has left
+//   warp 9   MMAs: the sums of block j, and S and T of block j + 2 as soon as block j has left their columns: S when it has been read (dq) or its P
+//            has been used (dv), T when its ds has been used
 //   warp 10  dq: weights of the block's points, rows of points left out zeroed; dk, dv: lse and D of the block's queries
-//   warps 0-3 and 4-7  element-wise, blocks of even and of odd number; thread = row; ds and p go back over T and S
+//   warps 0-3 and 4-7  element-wise, blocks of even and of odd number; thread = row; p while T is computed; p and ds go back over S and T
 // Blocks of 64 points need two buffers of S and T to keep both sides busy: 256 of the 512 columns.  An MMA of 64 columns that reads its
 // A operand from shared memory is bound by that (6 KB at 128 bytes per clock: 48 cycles instead of 32), so A1 and A2 are kept in TMEM; only for dk, dv of wide
 // heads, whose two sums take the other 256 columns, are they in shared memory.
@@ -351,13 +386,15 @@ constexpr int BWD_THREADS = 384, BLOCK = 64, BSLAB = BLOCK * 128;
 template <int D, bool DKDV> struct Backward {
     static constexpr bool A_IN_TMEM = D == 64 || !DKDV;
     static constexpr int SLABS = D / 64, STAGES = D == 64 ? 8 : A_IN_TMEM ? 6 : 4, STAGE_BYTES = 2 * SLABS * BSLAB, A_BYTES = A_IN_TMEM ? 0 : 2 * SLABS * SLAB;
-    static constexpr size_t SMEM = A_BYTES + STAGES * STAGE_BYTES + 1024;
+    // dq: ones, and the weights' parts per stage (see the forward kernel)
+    static constexpr int EXTRA_BYTES = BLOCK * 32, OFF_ONES = A_BYTES + STAGES * STAGE_BYTES, OFF_W = OFF_ONES + (DKDV ? 0 : TILE * 32);
+    static constexpr size_t SMEM = OFF_W + (DKDV ? 0 : STAGES * EXTRA_BYTES) + 1024;
     static constexpr int SLOTS = 8;         // at least the stages: a slot is written again when its block's stage is, or later
     // TMEM columns: buffers of (S, T), sums, operands
     static constexpr int T_BUF = 0, T_ACC = 256, T_A = T_ACC + (DKDV ? 2 : 1) * D;
     static_assert(T_A + (A_IN_TMEM ? D : 0) <= 512, "TMEM");
-    enum { A_FULL = 0, A_READY = 1, FULL = 2, READY = FULL + STAGES, FREE = READY + STAGES, W_READY = FREE + STAGES, ST_FULL = W_READY + SLOTS, PD_READY = ST_FULL + 2,
-           ACC_DONE = PD_READY + 2, COUNT };
+    enum { A_FULL = 0, A_READY = 1, FULL = 2, READY = FULL + STAGES, FREE = READY + STAGES, W_READY = FREE + STAGES, S_FULL = W_READY + SLOTS, T_FULL = S_FULL + 2,
+           S_DONE = T_FULL + 2 /* S read (dq) or P ready (dk, dv) */, D_READY = S_DONE + 2, ACC_DONE = D_READY + 2, COUNT };
 };
 
 template <typename T, int D, bool DKDV, bool WEIGHTS>
@@ -365,12 +402,12 @@ __global__ void __launch_bounds__(BWD_THREADS, 1)
 attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats stats, const __grid_constant__ CUtensorMap map_a1, const __grid_constant__ CUtensorMap map_a2,
                           const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_b2, int tiles) {
     using K = Backward<D, DKDV>;
-    constexpr bool COLUMNS = DKDV || WEIGHTS;           // something is read per streamed point
+    constexpr bool COLUMNS = DKDV;                      // statistics are read per streamed point
     constexpr bool CLEARED = !DKDV && WEIGHTS;          // streamed points may be left out
     extern __shared__ unsigned char raw[];
     unsigned char* base = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     __shared__ unsigned long long bars[K::COUNT];
-    __shared__ __align__(16) float column[COLUMNS ? K::SLOTS : 1][DKDV ? 2 : 1][BLOCK];        // dq: weights; dk, dv: -lse, -D
+    __shared__ __align__(16) float column[COLUMNS ? K::SLOTS : 1][2][BLOCK];        // -lse, -D
     __shared__ uint32_t tmem_s;
     __shared__ int fail_s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -384,13 +421,19 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     auto stage = [&](int st) { return s32(base) + K::A_BYTES + st * K::STAGE_BYTES; };
 
     if (tid == 0) {
-        for (int i = 0; i < K::COUNT; ++i) mb_init(bar(i), i == K::A_READY && K::A_IN_TMEM ? 256 : i >= K::PD_READY && i < K::PD_READY + 2 ? 128 : 1);
+        for (int i = 0; i < K::COUNT; ++i) mb_init(bar(i), i == K::A_READY && K::A_IN_TMEM ? 8 : i >= K::S_DONE && i < K::ACC_DONE ? 4 : 1);
         fail_s = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s32(&tmem_s)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+    if (CLEARED) {
+        for (int e = tid; e < TILE * 2; e += BWD_THREADS)
+            *reinterpret_cast<uint4*>(base + K::OFF_ONES + e * 16) = (e & 8) ? make_uint4(0, 0, 0, 0) : make_uint4(EXTRA_ONES_0, EXTRA_ONES_1, 0, 0);
+        for (int e = tid; e < K::STAGES * K::EXTRA_BYTES / 16; e += BWD_THREADS) *reinterpret_cast<uint4*>(base + K::OFF_W + e * 16) = make_uint4(0, 0, 0, 0);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     tm_before();
     __syncthreads();
@@ -427,43 +470,58 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
         } else if (warp == 9 && elect_one()) {
             // ---------------------------------------------------------------- MMAs
             const uint32_t ids = idesc<T>(BLOCK, false), ido = idesc<T>(steps * 16, true);
-            auto ready = [&](int it) { return mb_wait(bar((CLEARED ? K::READY : K::FULL) + it % K::STAGES), (it / K::STAGES) & 1, ok); };
-            auto first = [&](int it) {
-                const uint32_t at = stage(it % K::STAGES), to = tm + K::T_BUF + (it & 1) * 2 * BLOCK;
+            const uint32_t idw = idesc<__nv_bfloat16>(BLOCK, false);
+            const uint32_t da = desc_channels(s32(base)), db = desc_channels(stage(0)), dp = desc_points(stage(0), BSLAB);
+            const uint32_t dones = desc_extra(s32(base) + K::OFF_ONES), dw = desc_extra(s32(base) + K::OFF_W);
+            auto ready = [&](int it) { return mb_wait(bar((CLEARED ? K::READY : K::FULL) + it % K::STAGES), (it / K::STAGES) & 1, true); };
+            // which: 0 S, 1 T
+            auto first = [&](int it, int which) {
+                const int st = it % K::STAGES;
+                const uint32_t to = tm + K::T_BUF + (it & 1) * 2 * BLOCK + which * BLOCK, bd = db + st * (K::STAGE_BYTES >> 4) + which * K::SLABS * (BSLAB >> 4);
 #pragma unroll
-                for (int which = 0; which < 2; ++which)
-                    for (int ks = 0; ks < steps; ++ks) {
-                        const uint64_t bd = desc_channels(at + (which * K::SLABS + (ks >> 2)) * BSLAB + (ks & 3) * 32);
-                        if (K::A_IN_TMEM) mma_ts(to + which * BLOCK, tm + K::T_A + which * (D / 2) + ks * 8, bd, ids, ks > 0);
-                        else mma_ss(to + which * BLOCK, desc_channels(s32(base) + (which * K::SLABS + (ks >> 2)) * SLAB + (ks & 3) * 32), bd, ids, ks > 0);
+                for (int ks = 0; ks < D / 16; ++ks)
+                    if (ks < steps) {
+                        if constexpr (K::A_IN_TMEM) mma_ts(to, tm + K::T_A + which * (D / 2) + ks * 8, bd + (ks >> 2) * (BSLAB >> 4) + (ks & 3) * 2, ids, ks > 0);
+                        else mma_ss(to, da + (which * K::SLABS + (ks >> 2)) * (SLAB >> 4) + (ks & 3) * 2, bd + (ks >> 2) * (BSLAB >> 4) + (ks & 3) * 2, ids, ks > 0);
                     }
-                mma_commit(bar(K::ST_FULL + (it & 1)));
+                if (CLEARED && which == 0) mma_ss<DESC_EXTRA_HIGH>(to, dones, dw + st * (K::EXTRA_BYTES >> 4), idw, 1);
+                mma_commit(bar((which == 0 ? K::S_FULL : K::T_FULL) + (it & 1)));
             };
-            ok = mb_wait(bar(K::A_IN_TMEM || (DKDV && WEIGHTS) ? K::A_READY : K::A_FULL), 0, ok);
+            ok = mb_wait(bar(K::A_IN_TMEM || (DKDV && WEIGHTS) ? K::A_READY : K::A_FULL), 0, true);
             tm_after();
             for (int it = 0; it < 2 && it < count && ok; ++it) {
                 ok = ready(it);
-                if (ok) first(it);
+                if (!ok) break;
+                first(it, 0);
+                first(it, 1);
             }
             for (int it = 0; it < count && ok; ++it) {
-                const uint32_t at = stage(it % K::STAGES), from = tm + K::T_BUF + (it & 1) * 2 * BLOCK;
-                ok = mb_wait(bar(K::PD_READY + (it & 1)), (it >> 1) & 1, ok);
+                const int st = it % K::STAGES;
+                const uint32_t at = dp + st * (K::STAGE_BYTES >> 4), from = tm + K::T_BUF + (it & 1) * 2 * BLOCK;
+                const bool more = it + 2 < count;
+                ok = mb_wait(bar(K::S_DONE + (it & 1)), (it >> 1) & 1, true);
+                if (!ok) break;
+                tm_after();
+                if (DKDV)
+#pragma unroll
+                    for (int kk = 0; kk < BLOCK / 16; ++kk)
+                        mma_ts(tm + K::T_ACC + D, from + kk * 8, at + K::SLABS * (BSLAB >> 4) + kk * (2048 >> 4), ido, it > 0 || kk > 0);
+                if (more) {
+                    ok = ready(it + 2);
+                    if (!ok) break;
+                    first(it + 2, 0);
+                }
+                ok = mb_wait(bar(K::D_READY + (it & 1)), (it >> 1) & 1, true);
                 if (!ok) break;
                 tm_after();
 #pragma unroll
-                for (int kk = 0; kk < BLOCK / 16; ++kk) {
-                    mma_ts(tm + K::T_ACC, from + BLOCK + kk * 8, desc_points(at + kk * 2048, BSLAB), ido, it > 0 || kk > 0);
-                    if (DKDV) mma_ts(tm + K::T_ACC + D, from + kk * 8, desc_points(at + K::SLABS * BSLAB + kk * 2048, BSLAB), ido, it > 0 || kk > 0);
-                }
-                mma_commit(bar(K::FREE + it % K::STAGES));
-                if (it + 2 < count) {
-                    ok = ready(it + 2);
-                    if (ok) first(it + 2);
-                }
+                for (int kk = 0; kk < BLOCK / 16; ++kk) mma_ts(tm + K::T_ACC, from + BLOCK + kk * 8, at + kk * (2048 >> 4), ido, it > 0 || kk > 0);
+                mma_commit(bar(K::FREE + st));
+                if (more) first(it + 2, 1);
             }
             mma_commit(bar(K::ACC_DONE));
             mb_wait(bar(K::ACC_DONE), 0, true);
-        } else if (COLUMNS && warp == 10) {
+        } else if ((COLUMNS || CLEARED) && warp == 10) {
             // ---------------------------------------------------------------- what is read per streamed point
             if (!K::A_IN_TMEM && WEIGHTS) {
                 ok = all_lanes(mb_wait(bar(K::A_FULL), 0, ok));
@@ -487,7 +545,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                         x[i] = n < M ? -stats.lse2[at] : -INFINITY;
                         y[i] = n < M ? -stats.D[at] : 0.f;
                     } else {
-                        x[i] = n < M ? weight2(weights, n) : -INFINITY;
+                        x[i] = n >= M ? -INFINITY : weights == nullptr ? 0.f : weights[n];
                         y[i] = 0.f;
                     }
                 }
@@ -497,18 +555,26 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                 const int st = it % K::STAGES, slot = it % K::SLOTS;
                 float now[2], also[2];
                 uint32_t gone[2];
+                uint2 parts[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     now[i] = x[i]; also[i] = y[i];
-                    gone[i] = CLEARED ? __ballot_sync(0xffffffffu, x[i] == -INFINITY && it * BLOCK + i * 32 + lane < M) : 0;
+                    if (CLEARED) {
+                        const bool out = x[i] <= EXCLUDED;
+                        gone[i] = __ballot_sync(0xffffffffu, out && it * BLOCK + i * 32 + lane < M);
+                        parts[i] = out ? make_uint2(EXTRA_OUT, 0) : extra_parts(x[i] * (1.f / p.scale));
+                    }
                 }
                 if (it + 1 < count) fetch(it + 1);
-                ok = all_lanes(mb_wait(bar(K::FULL + st), (it / K::STAGES) & 1, ok));       // (then the slot's last readers are done, too)
+                ok = all_lanes(mb_wait(bar(K::FULL + st), (it / K::STAGES) & 1, ok));       // (then the slot's and the stage's last readers are done, too)
                 if (!ok) break;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    column[slot][0][i * 32 + lane] = now[i];
-                    if (DKDV) column[slot][DKDV ? 1 : 0][i * 32 + lane] = also[i];
+                    if (COLUMNS) {
+                        column[COLUMNS ? slot : 0][0][i * 32 + lane] = now[i];
+                        column[COLUMNS ? slot : 0][1][i * 32 + lane] = also[i];
+                    }
+                    if (CLEARED) *reinterpret_cast<uint2*>(base + K::OFF_W + st * K::EXTRA_BYTES + extra_at(i * 32 + lane)) = parts[i];
                 }
                 if (CLEARED) {
                     if (gone[0] | gone[1])
@@ -520,7 +586,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                 }
                 __syncwarp();
                 if (lane == 0) {
-                    mb_arrive(bar(K::W_READY + slot));
+                    if (COLUMNS) mb_arrive(bar(K::W_READY + slot));
                     if (CLEARED) mb_arrive(bar(K::READY + st));
                 }
             }
@@ -548,8 +614,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                 tm_st32(tm + K::T_A + group * (D / 2) + half * 32 + lanes, x);
             }
             tm_st_wait();
-            tm_before();
-            mb_arrive(bar(K::A_READY));
+            warp_arrive(bar(K::A_READY), lane);
         }
         const float factor = ds_scale<T>(stats, b * p.Hk + hk);
         float neg_lse = 0.f, neg_D = 0.f;       // dq: the row's
@@ -561,17 +626,18 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
         const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), row_x = DKDV ? pack2(w, w) : pack2(neg_lse, neg_lse), row_D = pack2(neg_D, neg_D), factor2 = pack2(factor, factor);
         for (int it = group; it < count && ok; it += 2) {
             const uint32_t from = tm + K::T_BUF + group * 2 * BLOCK + lanes;
-            uint32_t s[BLOCK], t[BLOCK];
-            ok = all_lanes(mb_wait(bar(K::ST_FULL + group), (it >> 1) & 1, ok));
+            uint32_t s[BLOCK];
+            ok = all_lanes(mb_wait(bar(K::S_FULL + group), (it >> 1) & 1, ok));
             if (COLUMNS) ok = all_lanes(mb_wait(bar(K::W_READY + it % K::SLOTS), (it / K::SLOTS) & 1, ok)) && ok;
             if (!ok) break;
             tm_after();
             tm_ld32(s, from);
             tm_ld32(s + 32, from + 32);
-            tm_ld32(t, from + BLOCK);
-            tm_ld32(t + 32, from + BLOCK + 32);
             tm_ld_wait();
-            if (!COLUMNS && (it + 1) * BLOCK > M) {
+            if (!DKDV) {
+                warp_arrive(bar(K::S_DONE + group), lane);
+            }
+            if (!DKDV && !WEIGHTS && (it + 1) * BLOCK > M) {
                 // points that are not there: zero rows, whose probability must not overflow (the scale is positive)
                 const int left = M - it * BLOCK;
 #pragma unroll
@@ -579,40 +645,54 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                     if (i >= left) s[i] = 0xff800000u;
             }
             const float4* c0 = reinterpret_cast<const float4*>(column[COLUMNS ? it % K::SLOTS : 0][0]);
-            const float4* c1 = reinterpret_cast<const float4*>(column[COLUMNS ? it % K::SLOTS : 0][DKDV ? 1 : 0]);
-            uint32_t pr[DKDV ? 32 : 1], ds[32];
+            const float4* c1 = reinterpret_cast<const float4*>(column[COLUMNS ? it % K::SLOTS : 0][1]);
 #pragma unroll
             for (int i = 0; i < BLOCK / 4; ++i) {
-                float4 cx, cd;
-                if (COLUMNS) cx = c0[i];
-                if (DKDV) cd = c1[i];
+                float4 c;
+                if (COLUMNS) c = c0[i];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const uint64_t s2 = pack2(__uint_as_float(s[4 * i + 2 * k]), __uint_as_float(s[4 * i + 2 * k + 1]));
-                    const uint64_t t2 = pack2(__uint_as_float(t[4 * i + 2 * k]), __uint_as_float(t[4 * i + 2 * k + 1]));
-                    uint64_t x2;
-                    if (COLUMNS) {
-                        x2 = fma2(s2, scale2, k == 0 ? pack2(cx.x, cx.y) : pack2(cx.z, cx.w));
-                        if (!DKDV || WEIGHTS) x2 = add2(x2, row_x);
-                    } else {
-                        x2 = fma2(s2, scale2, row_x);
-                    }
+                    const int at = 4 * i + 2 * k;
+                    uint64_t x2 = fma2(pack2(__uint_as_float(s[at]), __uint_as_float(s[at + 1])), scale2, !COLUMNS ? row_x : k == 0 ? pack2(c.x, c.y) : pack2(c.z, c.w));
+                    if (DKDV && WEIGHTS) x2 = add2(x2, row_x);
                     float e0, e1;
                     unpack2(x2, e0, e1);
-                    e0 = ex2(e0); e1 = ex2(e1);
-                    uint64_t d2 = add2(t2, DKDV ? (k == 0 ? pack2(cd.x, cd.y) : pack2(cd.z, cd.w)) : row_D);
+                    s[at] = __float_as_uint(ex2(e0));
+                    s[at + 1] = __float_as_uint(ex2(e1));
+                }
+            }
+            if (DKDV) {
+                uint32_t pr[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) pr[i] = pack16<T>(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+                tm_st32(from, pr);
+                tm_st_wait();
+                warp_arrive(bar(K::S_DONE + group), lane);
+            }
+            ok = all_lanes(mb_wait(bar(K::T_FULL + group), (it >> 1) & 1, ok));
+            if (!ok) break;
+            tm_after();
+            uint32_t t[BLOCK], ds[32];
+            tm_ld32(t, from + BLOCK);
+            tm_ld32(t + 32, from + BLOCK + 32);
+            tm_ld_wait();
+#pragma unroll
+            for (int i = 0; i < BLOCK / 4; ++i) {
+                float4 c;
+                if (COLUMNS) c = c1[i];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int at = 4 * i + 2 * k;
+                    uint64_t d2 = add2(pack2(__uint_as_float(t[at]), __uint_as_float(t[at + 1])), !COLUMNS ? row_D : k == 0 ? pack2(c.x, c.y) : pack2(c.z, c.w));
                     if (SHIFT<T> != 0.f) d2 = mul2(d2, factor2);
                     float d0, d1;
-                    unpack2(mul2(d2, pack2(e0, e1)), d0, d1);
-                    if (DKDV) pr[DKDV ? 2 * i + k : 0] = pack16<T>(e0, e1);
+                    unpack2(mul2(d2, pack2(__uint_as_float(s[at]), __uint_as_float(s[at + 1]))), d0, d1);
                     ds[2 * i + k] = pack16<T>(d0, d1);
                 }
             }
-            if constexpr (DKDV) tm_st32(from, pr);
             tm_st32(from + BLOCK, ds);
             tm_st_wait();
-            tm_before();
-            mb_arrive(bar(K::PD_READY + group));
+            warp_arrive(bar(K::D_READY + group), lane);
         }
         // ---------------------------------------------------------------- results: dq by halves of the channels, or dk by group 0 and dv by group 1
         ok = all_lanes(mb_wait(bar(K::ACC_DONE), 0, ok)) && ok;
@@ -685,7 +765,7 @@ bool backward_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream
     if (!make_map(&maps[q_at], p.q, dtype, p.C, p.Nq, p.Hq, p.B, q_rows) || !make_map(&maps[q_at + 1], p.dout, dtype, p.C, p.Nq, p.Hq, p.B, q_rows) ||
         !make_map(&maps[k_at], p.k, dtype, p.C, p.Nk, p.Hk, p.B, k_rows) || !make_map(&maps[k_at + 1], p.v, dtype, p.C, p.Nk, p.Hk, p.B, k_rows))
         return false;
-    const bool weights = p.log_weights != nullptr || !(p.scale > 0.f);
+    const bool weights = p.log_weights != nullptr;
     auto run = [&](auto t, auto width) {
         using T = decltype(t);
         constexpr int D = decltype(width)::value;
@@ -720,7 +800,7 @@ bool forward_tc(const Problem& p, sna_dtype_t dtype, int splits, float* partials
     if (!make_map(&maps[0], p.q, dtype, p.C, p.Nq, p.Hq, p.B, TILE) || !make_map(&maps[1], p.k, dtype, p.C, p.Nk, p.Hk, p.B, TILE) ||
         !make_map(&maps[2], p.v, dtype, p.C, p.Nk, p.Hk, p.B, TILE))
         return false;
-    const bool weights = p.log_weights != nullptr || !(p.scale > 0.f);
+    const bool weights = p.log_weights != nullptr;
     auto run = [&](auto t, auto width) {
         using T = decltype(t);
         constexpr int D = decltype(width)::value;
