@@ -62,7 +62,8 @@ int splits_of(const Problem& p, int sms) {
 }
 
 size_t forward_bytes(const Problem& p, int splits) { return splits > 1 ? align256((size_t)splits * rows_of(p) * (1 + p.C) * sizeof(float)) : 0; }
-size_t backward_bytes(const Problem& p) { return 2 * align256((size_t)rows_of(p) * sizeof(float)) + align256((size_t)p.B * p.Hk * 2 * sizeof(uint32_t)); }
+size_t extra_bytes(const Problem& p) { return (size_t)query_blocks_of(p) * 2 * STATS_BLOCK * sizeof(uint4); }
+size_t backward_bytes(const Problem& p) { return 2 * align256((size_t)rows_of(p) * sizeof(float)) + align256((size_t)p.B * p.Hk * 2 * sizeof(uint32_t)) + extra_bytes(p); }
 
 }  // namespace
 }  // namespace attend
@@ -114,9 +115,14 @@ sna_status_t sna_attention_backward(const sna_attention_t* a, sna_dtype_t dtype,
     if (st != SNA_OK) return st;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     Stats s;
-    s.lse2 = static_cast<float*>(workspace);
-    s.D = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256((size_t)rows_of(p) * sizeof(float)));
-    s.norms = reinterpret_cast<uint32_t*>(static_cast<char*>(workspace) + 2 * align256((size_t)rows_of(p) * sizeof(float)));
+    char* at = static_cast<char*>(workspace);
+    s.extra = reinterpret_cast<uint4*>(at);
+    at += extra_bytes(p);
+    s.lse2 = reinterpret_cast<float*>(at);
+    at += align256((size_t)rows_of(p) * sizeof(float));
+    s.D = reinterpret_cast<float*>(at);
+    at += align256((size_t)rows_of(p) * sizeof(float));
+    s.norms = reinterpret_cast<uint32_t*>(at);
     cudaError_t e = launch_statistics(p, s, dtype, stream);
     const bool on_tc = on_tensor_memory(p);
     if (e == cudaSuccess && queries && (!on_tc || !backward_dq_tc(p, s, dtype, stream, e))) e = launch_backward_dq(p, s, dtype, stream);

@@ -30,7 +30,10 @@ struct Stats {
     float* lse2;                    // [B][Hq][Nq]: log2 of the sum of weights, +infinity for rows without any
     float* D;                       // [B][Hq][Nq]
     uint32_t* norms;                // [B][Hk][2]: of dout's rows, of v's rows (float16 only)
+    uint4* extra;                   // [B][Hq][blocks of 64 queries][2][64]: what the tcgen05 dk/dv kernel adds to S and T per query (see there)
 };
+constexpr int STATS_BLOCK = 64;
+__host__ __device__ inline int64_t query_blocks_of(const Problem& p) { return (int64_t)p.B * p.Hq * ((p.Nq + STATS_BLOCK - 1) / STATS_BLOCK); }
 
 // Powers of two that keep float16 operands of the second products away from the numbers that its exponent has no room for: softmax
 // weights (at most 1) and, in the backward pass, probabilities are held times 2^SHIFT.
@@ -38,6 +41,17 @@ template <typename T> constexpr float SHIFT = 0.f;
 template <> constexpr float SHIFT<__half> = 14.f;
 
 #ifdef __CUDACC__
+// A number in three bfloat16 parts (24 bits), whose products with ones a tensor core adds up; the lowest, for a point left out: times a scale of 2^-20
+// or more, below any finite score of a point that takes part.
+constexpr uint32_t EXTRA_ONES_0 = 0x3f803f80u, EXTRA_ONES_1 = 0x00003f80u;
+constexpr uint32_t EXTRA_OUT = 0x0000ff61u;        // -2.99e38: times a scale of 2^-20 or more, below any finite score of a point that takes part
+__device__ __forceinline__ uint2 extra_parts(float x) {
+    const __nv_bfloat16 hi = __float2bfloat16_rn(x);
+    const float rest = x - __bfloat162float(hi);
+    const __nv_bfloat16 mid = __float2bfloat16_rn(rest), lo = __float2bfloat16_rn(rest - __bfloat162float(mid));
+    return make_uint2((uint32_t)__bfloat16_as_ushort(hi) | ((uint32_t)__bfloat16_as_ushort(mid) << 16), __bfloat16_as_ushort(lo));
+}
+
 // The power of two that ds is held times.  The probabilities in it are already held times 2^SHIFT; with |t - D| <= bound the products stay below 2^15.
 template <typename T>
 __device__ __forceinline__ float ds_scale(const Stats& s, int bk) {

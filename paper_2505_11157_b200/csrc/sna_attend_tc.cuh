@@ -20,14 +20,22 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ void mb_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
 __device__ __forceinline__ void mb_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ void mb_expect(uint32_t bar, uint32_t bytes) { asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory"); }
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mb_try(uint32_t bar, uint32_t parity) {
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}\n"
+                 : "=r"(done) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
+    return done != 0;
+}
 // Bounded wait; once one has run out (`healthy` false) later ones give up at once.
 __device__ __forceinline__ bool mb_wait(uint32_t bar, uint32_t parity, bool healthy) {
-    uint32_t done = 0;
+    if (mb_try(bar, parity)) return true;
+    bool done = false;
     const int limit = healthy ? WAIT_POLLS : 4;
-    for (int it = 0; it < limit && !done; ++it)
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}\n"
-                     : "=r"(done) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
-    return done != 0;
+    for (int it = 0; it < limit && !done; ++it) done = mb_try(bar, parity);
+    return done;
 }
 // [channel, point, head, batch]: 64 channels (128 bytes) of the map's rows, 128-byte swizzle
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int c, int point, int head, int batch, uint32_t bar) {
@@ -47,24 +55,19 @@ __device__ __forceinline__ uint32_t desc_points(uint32_t addr, uint32_t slab) { 
 constexpr uint32_t DESC_EXTRA_HIGH = (256 >> 4) | (1u << 14);
 __device__ __forceinline__ uint32_t desc_extra(uint32_t addr) { return (addr >> 4) | ((128u >> 4) << 16); }
 __device__ __forceinline__ int extra_at(int row) { return (row >> 3) * 256 + (row & 7) * 16; }
-constexpr uint32_t EXTRA_ONES_0 = 0x3f803f80u, EXTRA_ONES_1 = 0x00003f80u;
-constexpr uint32_t EXTRA_OUT = 0x0000ff61u;        // -2.99e38: times a scale of 2^-20 or more, below any finite score of a point that takes part
-__device__ __forceinline__ uint2 extra_parts(float x) {
-    const __nv_bfloat16 hi = __float2bfloat16_rn(x);
-    const float rest = x - __bfloat162float(hi);
-    const __nv_bfloat16 mid = __float2bfloat16_rn(rest), lo = __float2bfloat16_rn(rest - __bfloat162float(mid));
-    return make_uint2((uint32_t)__bfloat16_as_ushort(hi) | ((uint32_t)__bfloat16_as_ushort(mid) << 16), __bfloat16_as_ushort(lo));
-}
+// The same as a B operand without the second half: 8 rows 128 bytes apart, and the first half read in its place (against zeros).
+constexpr uint32_t DESC_DENSE_HIGH = (128 >> 4) | (1u << 14);
+__device__ __forceinline__ uint32_t desc_dense(uint32_t addr) { return addr >> 4; }
 
 // fp32 accumulator, both operands T, 128 rows, n columns
 template <typename T> __device__ __forceinline__ uint32_t idesc(int n, bool b_is_points) {
     const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
     return (1u << 4) | (type << 7) | (type << 10) | ((b_is_points ? 1u : 0u) << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
 }
-template <uint32_t HIGH = DESC_HIGH>
+template <uint32_t HIGH_A = DESC_HIGH, uint32_t HIGH_B = HIGH_A>
 __device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
-    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
-                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}\n" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "n"(HIGH) : "memory");
+    asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %6};\n\t"
+                 "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}\n" ::"r"(d), "r"(a), "r"(b), "r"(idesc), "r"(acc), "n"(HIGH_A), "n"(HIGH_B) : "memory");
 }
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a_tmem, uint32_t b, uint32_t idesc, uint32_t acc) {
     asm volatile("{\n\t.reg .pred p;\n\t.reg .b64 b;\n\tsetp.ne.b32 p, %4, 0;\n\tmov.b64 b, {%2, %5};\n\t"
@@ -100,26 +103,28 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t d; a
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
 
 // 2^x for two numbers of at most 2^6 on the FMA pipe, beside the special-function unit that ex2 uses: x = n + f with |f| <= 1/2 (Cody and Waite),
-// 2^f by the polynomial of degree 4 with the least relative error there (2.6e-6: 2^-18.5, found by iterated least squares), n added to the exponent.  Numbers below -126 count as -126; NaN and
-// infinities are not kept: the caller has to see to them.
+// 2^f by the polynomial of degree 4 with the least relative error there (2.6e-6 = 2^-18.5, found by iterated least squares), times 2^n.  Numbers below -126
+// count as -126; NaN stays NaN.
 __device__ __forceinline__ void exp2_by_fma(uint64_t x2, float& y0, float& y1) {
     float x0, x1;
     unpack2(x2, x0, x1);
-    x2 = pack2(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
-    const uint64_t round2 = pack2(12582912.f, 12582912.f), back2 = pack2(-12582912.f, -12582912.f), minus2 = pack2(-1.f, -1.f);
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x0) : "f"(-126.f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x1) : "f"(-126.f));
+    x2 = pack2(x0, x1);
+    const uint64_t round2 = pack2(12582912.f, 12582912.f), back2 = pack2(-12582912.f, -12582912.f), minus2 = pack2(-1.f, -1.f);     // 1.5 * 2^23: n in the low bits
     const uint64_t t2 = add2(x2, round2), f2 = fma2(add2(t2, back2), minus2, x2);
     uint64_t p2 = pack2(0.009570102f, 0.009570102f);
     p2 = fma2(p2, f2, pack2(0.055917863f, 0.055917863f));
     p2 = fma2(p2, f2, pack2(0.24024744f, 0.24024744f));
     p2 = fma2(p2, f2, pack2(0.6931218f, 0.6931218f));
     p2 = fma2(p2, f2, pack2(0.9999993f, 0.9999993f));
-    float t0, t1, p0, p1;
+    float t0, t1;
     unpack2(t2, t0, t1);
-    unpack2(p2, p0, p1);
-    y0 = __uint_as_float(__float_as_uint(p0) + (__float_as_uint(t0) << 23));
-    y1 = __uint_as_float(__float_as_uint(p1) + (__float_as_uint(t1) << 23));
+    t0 = __uint_as_float((__float_as_uint(t0) << 23) + 0x3f800000u);
+    t1 = __uint_as_float((__float_as_uint(t1) << 23) + 0x3f800000u);
+    unpack2(mul2(p2, pack2(t0, t1)), y0, y1);
 }
-__device__ __forceinline__ float max_or_nan(float a, float b) { float r; asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ float max3(float a, float b, float c) { float r; asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c)); return r; }
 
 template <typename T> __device__ __forceinline__ uint32_t pack16(float lo, float hi);
 template <> __device__ __forceinline__ uint32_t pack16<__nv_bfloat16>(float lo, float hi) {

@@ -337,61 +337,64 @@ __global__ void __launch_bounds__(THREADS) attend_join_kernel(const __grid_const
 
 // ---- backward: statistics -----------------------------------------------------------------------------------------------------
 
-// Per query: D = dout . out, and log2 of the sum of weights.  float16: also the largest norm of a row of dout and of v per key head, which bound
-// |t - D| <= 2 |dout| |v| (the blocks beyond the queries' take v's rows).  A maximum does not depend on the order of its atomics.  Four lanes per row.
+// Per query: D = dout . out, log2 of the sum of weights, and both as the extra rows that the tcgen05 dk/dv kernel copies.  float16: also the largest norm
+// of a row of dout and of v per key head, which bound |t - D| <= 2 |dout| |v| (the blocks behind the queries' take v's rows); a maximum does not depend on the
+// order of its atomics, of which there is one per block (one per row took ten times as long as the rest).  A block takes 64 points of one head,
+// four lanes each.
 template <typename T>
 __global__ void __launch_bounds__(256) attend_statistics_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats s, int64_t query_blocks) {
     constexpr bool SCALED = SHIFT<T> != 0.f;
-    const int part = threadIdx.x & 3;
+    __shared__ uint32_t most;
+    const int part = threadIdx.x & 3, place = threadIdx.x >> 2;
     const bool queries = blockIdx.x < query_blocks;
-    const int64_t row = ((int64_t)blockIdx.x - (queries ? 0 : query_blocks)) * 64 + (threadIdx.x >> 2);
-    const int64_t rows = queries ? rows_of(p) : (int64_t)p.B * p.Hk * p.Nk;
+    const int64_t block = (int64_t)blockIdx.x - (queries ? 0 : query_blocks);
+    const int N = queries ? p.Nq : p.Nk, H = queries ? p.Hq : p.Hk, per_head = (N + STATS_BLOCK - 1) / STATS_BLOCK;
+    const int64_t bh = block / per_head, b = bh / H, h = bh - b * H;
+    const int n = (int)(block - bh * per_head) * STATS_BLOCK + place;
+    const bool there = n < N && (queries || p.log_weights == nullptr || !(p.log_weights[b * p.log_weights_batch + n] <= EXCLUDED));
     float square = 0.f, dot = 0.f;
-    int64_t bk = 0;
-    bool there = row < rows;
     if (there) {
-        const int N = queries ? p.Nq : p.Nk, H = queries ? p.Hq : p.Hk;
-        const int64_t bh = row / N, n = row - bh * N, b = bh / H, h = bh - b * H;
-        bk = queries ? b * p.Hk + h / p.G : bh;
-        if (!queries && p.log_weights != nullptr && p.log_weights[b * p.log_weights_batch + n] <= EXCLUDED) there = false;
         const View& x = queries ? p.dout : p.v;
         const T* px = static_cast<const T*>(x.data) + b * x.batch + h * x.head + n * x.point;
         const T* py = queries ? static_cast<const T*>(p.out.data) + b * p.out.batch + h * p.out.head + n * p.out.point : px;
-        if (there)
-            for (int c = part * 8; c < p.C; c += 32) {
-                const Pack<T, 8> a = *reinterpret_cast<const Pack<T, 8>*>(px + c), o = *reinterpret_cast<const Pack<T, 8>*>(py + c);
+        for (int c = part * 8; c < p.C; c += 32) {
+            const Pack<T, 8> a = *reinterpret_cast<const Pack<T, 8>*>(px + c), o = *reinterpret_cast<const Pack<T, 8>*>(py + c);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float f = to_float(a.v[i]);
-                    dot = fmaf(f, to_float(o.v[i]), dot);
-                    if (SCALED) square = fmaf(f, f, square);
-                }
+            for (int i = 0; i < 8; ++i) {
+                const float f = to_float(a.v[i]);
+                dot = fmaf(f, to_float(o.v[i]), dot);
+                if (SCALED) square = fmaf(f, f, square);
             }
+        }
     }
 #pragma unroll
     for (int o = 1; o < 4; o <<= 1) {
         dot += __shfl_xor_sync(0xffffffffu, dot, o);
         if (SCALED) square += __shfl_xor_sync(0xffffffffu, square, o);
     }
-    if (there && part == 0) {
-        if (queries) {
+    if (queries && part < 2) {
+        float lse2 = INFINITY, D = 0.f;
+        if (there) {
+            const int64_t row = bh * p.Nq + n;
             const float lse = p.lse[row];
-            s.D[row] = lse == -INFINITY ? 0.f : dot;
-            s.lse2[row] = lse == -INFINITY ? INFINITY : lse * LOG2E - SHIFT<T>;
+            if (lse != -INFINITY) {
+                lse2 = lse * LOG2E - SHIFT<T>;
+                D = dot;
+            }
+            if (part == 0) s.lse2[row] = lse2;
+            else s.D[row] = D;
         }
+        // (1, 1, 1, -lse / scale in parts) against (weight of a key in parts, 1, 1, 1), and (-D in parts) against ones
+        const uint2 parts = part == 1 ? extra_parts(-D) : lse2 == INFINITY ? make_uint2(EXTRA_OUT, 0) : extra_parts(-lse2 / p.scale_log2);
+        s.extra[(block * 2 + part) * STATS_BLOCK + place] =
+            part == 1 ? make_uint4(parts.x, parts.y, 0, 0) : make_uint4(EXTRA_ONES_0, EXTRA_ONES_1 | (parts.x << 16), (parts.x >> 16) | (parts.y << 16), 0);
     }
     if (SCALED) {
-        // one atomic per block where its rows belong to one key head (contended ones, one per row, took ten times as long as the rest)
-        __shared__ uint32_t most;
-        __shared__ int64_t head;
-        if (threadIdx.x == 0) { most = 0; head = bk; }
+        if (threadIdx.x == 0) most = 0;
         __syncthreads();
-        if (there && part == 0) {
-            if (bk == head) atomicMax(&most, __float_as_uint(sqrtf(square)));
-            else atomicMax(s.norms + bk * 2 + (queries ? 0 : 1), __float_as_uint(sqrtf(square)));
-        }
+        if (there && part == 0) atomicMax(&most, __float_as_uint(sqrtf(square)));
         __syncthreads();
-        if (threadIdx.x == 0 && most != 0) atomicMax(s.norms + head * 2 + (queries ? 0 : 1), most);
+        if (threadIdx.x == 0 && most != 0) atomicMax(s.norms + (b * p.Hk + (queries ? h / p.G : h)) * 2 + (queries ? 0 : 1), most);
     }
 }
 
@@ -701,7 +704,7 @@ cudaError_t launch_forward(const Problem& p, sna_dtype_t dtype, int splits, floa
 }
 
 cudaError_t launch_statistics(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream) {
-    const int64_t query_blocks = (rows_of(p) + 63) / 64, key_blocks = ((int64_t)p.B * p.Hk * p.Nk + 63) / 64;
+    const int64_t query_blocks = query_blocks_of(p), key_blocks = (int64_t)p.B * p.Hk * ((p.Nk + STATS_BLOCK - 1) / STATS_BLOCK);
     if (dtype == SNA_BFLOAT16) {
         if (query_blocks == 0) return cudaSuccess;
         attend_statistics_kernel<__nv_bfloat16><<<(unsigned)query_blocks, 256, 0, stream>>>(p, s, query_blocks);

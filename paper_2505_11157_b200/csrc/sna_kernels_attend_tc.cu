@@ -56,7 +56,10 @@ template <int D> struct Forward {
 template <typename T> constexpr float FORWARD_SHIFT = 0.f;
 template <> constexpr float FORWARD_SHIFT<__half> = 7.f;
 constexpr float GROWTH = 8.f;
-constexpr int BY_FMA = 4;               // one pair of this many takes its exponentials on the FMA pipe
+#ifndef V0
+#define V0 4
+#endif
+constexpr int BY_FMA = V0;               // one pair of this many takes its exponentials on the FMA pipe
 constexpr float NOTHING = -1e31f;       // scores below belong to points left out
 
 template <typename T, int D, bool WEIGHTS>
@@ -102,7 +105,7 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
     bool ok = true;
 
     if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == 8 && elect_one()) {
             // ---------------------------------------------------------------- TMA
             for (int t = 0; t < halves; ++t) {
@@ -257,10 +260,9 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
 #pragma unroll
                 for (int i = 0; i < TILE; i += 8)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) top[k] = max_or_nan(top[k], max_or_nan(__uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1])));
-                float now = max_or_nan(max_or_nan(top[0], top[1]), max_or_nan(top[2], top[3])) * p.scale_log2;
+                    for (int k = 0; k < 4; ++k) top[k] = max3(top[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
+                float now = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
                 if (WEIGHTS && now < NOTHING) now = -INFINITY;
-                if (!(now < INFINITY)) ref = NAN;            // a score that is NaN or infinite makes its row NaN, from here on
                 const bool grown = now > ref + GROWTH;       // (also the first finite maximum: the reference is -infinity until then)
                 if (__any_sync(0xffffffffu, grown)) {
                     const float factor = grown ? ex2(ref - now) : 1.f;
@@ -376,24 +378,33 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
 //   warp 8   TMA of the blocks
 //   warp 9   MMAs: the sums of block j, and S and T of block j + 2 as soon as block j has left their columns: S when it has been read (dq) or its P
 //            has been used (dv), T when its ds has been used
-//   warp 10  dq: weights of the block's points, rows of points left out zeroed; dk, dv: lse and D of the block's queries
+//   warp 10  dq: weights of the block's points, rows of points left out zeroed
 //   warps 0-3 and 4-7  element-wise, blocks of even and of odd number; thread = row; p while T is computed; p and ds go back over S and T
 // Blocks of 64 points need two buffers of S and T to keep both sides busy: 256 of the 512 columns.  An MMA of 64 columns that reads its
 // A operand from shared memory is bound by that (6 KB at 128 bytes per clock: 48 cycles instead of 32), so A1 and A2 are kept in TMEM; only for dk, dv of wide
 // heads, whose two sums take the other 256 columns, are they in shared memory.
+#ifndef V1
+#define V1 4
+#define V2 64
+#endif
+constexpr int BY_FMA_DKDV = V1, BY_FMA_DQ = V2;
 constexpr int BWD_THREADS = 384, BLOCK = 64, BSLAB = BLOCK * 128;
 
 template <int D, bool DKDV> struct Backward {
     static constexpr bool A_IN_TMEM = D == 64 || !DKDV;
     static constexpr int SLABS = D / 64, STAGES = D == 64 ? 8 : A_IN_TMEM ? 6 : 4, STAGE_BYTES = 2 * SLABS * BSLAB, A_BYTES = A_IN_TMEM ? 0 : 2 * SLABS * SLAB;
-    // dq: ones, and the weights' parts per stage (see the forward kernel)
-    static constexpr int EXTRA_BYTES = BLOCK * 32, OFF_ONES = A_BYTES + STAGES * STAGE_BYTES, OFF_W = OFF_ONES + (DKDV ? 0 : TILE * 32);
-    static constexpr size_t SMEM = OFF_W + (DKDV ? 0 : STAGES * EXTRA_BYTES) + 1024;
-    static constexpr int SLOTS = 8;         // at least the stages: a slot is written again when its block's stage is, or later
+    // Extra steps of the first products (see the forward kernel): one tile of 16 channels for each operand that takes part.
+    //   dq      S: ones x weights of the block's points
+    //   dk, dv  S: (weight of the row, ones) x (ones, -lse / scale of the block's queries), so that p = exp2(scale_log2 S); T: ones x -D, so that it is t - D
+    // (the queries' are written by the statistics kernel and copied with the block; with a warp of this kernel that made them, it was that warp's 1180 cycles
+    // per block that the others waited for)
+    static constexpr int EXTRA_A = TILE * 32, EXTRA_B = DKDV ? BLOCK * 16 : BLOCK * 32, EXTRAS = DKDV ? 2 : 1;
+    static constexpr int OFF_XA = A_BYTES + STAGES * STAGE_BYTES, OFF_XB = OFF_XA + EXTRAS * EXTRA_A;
+    static constexpr size_t SMEM = OFF_XB + STAGES * EXTRAS * EXTRA_B + 1024;
     // TMEM columns: buffers of (S, T), sums, operands
     static constexpr int T_BUF = 0, T_ACC = 256, T_A = T_ACC + (DKDV ? 2 : 1) * D;
     static_assert(T_A + (A_IN_TMEM ? D : 0) <= 512, "TMEM");
-    enum { A_FULL = 0, A_READY = 1, FULL = 2, READY = FULL + STAGES, FREE = READY + STAGES, W_READY = FREE + STAGES, S_FULL = W_READY + SLOTS, T_FULL = S_FULL + 2,
+    enum { A_FULL = 0, A_READY = 1, FULL = 2, READY = FULL + STAGES, FREE = READY + STAGES, S_FULL = FREE + STAGES, T_FULL = S_FULL + 2,
            S_DONE = T_FULL + 2 /* S read (dq) or P ready (dk, dv) */, D_READY = S_DONE + 2, ACC_DONE = D_READY + 2, COUNT };
 };
 
@@ -402,12 +413,12 @@ __global__ void __launch_bounds__(BWD_THREADS, 1)
 attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats stats, const __grid_constant__ CUtensorMap map_a1, const __grid_constant__ CUtensorMap map_a2,
                           const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_b2, int tiles) {
     using K = Backward<D, DKDV>;
-    constexpr bool COLUMNS = DKDV;                      // statistics are read per streamed point
     constexpr bool CLEARED = !DKDV && WEIGHTS;          // streamed points may be left out
+    constexpr bool EXTRA = DKDV || WEIGHTS;
+    static_assert(BLOCK == STATS_BLOCK, "the statistics kernel's blocks");
     extern __shared__ unsigned char raw[];
     unsigned char* base = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     __shared__ unsigned long long bars[K::COUNT];
-    __shared__ __align__(16) float column[COLUMNS ? K::SLOTS : 1][2][BLOCK];        // -lse, -D
     __shared__ uint32_t tmem_s;
     __shared__ int fail_s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -421,7 +432,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     auto stage = [&](int st) { return s32(base) + K::A_BYTES + st * K::STAGE_BYTES; };
 
     if (tid == 0) {
-        for (int i = 0; i < K::COUNT; ++i) mb_init(bar(i), i == K::A_READY && K::A_IN_TMEM ? 8 : i >= K::S_DONE && i < K::ACC_DONE ? 4 : 1);
+        for (int i = 0; i < K::COUNT; ++i) mb_init(bar(i), i == K::A_READY ? (K::A_IN_TMEM ? 8 : WEIGHTS ? 5 : 4) : i >= K::S_DONE && i < K::ACC_DONE ? 4 : 1);
         fail_s = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -429,10 +440,11 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(s32(&tmem_s)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
-    if (CLEARED) {
-        for (int e = tid; e < TILE * 2; e += BWD_THREADS)
-            *reinterpret_cast<uint4*>(base + K::OFF_ONES + e * 16) = (e & 8) ? make_uint4(0, 0, 0, 0) : make_uint4(EXTRA_ONES_0, EXTRA_ONES_1, 0, 0);
-        for (int e = tid; e < K::STAGES * K::EXTRA_BYTES / 16; e += BWD_THREADS) *reinterpret_cast<uint4*>(base + K::OFF_W + e * 16) = make_uint4(0, 0, 0, 0);
+    if (EXTRA) {
+        // ones (the tile of S for dk, dv gets its rows' weights later), and zeros behind what is written per block
+        for (int e = tid; e < K::EXTRAS * K::EXTRA_A / 16; e += BWD_THREADS)
+            *reinterpret_cast<uint4*>(base + K::OFF_XA + e * 16) = (e & 8) ? make_uint4(0, 0, 0, 0) : make_uint4(EXTRA_ONES_0, EXTRA_ONES_1, 0, 0);
+        for (int e = tid; !DKDV && e < K::STAGES * K::EXTRAS * K::EXTRA_B / 16; e += BWD_THREADS) *reinterpret_cast<uint4*>(base + K::OFF_XB + e * 16) = make_uint4(0, 0, 0, 0);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     tm_before();
@@ -442,7 +454,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     bool ok = true;
 
     if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == 8 && elect_one()) {
             // ---------------------------------------------------------------- TMA
             if (!K::A_IN_TMEM) {
@@ -458,7 +470,9 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                 if (turn > 0) ok = mb_wait(bar(K::FREE + st), (turn - 1) & 1, ok);
                 if (!ok) break;
                 const int g = DKDV ? it / per_head : 0, point = (it - g * per_head) * BLOCK, h = DKDV ? head * p.G + g : hk;
-                mb_expect(bar(K::FULL + st), 2 * slabs * BSLAB);
+                mb_expect(bar(K::FULL + st), 2 * slabs * BSLAB + (DKDV ? 2 * K::EXTRA_B : 0));
+                if (DKDV)
+                    bulk_load(s32(base) + K::OFF_XB + st * 2 * K::EXTRA_B, stats.extra + (((int64_t)b * p.Hq + h) * per_head + point / BLOCK) * 2 * BLOCK, 2 * K::EXTRA_B, bar(K::FULL + st));
                 for (int s = 0; s < slabs; ++s) {
                     tma_load(stage(st) + s * BSLAB, &map_b1, s * 64, point, h, b, bar(K::FULL + st));
                     tma_load(stage(st) + (K::SLABS + s) * BSLAB, &map_b2, s * 64, point, h, b, bar(K::FULL + st));
@@ -472,7 +486,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             const uint32_t ids = idesc<T>(BLOCK, false), ido = idesc<T>(steps * 16, true);
             const uint32_t idw = idesc<__nv_bfloat16>(BLOCK, false);
             const uint32_t da = desc_channels(s32(base)), db = desc_channels(stage(0)), dp = desc_points(stage(0), BSLAB);
-            const uint32_t dones = desc_extra(s32(base) + K::OFF_ONES), dw = desc_extra(s32(base) + K::OFF_W);
+            const uint32_t dxa = desc_extra(s32(base) + K::OFF_XA), dxb = DKDV ? desc_dense(s32(base) + K::OFF_XB) : desc_extra(s32(base) + K::OFF_XB);
             auto ready = [&](int it) { return mb_wait(bar((CLEARED ? K::READY : K::FULL) + it % K::STAGES), (it / K::STAGES) & 1, true); };
             // which: 0 S, 1 T
             auto first = [&](int it, int which) {
@@ -484,10 +498,10 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                         if constexpr (K::A_IN_TMEM) mma_ts(to, tm + K::T_A + which * (D / 2) + ks * 8, bd + (ks >> 2) * (BSLAB >> 4) + (ks & 3) * 2, ids, ks > 0);
                         else mma_ss(to, da + (which * K::SLABS + (ks >> 2)) * (SLAB >> 4) + (ks & 3) * 2, bd + (ks >> 2) * (BSLAB >> 4) + (ks & 3) * 2, ids, ks > 0);
                     }
-                if (CLEARED && which == 0) mma_ss<DESC_EXTRA_HIGH>(to, dones, dw + st * (K::EXTRA_BYTES >> 4), idw, 1);
+                if (EXTRA && which < K::EXTRAS) mma_ss<DESC_EXTRA_HIGH, DKDV ? DESC_DENSE_HIGH : DESC_EXTRA_HIGH>(to, dxa + which * (K::EXTRA_A >> 4), dxb + (st * K::EXTRAS + which) * (K::EXTRA_B >> 4), idw, 1);
                 mma_commit(bar((which == 0 ? K::S_FULL : K::T_FULL) + (it & 1)));
             };
-            ok = mb_wait(bar(K::A_IN_TMEM || (DKDV && WEIGHTS) ? K::A_READY : K::A_FULL), 0, true);
+            ok = mb_wait(bar(K::A_READY), 0, true) && (K::A_IN_TMEM || mb_wait(bar(K::A_FULL), 0, true));
             tm_after();
             for (int it = 0; it < 2 && it < count && ok; ++it) {
                 ok = ready(it);
@@ -521,74 +535,57 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             }
             mma_commit(bar(K::ACC_DONE));
             mb_wait(bar(K::ACC_DONE), 0, true);
-        } else if ((COLUMNS || CLEARED) && warp == 10) {
-            // ---------------------------------------------------------------- what is read per streamed point
-            if (!K::A_IN_TMEM && WEIGHTS) {
-                ok = all_lanes(mb_wait(bar(K::A_FULL), 0, ok));
-                for (int r = 0; r < 4 && ok; ++r) {
-                    const int n = row0 + r * 32 + lane;
-                    const uint32_t gone = __ballot_sync(0xffffffffu, n < p.Nk && weight2(weights, n) == -INFINITY);
-                    for (int which = 0; which < 2; ++which) zero_rows(base + which * K::SLABS * SLAB, slabs, SLAB, r, gone, lane);
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mb_arrive(bar(K::A_READY));
+        } else if (DKDV && WEIGHTS && !K::A_IN_TMEM && warp == 10) {
+            // ---------------------------------------------------------------- rows of keys left out
+            ok = all_lanes(mb_wait(bar(K::A_FULL), 0, ok));
+            for (int r = 0; r < 4 && ok; ++r) {
+                const int n = row0 + r * 32 + lane;
+                const uint32_t gone = __ballot_sync(0xffffffffu, n < p.Nk && weight2(weights, n) == -INFINITY);
+                for (int which = 0; which < 2; ++which) zero_rows(base + which * K::SLABS * SLAB, slabs, SLAB, r, gone, lane);
             }
-            float x[2], y[2];
-            auto fetch = [&](int it) {
-                const int g = DKDV ? it / per_head : 0;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mb_arrive(bar(K::A_READY));
+        } else if (CLEARED && warp == 10) {
+            // ---------------------------------------------------------------- weights of the streamed points, two blocks ahead
+            const float unscale = 1.f / p.scale;
+            float x[2][2];
+            auto fetch = [&](int it, float (&xs)[2]) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const int n = (it - g * per_head) * BLOCK + i * 32 + lane;
-                    if (DKDV) {
-                        const int64_t at = ((int64_t)b * p.Hq + head * p.G + g) * p.Nq + n;
-                        x[i] = n < M ? -stats.lse2[at] : -INFINITY;
-                        y[i] = n < M ? -stats.D[at] : 0.f;
-                    } else {
-                        x[i] = n >= M ? -INFINITY : weights == nullptr ? 0.f : weights[n];
-                        y[i] = 0.f;
-                    }
+                    const int n = it * BLOCK + i * 32 + lane;
+                    xs[i] = n >= M ? -INFINITY : weights[n];
                 }
             };
-            fetch(0);
-            for (int it = 0; it < count && ok; ++it) {
-                const int st = it % K::STAGES, slot = it % K::SLOTS;
-                float now[2], also[2];
-                uint32_t gone[2];
+            auto write = [&](int it, const float (&xs)[2]) {
+                const int st = it % K::STAGES;
                 uint2 parts[2];
+                uint32_t gone[2];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    now[i] = x[i]; also[i] = y[i];
-                    if (CLEARED) {
-                        const bool out = x[i] <= EXCLUDED;
-                        gone[i] = __ballot_sync(0xffffffffu, out && it * BLOCK + i * 32 + lane < M);
-                        parts[i] = out ? make_uint2(EXTRA_OUT, 0) : extra_parts(x[i] * (1.f / p.scale));
-                    }
+                    const bool out = xs[i] <= EXCLUDED;
+                    gone[i] = __ballot_sync(0xffffffffu, out && it * BLOCK + i * 32 + lane < M);
+                    parts[i] = out ? make_uint2(EXTRA_OUT, 0) : extra_parts(xs[i] * unscale);
                 }
-                if (it + 1 < count) fetch(it + 1);
-                ok = all_lanes(mb_wait(bar(K::FULL + st), (it / K::STAGES) & 1, ok));       // (then the slot's and the stage's last readers are done, too)
-                if (!ok) break;
+                ok = all_lanes(mb_wait(bar(K::FULL + st), (it / K::STAGES) & 1, ok));       // (then the stage's last readers are done, too)
+                if (!ok) return;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if (COLUMNS) {
-                        column[COLUMNS ? slot : 0][0][i * 32 + lane] = now[i];
-                        column[COLUMNS ? slot : 0][1][i * 32 + lane] = also[i];
-                    }
-                    if (CLEARED) *reinterpret_cast<uint2*>(base + K::OFF_W + st * K::EXTRA_BYTES + extra_at(i * 32 + lane)) = parts[i];
-                }
-                if (CLEARED) {
-                    if (gone[0] | gone[1])
+                for (int i = 0; i < 2; ++i) *reinterpret_cast<uint2*>(base + K::OFF_XB + st * K::EXTRA_B + extra_at(i * 32 + lane)) = parts[i];
+                if (gone[0] | gone[1])
 #pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            for (int which = 0; which < 2; ++which)
-                                zero_rows(base + K::A_BYTES + st * K::STAGE_BYTES + which * K::SLABS * BSLAB, slabs, BSLAB, i, gone[i], lane);
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                }
+                    for (int i = 0; i < 2; ++i)
+                        for (int which = 0; which < 2; ++which) zero_rows(base + K::A_BYTES + st * K::STAGE_BYTES + which * K::SLABS * BSLAB, slabs, BSLAB, i, gone[i], lane);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
-                if (lane == 0) {
-                    if (COLUMNS) mb_arrive(bar(K::W_READY + slot));
-                    if (CLEARED) mb_arrive(bar(K::READY + st));
-                }
+                if (lane == 0) mb_arrive(bar(K::READY + st));
+            };
+            fetch(0, x[0]);
+            if (count > 1) fetch(1, x[1]);
+            for (int it = 0; it < count && ok; it += 2) {
+                write(it, x[0]);
+                if (it + 2 < count) fetch(it + 2, x[0]);
+                if (it + 1 < count && ok) write(it + 1, x[1]);
+                if (it + 3 < count) fetch(it + 3, x[1]);
             }
         }
     } else {
@@ -597,25 +594,32 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const bool there = row < N;
         // ---------------------------------------------------------------- operands: group 0 those of S, group 1 those of T
-        float w = 0.f;          // dk, dv: the row's weight
-        if (DKDV && WEIGHTS) w = there ? weight2(weights, row) : -INFINITY;
+        bool taken = there;         // dk, dv: whether the row's point takes part
+        if (DKDV) {
+            const float weight = !there ? -INFINITY : WEIGHTS ? weights[row] : 0.f;
+            taken = weight > EXCLUDED || weight != weight;
+            if (group == 0) {
+                const uint2 parts = taken ? extra_parts(weight * (1.f / p.scale)) : make_uint2(EXTRA_OUT, 0);
+                *reinterpret_cast<uint4*>(base + K::OFF_XA + extra_at((warp & 3) * 32 + lane)) = make_uint4(parts.x, parts.y | 0x3f800000u, EXTRA_ONES_0, 0);
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+        }
         if (K::A_IN_TMEM) {
             const View& v = DKDV ? (group == 0 ? p.k : p.v) : (group == 0 ? p.q : p.dout);
             const uint4* from = reinterpret_cast<const uint4*>(static_cast<const T*>(v.data) + b * v.batch + head * v.head + (there ? row : 0) * v.point);
-            const bool take = there && w != -INFINITY;
 #pragma unroll
             for (int half = 0; half < D / 64; ++half) {
                 uint32_t x[32];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const uint4 q = take && half * 64 + i * 8 < p.C ? from[half * 8 + i] : make_uint4(0, 0, 0, 0);
+                    const uint4 q = taken && half * 64 + i * 8 < p.C ? from[half * 8 + i] : make_uint4(0, 0, 0, 0);
                     x[4 * i] = q.x; x[4 * i + 1] = q.y; x[4 * i + 2] = q.z; x[4 * i + 3] = q.w;
                 }
                 tm_st32(tm + K::T_A + group * (D / 2) + half * 32 + lanes, x);
             }
             tm_st_wait();
-            warp_arrive(bar(K::A_READY), lane);
         }
+        if (K::A_IN_TMEM || group == 0) warp_arrive(bar(K::A_READY), lane);
         const float factor = ds_scale<T>(stats, b * p.Hk + hk);
         float neg_lse = 0.f, neg_D = 0.f;       // dq: the row's
         if (!DKDV && there) {
@@ -623,12 +627,11 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             neg_lse = -stats.lse2[at];
             neg_D = -stats.D[at];
         }
-        const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), row_x = DKDV ? pack2(w, w) : pack2(neg_lse, neg_lse), row_D = pack2(neg_D, neg_D), factor2 = pack2(factor, factor);
+        const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), row_x = pack2(neg_lse, neg_lse), row_D = pack2(neg_D, neg_D), factor2 = pack2(factor, factor);
         for (int it = group; it < count && ok; it += 2) {
             const uint32_t from = tm + K::T_BUF + group * 2 * BLOCK + lanes;
             uint32_t s[BLOCK];
             ok = all_lanes(mb_wait(bar(K::S_FULL + group), (it >> 1) & 1, ok));
-            if (COLUMNS) ok = all_lanes(mb_wait(bar(K::W_READY + it % K::SLOTS), (it / K::SLOTS) & 1, ok)) && ok;
             if (!ok) break;
             tm_after();
             tm_ld32(s, from);
@@ -644,22 +647,18 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                 for (int i = 0; i < BLOCK; ++i)
                     if (i >= left) s[i] = 0xff800000u;
             }
-            const float4* c0 = reinterpret_cast<const float4*>(column[COLUMNS ? it % K::SLOTS : 0][0]);
-            const float4* c1 = reinterpret_cast<const float4*>(column[COLUMNS ? it % K::SLOTS : 0][1]);
 #pragma unroll
-            for (int i = 0; i < BLOCK / 4; ++i) {
-                float4 c;
-                if (COLUMNS) c = c0[i];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int at = 4 * i + 2 * k;
-                    uint64_t x2 = fma2(pack2(__uint_as_float(s[at]), __uint_as_float(s[at + 1])), scale2, !COLUMNS ? row_x : k == 0 ? pack2(c.x, c.y) : pack2(c.z, c.w));
-                    if (DKDV && WEIGHTS) x2 = add2(x2, row_x);
-                    float e0, e1;
+            for (int i = 0; i < 32; ++i) {
+                const uint64_t s2 = pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), x2 = DKDV ? mul2(s2, scale2) : fma2(s2, scale2, row_x);
+                float e0, e1;
+                if (i % (DKDV ? BY_FMA_DKDV : BY_FMA_DQ) == 1) {
+                    exp2_by_fma(x2, e0, e1);
+                } else {
                     unpack2(x2, e0, e1);
-                    s[at] = __float_as_uint(ex2(e0));
-                    s[at + 1] = __float_as_uint(ex2(e1));
+                    e0 = ex2(e0); e1 = ex2(e1);
                 }
+                s[2 * i] = __float_as_uint(e0);
+                s[2 * i + 1] = __float_as_uint(e1);
             }
             if (DKDV) {
                 uint32_t pr[32];
@@ -677,18 +676,13 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             tm_ld32(t + 32, from + BLOCK + 32);
             tm_ld_wait();
 #pragma unroll
-            for (int i = 0; i < BLOCK / 4; ++i) {
-                float4 c;
-                if (COLUMNS) c = c1[i];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const int at = 4 * i + 2 * k;
-                    uint64_t d2 = add2(pack2(__uint_as_float(t[at]), __uint_as_float(t[at + 1])), !COLUMNS ? row_D : k == 0 ? pack2(c.x, c.y) : pack2(c.z, c.w));
-                    if (SHIFT<T> != 0.f) d2 = mul2(d2, factor2);
-                    float d0, d1;
-                    unpack2(mul2(d2, pack2(__uint_as_float(s[at]), __uint_as_float(s[at + 1]))), d0, d1);
-                    ds[2 * i + k] = pack16<T>(d0, d1);
-                }
+            for (int i = 0; i < 32; ++i) {
+                uint64_t d2 = pack2(__uint_as_float(t[2 * i]), __uint_as_float(t[2 * i + 1]));
+                if (!DKDV) d2 = add2(d2, row_D);
+                if (SHIFT<T> != 0.f) d2 = mul2(d2, factor2);
+                float d0, d1;
+                unpack2(mul2(d2, pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]))), d0, d1);
+                ds[i] = pack16<T>(d0, d1);
             }
             tm_st32(from + BLOCK, ds);
             tm_st_wait();
@@ -699,6 +693,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
         if (ok) {
             tm_after();
             const float unshift = ex2(-SHIFT<T>), back = DKDV && group == 1 ? unshift : p.scale * unshift / factor;
+            const bool zero = DKDV && !taken;       // (exponentials on the FMA pipe end at 2^-126)
             const View& v = DKDV ? (group == 0 ? p.dk : p.dv) : p.dq;
             T* out = static_cast<T*>(v.data) + b * v.batch + head * v.head + (int64_t)row * v.point;
             for (int c = DKDV ? 0 : group * 32; c < p.C; c += DKDV ? 32 : 64) {
@@ -711,7 +706,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                     if (c + i < p.C) {
                         uint32_t x[4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) x[k] = pack16<T>(__uint_as_float(o[i + 2 * k]) * back, __uint_as_float(o[i + 2 * k + 1]) * back);
+                        for (int k = 0; k < 4; ++k) x[k] = zero ? 0u : pack16<T>(__uint_as_float(o[i + 2 * k]) * back, __uint_as_float(o[i + 2 * k + 1]) * back);
                         *reinterpret_cast<uint4*>(out + c + i) = make_uint4(x[0], x[1], x[2], x[3]);
                     }
             }
