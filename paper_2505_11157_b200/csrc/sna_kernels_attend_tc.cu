@@ -375,20 +375,22 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
 // dq and dk, dv are the same walk with the sides exchanged.  A block owns 128 rows x (queries: dq; keys: dk, dv) with their operands A1 (q or k) and
 // A2 (dout or v), and walks the other side's points in blocks of 64, B1 (k or q) and B2 (v or dout):
 //   S = A1 B1^T, T = A2 B2^T;  p = exp(S - lse), ds = p (T - D);  acc1 += ds B1 (dq or dk);  dk, dv: acc2 += p B2 (dv)
-//   warp 8   TMA of the blocks
-//   warp 9   MMAs: the sums of block j, and S and T of block j + 2 as soon as block j has left their columns: S when it has been read (dq) or its P
-//            has been used (dv), T when its ds has been used
-//   warp 10  dq: weights of the block's points, rows of points left out zeroed
-//   warps 0-3 and 4-7  element-wise, blocks of even and of odd number; thread = row; p while T is computed; p and ds go back over S and T
+//   warp 16  TMA of the blocks
+//   warps 17, 19  MMAs, as soon as block j has left the columns: dv of block j and S of block j + 2 (dq: S alone, when S has been read); dk or dq of
+//            block j and T of block j + 2.  (One thread for all of them was busy all the time: a wait costs it 60 cycles or more even if it need not wait.)
+//   warp 18  dq: weights of the block's points, rows of points left out zeroed
+//   warps 0-15  element-wise: a group of four warps takes one half of the columns of the blocks of even or of odd number, thread = row; p while T is computed;
+//            p and ds go back over S and T, each half over its own.  (Two groups, with whole rows per thread, were bound by latencies: issue slots 39 %,
+//            special-function unit 55 % busy.)
 // Blocks of 64 points need two buffers of S and T to keep both sides busy: 256 of the 512 columns.  An MMA of 64 columns that reads its
 // A operand from shared memory is bound by that (6 KB at 128 bytes per clock: 48 cycles instead of 32), so A1 and A2 are kept in TMEM; only for dk, dv of wide
 // heads, whose two sums take the other 256 columns, are they in shared memory.
 #ifndef V1
 #define V1 4
-#define V2 64
+#define V2 4
 #endif
 constexpr int BY_FMA_DKDV = V1, BY_FMA_DQ = V2;
-constexpr int BWD_THREADS = 384, BLOCK = 64, BSLAB = BLOCK * 128;
+constexpr int BWD_THREADS = 640, BLOCK = 64, BSLAB = BLOCK * 128;
 
 template <int D, bool DKDV> struct Backward {
     static constexpr bool A_IN_TMEM = D == 64 || !DKDV;
@@ -432,7 +434,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     auto stage = [&](int st) { return s32(base) + K::A_BYTES + st * K::STAGE_BYTES; };
 
     if (tid == 0) {
-        for (int i = 0; i < K::COUNT; ++i) mb_init(bar(i), i == K::A_READY ? (K::A_IN_TMEM ? 8 : WEIGHTS ? 5 : 4) : i >= K::S_DONE && i < K::ACC_DONE ? 4 : 1);
+        for (int i = 0; i < K::COUNT; ++i) mb_init(bar(i), i == K::A_READY ? (K::A_IN_TMEM ? 16 : WEIGHTS ? 5 : 4) : i >= K::S_DONE && i < K::ACC_DONE ? 8 : i == K::ACC_DONE || (DKDV && i >= K::FREE && i < K::S_FULL) ? 2 : 1);
         fail_s = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -453,9 +455,9 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     const uint32_t tm = tmem_s;
     bool ok = true;
 
-    if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-        if (warp == 8 && elect_one()) {
+    if (warp >= 16) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (warp == 16 && elect_one()) {
             // ---------------------------------------------------------------- TMA
             if (!K::A_IN_TMEM) {
                 mb_expect(bar(K::A_FULL), 2 * slabs * SLAB);
@@ -481,61 +483,49 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             // the copies under way (all there already if all went well)
             if (!K::A_IN_TMEM) mb_wait(bar(K::A_FULL), 0, true);
             for (int i = max(0, it - K::STAGES); i < it; ++i) mb_wait(bar(K::FULL + i % K::STAGES), (i / K::STAGES) & 1, true);
-        } else if (warp == 9 && elect_one()) {
-            // ---------------------------------------------------------------- MMAs
-            const uint32_t ids = idesc<T>(BLOCK, false), ido = idesc<T>(steps * 16, true);
-            const uint32_t idw = idesc<__nv_bfloat16>(BLOCK, false);
-            const uint32_t da = desc_channels(s32(base)), db = desc_channels(stage(0)), dp = desc_points(stage(0), BSLAB);
-            const uint32_t dxa = desc_extra(s32(base) + K::OFF_XA), dxb = DKDV ? desc_dense(s32(base) + K::OFF_XB) : desc_extra(s32(base) + K::OFF_XB);
-            auto ready = [&](int it) { return mb_wait(bar((CLEARED ? K::READY : K::FULL) + it % K::STAGES), (it / K::STAGES) & 1, true); };
-            // which: 0 S, 1 T
-            auto first = [&](int it, int which) {
+        } else if ((warp == 17 || warp == 19) && elect_one()) {
+            // ---------------------------------------------------------------- MMAs: warp 17 S and dv, warp 19 T and dq or dk
+            const int which = warp == 17 ? 0 : 1;
+            const uint32_t ids = idesc<T>(BLOCK, false), ido = idesc<T>(steps * 16, true), idw = idesc<__nv_bfloat16>(BLOCK, false);
+            const uint32_t da = desc_channels(s32(base) + which * K::SLABS * SLAB), db = desc_channels(stage(0) + which * K::SLABS * BSLAB);
+            const uint32_t dp = desc_points(stage(0) + (which == 0 ? K::SLABS * BSLAB : 0), BSLAB), ta = tm + K::T_A + which * (D / 2);
+            const uint32_t dxa = desc_extra(s32(base) + K::OFF_XA + which * K::EXTRA_A);
+            const uint32_t dxb = (DKDV ? desc_dense(s32(base) + K::OFF_XB) : desc_extra(s32(base) + K::OFF_XB)) + which * (K::EXTRA_B >> 4);
+            const bool sums = DKDV || which == 1, extra = EXTRA && which < K::EXTRAS;
+            const int done = (which == 0 ? K::S_DONE : K::D_READY), full = (which == 0 ? K::S_FULL : K::T_FULL);
+            auto first = [&](int it) {
                 const int st = it % K::STAGES;
-                const uint32_t to = tm + K::T_BUF + (it & 1) * 2 * BLOCK + which * BLOCK, bd = db + st * (K::STAGE_BYTES >> 4) + which * K::SLABS * (BSLAB >> 4);
+                if (!mb_wait(bar((CLEARED ? K::READY : K::FULL) + st), (it / K::STAGES) & 1, true)) return false;
+                const uint32_t to = tm + K::T_BUF + (it & 1) * 2 * BLOCK + which * BLOCK, bd = db + st * (K::STAGE_BYTES >> 4);
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks)
                     if (ks < steps) {
-                        if constexpr (K::A_IN_TMEM) mma_ts(to, tm + K::T_A + which * (D / 2) + ks * 8, bd + (ks >> 2) * (BSLAB >> 4) + (ks & 3) * 2, ids, ks > 0);
-                        else mma_ss(to, da + (which * K::SLABS + (ks >> 2)) * (SLAB >> 4) + (ks & 3) * 2, bd + (ks >> 2) * (BSLAB >> 4) + (ks & 3) * 2, ids, ks > 0);
+                        if constexpr (K::A_IN_TMEM) mma_ts(to, ta + ks * 8, bd + (ks >> 2) * (BSLAB >> 4) + (ks & 3) * 2, ids, ks > 0);
+                        else mma_ss(to, da + (ks >> 2) * (SLAB >> 4) + (ks & 3) * 2, bd + (ks >> 2) * (BSLAB >> 4) + (ks & 3) * 2, ids, ks > 0);
                     }
-                if (EXTRA && which < K::EXTRAS) mma_ss<DESC_EXTRA_HIGH, DKDV ? DESC_DENSE_HIGH : DESC_EXTRA_HIGH>(to, dxa + which * (K::EXTRA_A >> 4), dxb + (st * K::EXTRAS + which) * (K::EXTRA_B >> 4), idw, 1);
-                mma_commit(bar((which == 0 ? K::S_FULL : K::T_FULL) + (it & 1)));
+                if (extra) mma_ss<DESC_EXTRA_HIGH, DKDV ? DESC_DENSE_HIGH : DESC_EXTRA_HIGH>(to, dxa, dxb + st * (K::EXTRAS * K::EXTRA_B >> 4), idw, 1);
+                mma_commit(bar(full + (it & 1)));
+                return true;
             };
             ok = mb_wait(bar(K::A_READY), 0, true) && (K::A_IN_TMEM || mb_wait(bar(K::A_FULL), 0, true));
             tm_after();
-            for (int it = 0; it < 2 && it < count && ok; ++it) {
-                ok = ready(it);
-                if (!ok) break;
-                first(it, 0);
-                first(it, 1);
-            }
+            for (int it = 0; it < 2 && it < count && ok; ++it) ok = first(it);
             for (int it = 0; it < count && ok; ++it) {
-                const int st = it % K::STAGES;
-                const uint32_t at = dp + st * (K::STAGE_BYTES >> 4), from = tm + K::T_BUF + (it & 1) * 2 * BLOCK;
-                const bool more = it + 2 < count;
-                ok = mb_wait(bar(K::S_DONE + (it & 1)), (it >> 1) & 1, true);
+                ok = mb_wait(bar(done + (it & 1)), (it >> 1) & 1, true);
                 if (!ok) break;
                 tm_after();
-                if (DKDV)
+                if (sums) {
+                    const int st = it % K::STAGES;
+                    const uint32_t at = dp + st * (K::STAGE_BYTES >> 4), from = tm + K::T_BUF + (it & 1) * 2 * BLOCK + which * BLOCK, to = tm + K::T_ACC + (which == 0 ? D : 0);
 #pragma unroll
-                    for (int kk = 0; kk < BLOCK / 16; ++kk)
-                        mma_ts(tm + K::T_ACC + D, from + kk * 8, at + K::SLABS * (BSLAB >> 4) + kk * (2048 >> 4), ido, it > 0 || kk > 0);
-                if (more) {
-                    ok = ready(it + 2);
-                    if (!ok) break;
-                    first(it + 2, 0);
+                    for (int kk = 0; kk < BLOCK / 16; ++kk) mma_ts(to, from + (kk >> 1) * 32 + (kk & 1) * 8, at + kk * (2048 >> 4), ido, it > 0 || kk > 0);
+                    mma_commit(bar(K::FREE + st));
                 }
-                ok = mb_wait(bar(K::D_READY + (it & 1)), (it >> 1) & 1, true);
-                if (!ok) break;
-                tm_after();
-#pragma unroll
-                for (int kk = 0; kk < BLOCK / 16; ++kk) mma_ts(tm + K::T_ACC, from + BLOCK + kk * 8, at + kk * (2048 >> 4), ido, it > 0 || kk > 0);
-                mma_commit(bar(K::FREE + st));
-                if (more) first(it + 2, 1);
+                if (it + 2 < count) ok = first(it + 2);
             }
             mma_commit(bar(K::ACC_DONE));
             mb_wait(bar(K::ACC_DONE), 0, true);
-        } else if (DKDV && WEIGHTS && !K::A_IN_TMEM && warp == 10) {
+        } else if (DKDV && WEIGHTS && !K::A_IN_TMEM && warp == 18) {
             // ---------------------------------------------------------------- rows of keys left out
             ok = all_lanes(mb_wait(bar(K::A_FULL), 0, ok));
             for (int r = 0; r < 4 && ok; ++r) {
@@ -546,7 +536,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mb_arrive(bar(K::A_READY));
-        } else if (CLEARED && warp == 10) {
+        } else if (CLEARED && warp == 18) {
             // ---------------------------------------------------------------- weights of the streamed points, two blocks ahead
             const float unscale = 1.f / p.scale;
             float x[2][2];
@@ -589,16 +579,16 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        const int group = warp >> 2, row = row0 + (warp & 3) * 32 + lane;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+        const int group = (warp >> 2) & 1, half = warp >> 3, row = row0 + (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
         const bool there = row < N;
-        // ---------------------------------------------------------------- operands: group 0 those of S, group 1 those of T
+        // ---------------------------------------------------------------- operands: group 0 those of S, group 1 those of T, each half its channels
         bool taken = there;         // dk, dv: whether the row's point takes part
         if (DKDV) {
             const float weight = !there ? -INFINITY : WEIGHTS ? weights[row] : 0.f;
             taken = weight > EXCLUDED || weight != weight;
-            if (group == 0) {
+            if (group == 0 && half == 0) {
                 const uint2 parts = taken ? extra_parts(weight * (1.f / p.scale)) : make_uint2(EXTRA_OUT, 0);
                 *reinterpret_cast<uint4*>(base + K::OFF_XA + extra_at((warp & 3) * 32 + lane)) = make_uint4(parts.x, parts.y | 0x3f800000u, EXTRA_ONES_0, 0);
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -608,18 +598,19 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             const View& v = DKDV ? (group == 0 ? p.k : p.v) : (group == 0 ? p.q : p.dout);
             const uint4* from = reinterpret_cast<const uint4*>(static_cast<const T*>(v.data) + b * v.batch + head * v.head + (there ? row : 0) * v.point);
 #pragma unroll
-            for (int half = 0; half < D / 64; ++half) {
-                uint32_t x[32];
+            for (int part = 0; part < D / 64; ++part) {
+                const int c = half * (D / 2) + part * 32;
+                uint32_t x[16];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const uint4 q = taken && half * 64 + i * 8 < p.C ? from[half * 8 + i] : make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < 4; ++i) {
+                    const uint4 q = taken && c + i * 8 < p.C ? from[c / 8 + i] : make_uint4(0, 0, 0, 0);
                     x[4 * i] = q.x; x[4 * i + 1] = q.y; x[4 * i + 2] = q.z; x[4 * i + 3] = q.w;
                 }
-                tm_st32(tm + K::T_A + group * (D / 2) + half * 32 + lanes, x);
+                tm_st16(tm + K::T_A + group * (D / 2) + c / 2 + lanes, x);
             }
             tm_st_wait();
         }
-        if (K::A_IN_TMEM || group == 0) warp_arrive(bar(K::A_READY), lane);
+        if (K::A_IN_TMEM || (group == 0 && half == 0)) warp_arrive(bar(K::A_READY), lane);
         const float factor = ds_scale<T>(stats, b * p.Hk + hk);
         float neg_lse = 0.f, neg_D = 0.f;       // dq: the row's
         if (!DKDV && there) {
@@ -628,27 +619,24 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             neg_D = -stats.D[at];
         }
         const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), row_x = pack2(neg_lse, neg_lse), row_D = pack2(neg_D, neg_D), factor2 = pack2(factor, factor);
+        const uint32_t from = tm + K::T_BUF + group * 2 * BLOCK + half * 32 + lanes;
         for (int it = group; it < count && ok; it += 2) {
-            const uint32_t from = tm + K::T_BUF + group * 2 * BLOCK + lanes;
-            uint32_t s[BLOCK];
+            uint32_t s[32], t[32], x[16];
             ok = all_lanes(mb_wait(bar(K::S_FULL + group), (it >> 1) & 1, ok));
             if (!ok) break;
             tm_after();
             tm_ld32(s, from);
-            tm_ld32(s + 32, from + 32);
             tm_ld_wait();
-            if (!DKDV) {
-                warp_arrive(bar(K::S_DONE + group), lane);
-            }
+            if (!DKDV) warp_arrive(bar(K::S_DONE + group), lane);
             if (!DKDV && !WEIGHTS && (it + 1) * BLOCK > M) {
                 // points that are not there: zero rows, whose probability must not overflow (the scale is positive)
-                const int left = M - it * BLOCK;
+                const int left = M - it * BLOCK - half * 32;
 #pragma unroll
-                for (int i = 0; i < BLOCK; ++i)
+                for (int i = 0; i < 32; ++i)
                     if (i >= left) s[i] = 0xff800000u;
             }
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
+            for (int i = 0; i < 16; ++i) {
                 const uint64_t s2 = pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), x2 = DKDV ? mul2(s2, scale2) : fma2(s2, scale2, row_x);
                 float e0, e1;
                 if (i % (DKDV ? BY_FMA_DKDV : BY_FMA_DQ) == 1) {
@@ -659,36 +647,32 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                 }
                 s[2 * i] = __float_as_uint(e0);
                 s[2 * i + 1] = __float_as_uint(e1);
+                if (DKDV) x[i] = pack16<T>(e0, e1);
             }
             if (DKDV) {
-                uint32_t pr[32];
-#pragma unroll
-                for (int i = 0; i < 32; ++i) pr[i] = pack16<T>(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
-                tm_st32(from, pr);
+                tm_st16(from, x);
                 tm_st_wait();
                 warp_arrive(bar(K::S_DONE + group), lane);
             }
             ok = all_lanes(mb_wait(bar(K::T_FULL + group), (it >> 1) & 1, ok));
             if (!ok) break;
             tm_after();
-            uint32_t t[BLOCK], ds[32];
             tm_ld32(t, from + BLOCK);
-            tm_ld32(t + 32, from + BLOCK + 32);
             tm_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
+            for (int i = 0; i < 16; ++i) {
                 uint64_t d2 = pack2(__uint_as_float(t[2 * i]), __uint_as_float(t[2 * i + 1]));
                 if (!DKDV) d2 = add2(d2, row_D);
                 if (SHIFT<T> != 0.f) d2 = mul2(d2, factor2);
                 float d0, d1;
                 unpack2(mul2(d2, pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]))), d0, d1);
-                ds[i] = pack16<T>(d0, d1);
+                x[i] = pack16<T>(d0, d1);
             }
-            tm_st32(from + BLOCK, ds);
+            tm_st16(from + BLOCK, x);
             tm_st_wait();
             warp_arrive(bar(K::D_READY + group), lane);
         }
-        // ---------------------------------------------------------------- results: dq by halves of the channels, or dk by group 0 and dv by group 1
+        // ---------------------------------------------------------------- results in pieces of 32 channels: dq by all groups, or dk by group 0 and dv by group 1
         ok = all_lanes(mb_wait(bar(K::ACC_DONE), 0, ok)) && ok;
         if (ok) {
             tm_after();
@@ -696,7 +680,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             const bool zero = DKDV && !taken;       // (exponentials on the FMA pipe end at 2^-126)
             const View& v = DKDV ? (group == 0 ? p.dk : p.dv) : p.dq;
             T* out = static_cast<T*>(v.data) + b * v.batch + head * v.head + (int64_t)row * v.point;
-            for (int c = DKDV ? 0 : group * 32; c < p.C; c += DKDV ? 32 : 64) {
+            for (int c = 32 * (DKDV ? half : 2 * half + group); c < p.C; c += DKDV ? 64 : 128) {
                 uint32_t o[32];
                 tm_ld32(o, tm + K::T_ACC + (DKDV ? group * D : 0) + c + lanes);
                 tm_ld_wait();
@@ -704,10 +688,10 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
 #pragma unroll
                 for (int i = 0; i < 32; i += 8)
                     if (c + i < p.C) {
-                        uint32_t x[4];
+                        uint32_t y[4];
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) x[k] = zero ? 0u : pack16<T>(__uint_as_float(o[i + 2 * k]) * back, __uint_as_float(o[i + 2 * k + 1]) * back);
-                        *reinterpret_cast<uint4*>(out + c + i) = make_uint4(x[0], x[1], x[2], x[3]);
+                        for (int k = 0; k < 4; ++k) y[k] = zero ? 0u : pack16<T>(__uint_as_float(o[i + 2 * k]) * back, __uint_as_float(o[i + 2 * k + 1]) * back);
+                        *reinterpret_cast<uint4*>(out + c + i) = make_uint4(y[0], y[1], y[2], y[3]);
                     }
             }
         }
