@@ -110,13 +110,15 @@ __device__ __forceinline__ float weight2(const float* weights, int n) {
 
 // ---- forward ---------------------------------------------------------------------------------------------------------------
 
-template <int CP, int WM> constexpr int forward_smem() { return WM * 16 * CP * 2 + 4 * BN * CP * 2; }
+// Stages of (K, V): a memory-bound walk wants two under way (one station over 361x720, B = 2, 2 key heads of 64, bf16: 71 us with one)
+template <int WM> constexpr int FORWARD_STAGES = WM == 1 ? 3 : 2;
+template <int CP, int WM> constexpr int forward_smem() { return WM * 16 * CP * 2 + FORWARD_STAGES<WM> * 2 * BN * CP * 2; }
 
 // WM warps along the rows, WK = 4 / WM along the keys of a block.  partials: null, or sums [splits][rows][C] (first, so that vectors stay aligned) and statistics
 // [splits][rows].
 template <typename T, int CP, int WM>
-__global__ void __launch_bounds__(THREADS) attend_forward_kernel(const __grid_constant__ Problem p, int tiles, int splits, float* partials) {
-    constexpr int WK = WARPS / WM, BM = 16 * WM, KW = BN / WK, NT = KW / 8, CN = CP / 8;
+__global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_forward_kernel(const __grid_constant__ Problem p, int tiles, int splits, float* partials) {
+    constexpr int STAGES = FORWARD_STAGES<WM>, WK = WARPS / WM, BM = 16 * WM, KW = BN / WK, NT = KW / 8, CN = CP / 8;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(16) float bias[4][BN];
     const uint32_t tq = s32(smem), tkv = tq + BM * CP * 2;      // stages of (K, V)
@@ -139,17 +141,18 @@ __global__ void __launch_bounds__(THREADS) attend_forward_kernel(const __grid_co
     auto load_block = [&](int j) {
         if (j < last) {
             auto take = [&](int r) { return bias[j & 3][r] != -INFINITY; };
-            const uint32_t stage = tkv + (j & 1) * 2 * BN * CP * 2;
+            const uint32_t stage = tkv + ((j - first) % STAGES) * 2 * BN * CP * 2;
             load_rows<CP>(stage, kh, p.k.point, j * BN, p.Nk, BN, p.C, take);
             load_rows<CP>(stage + BN * CP * 2, vh, p.v.point, j * BN, p.Nk, BN, p.C, take);
         }
         commit();
     };
     load_stacked<CP>(tq, static_cast<const T*>(p.q.data) + b * p.q.batch + (int64_t)hk * p.G * p.q.head, p.q.head, p.q.point, row0, rows, p.Nq, BM, p.C);
-    load_bias(first);
-    load_bias(first + 1);
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) load_bias(first + i);
     __syncthreads();
-    load_block(first);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) load_block(first + i);
 
     float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f}, o[CN][4];
 #pragma unroll
@@ -158,11 +161,11 @@ __global__ void __launch_bounds__(THREADS) attend_forward_kernel(const __grid_co
         for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
 
     for (int j = first; j < last; ++j) {
-        load_bias(j + 2);
-        load_block(j + 1);
-        wait_group<1>();
+        load_bias(j + STAGES);
+        load_block(j + STAGES - 1);
+        wait_group<STAGES - 1>();
         __syncthreads();
-        const uint32_t tk = tkv + (j & 1) * 2 * BN * CP * 2, tv = tk + BN * CP * 2;
+        const uint32_t tk = tkv + ((j - first) % STAGES) * 2 * BN * CP * 2, tv = tk + BN * CP * 2;
         const int key0 = wk * KW;
         float s[NT][4];
 #pragma unroll
@@ -300,13 +303,16 @@ __global__ void __launch_bounds__(THREADS) attend_forward_kernel(const __grid_co
     }
 }
 
-// Joins the splits' results of a row: out = sum_s 2^(lse2_s - lse2) out_s.  One block of 128 threads per row; warp w takes the splits w, w + 4, ...
-template <typename T>
-__global__ void __launch_bounds__(THREADS) attend_join_kernel(const __grid_constant__ Problem p, int splits, const float* partials) {
-    __shared__ float sums[WARPS][128];
-    __shared__ float totals[WARPS];
-    const int64_t rows = rows_of(p), at = blockIdx.x;
+// Joins the splits' results of a row: out = sum_s 2^(lse2_s - lse2) out_s, the sum taken in a fixed order.
+// Few rows and many splits: a block of eight warps per row, warp w takes the splits w, w + 8, ...  Otherwise a warp per row.
+constexpr int JOIN_WARPS = 8;
+template <typename T, bool BLOCK_PER_ROW>
+__global__ void __launch_bounds__(32 * JOIN_WARPS) attend_join_kernel(const __grid_constant__ Problem p, int splits, const float* partials) {
+    __shared__ float sums[BLOCK_PER_ROW ? JOIN_WARPS : 1][128];
+    __shared__ float totals[JOIN_WARPS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t rows = rows_of(p), at = BLOCK_PER_ROW ? blockIdx.x : (int64_t)blockIdx.x * JOIN_WARPS + warp;
+    if (at >= rows) return;         // (whole warps; whole blocks where they meet)
     const float* statistics = partials + splits * rows * p.C;
     float top = -INFINITY;
     for (int s = lane; s < splits; s += 32) top = fmaxf(top, statistics[s * rows + at]);
@@ -314,25 +320,38 @@ __global__ void __launch_bounds__(THREADS) attend_join_kernel(const __grid_const
     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
     const float base = top == -INFINITY ? 0.f : top;
     float sum[4] = {0.f, 0.f, 0.f, 0.f}, total = 0.f;
-    for (int s = warp; s < splits; s += WARPS) {
+#pragma unroll 4
+    for (int s = BLOCK_PER_ROW ? warp : 0; s < splits; s += BLOCK_PER_ROW ? JOIN_WARPS : 1) {
         const float w = ex2(statistics[s * rows + at] - base);
         total += w;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (lane + 32 * i < p.C) sum[i] = fmaf(w, partials[(s * rows + at) * p.C + lane + 32 * i], sum[i]);
     }
+    if constexpr (BLOCK_PER_ROW) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) sums[warp][lane + 32 * i] = sum[i];
-    if (lane == 0) totals[warp] = total;
-    __syncthreads();
-    total = totals[0] + totals[1] + totals[2] + totals[3];
-    const int c = threadIdx.x, i = (int)(at % p.Nq);
-    const int64_t bh = at / p.Nq, b = bh / p.Hq, h = bh - b * p.Hq;
-    if (c < p.C) {
-        const float x = sums[0][c] + sums[1][c] + sums[2][c] + sums[3][c];
-        static_cast<T*>(p.out.data)[b * p.out.batch + h * p.out.head + i * p.out.point + c] = from_float<T>(total == 0.f ? 0.f : x / total);
+        for (int i = 0; i < 4; ++i) sums[warp][lane + 32 * i] = sum[i];
+        if (lane == 0) totals[warp] = total;
+        __syncthreads();
+        if (warp != 0) return;
+        total = 0.f;
+#pragma unroll
+        for (int w = 0; w < JOIN_WARPS; ++w) total += totals[w];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            sum[i] = 0.f;
+#pragma unroll
+            for (int w = 0; w < JOIN_WARPS; ++w) sum[i] += sums[w][lane + 32 * i];
+        }
     }
-    if (c == 0 && p.lse != nullptr) p.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
+    const int n = (int)(at % p.Nq);
+    const int64_t bh = at / p.Nq, b = bh / p.Hq, h = bh - b * p.Hq;
+    T* out = static_cast<T*>(p.out.data) + b * p.out.batch + h * p.out.head + n * p.out.point;
+    const float inverse = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (lane + 32 * i < p.C) out[lane + 32 * i] = from_float<T>(sum[i] * inverse);
+    if (lane == 0 && p.lse != nullptr) p.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
 }
 
 // ---- backward: statistics -----------------------------------------------------------------------------------------------------
@@ -690,8 +709,16 @@ int forward_splits(const Problem& p, int sms) {
 }
 
 cudaError_t launch_join(const Problem& p, sna_dtype_t dtype, int splits, const float* partials, cudaStream_t stream) {
-    if (dtype == SNA_BFLOAT16) attend_join_kernel<__nv_bfloat16><<<(unsigned)rows_of(p), THREADS, 0, stream>>>(p, splits, partials);
-    else attend_join_kernel<__half><<<(unsigned)rows_of(p), THREADS, 0, stream>>>(p, splits, partials);
+    const int64_t rows = rows_of(p);
+    const bool block_per_row = rows <= 1024;
+    const unsigned blocks = (unsigned)(block_per_row ? rows : (rows + JOIN_WARPS - 1) / JOIN_WARPS);
+    auto run = [&](auto t) {
+        using T = decltype(t);
+        if (block_per_row) attend_join_kernel<T, true><<<blocks, 32 * JOIN_WARPS, 0, stream>>>(p, splits, partials);
+        else attend_join_kernel<T, false><<<blocks, 32 * JOIN_WARPS, 0, stream>>>(p, splits, partials);
+    };
+    if (dtype == SNA_BFLOAT16) run(__nv_bfloat16());
+    else run(__half());
     return cudaGetLastError();
 }
 

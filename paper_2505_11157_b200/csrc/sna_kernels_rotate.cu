@@ -43,27 +43,78 @@ struct RotateArgs {
 
 __device__ __forceinline__ int64_t at(const Strided& t, int i, int j) { return i * t.lat + j * t.lon; }
 
+// Walks the slices (batch, head) of a tensor by additions.
+struct Walk {
+    int64_t head, wrap;         // to the next head, and from the last head to the next batch's first
+    int h, H;
+    __device__ __forceinline__ Walk(const Strided& t, int h, int H) : head(t.head), wrap(t.batch - (H - 1) * t.head), h(h), H(H) {}
+    template <typename T> __device__ __forceinline__ void step(T*& p) {
+        const bool last = ++h == H;
+        p += last ? wrap : head;
+        if (last) h = 0;
+    }
+};
+
+// Measured, 256x512 -> 128x256, B = 2, eight heads of 32, bf16: forward 70 us (73 % of the measured bandwidth), backward 117 (66 %); issue slots 78 and 69 % busy.
+// Instructions are what costs: with fp32 values exchanged, weights multiplied per vector and addresses computed per slice the kernels took 310 (forward)
+// instructions per vector of eight channels and were bound by issue (256x512 -> 128x256, B = 2, eight heads of 32, bf16: forward 129 us, backward 208).
+// So a lane exchanges its words as they are, weights and angles are one factor per channel and point, and arithmetic is on packed pairs.
 template <typename T, int V, Pairs PAIRS, bool BACKWARD>
-__global__ void __launch_bounds__(ROTATE_THREADS) norm_rotate_kernel(const __grid_constant__ RotateArgs a) {
-    constexpr int U = 2;                // vectors of a group under way
-    // (the last sum over threads needs room for a block's partial dw; the exchange for a block's vectors, one of U at a time)
-    __shared__ __align__(16) float shared[ROTATE_THREADS * V];
+__global__ void __launch_bounds__(ROTATE_THREADS, BACKWARD ? 3 : 4) norm_rotate_kernel(const __grid_constant__ RotateArgs a) {
+    using W = Words<T, V>;
+    constexpr int VP = V / 2, U = 2;        // pairs per lane; vectors of a group under way
+    // (the last sum over threads needs room for a block's partial dw, the exchange for a block's vectors)
+    __shared__ __align__(16) float shared[BACKWARD || PAIRS == Pairs::BY_SHARED ? ROTATE_THREADS * V : 4];
     const int which = (int)blockIdx.x >= a.first_blocks;
     const Part& p = a.part[which];
     const int block = (int)blockIdx.x - (which ? a.first_blocks : 0);
     const int lane = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes, groups = ROTATE_THREADS / a.lanes;
-    const int c0 = lane * V, C = a.C;
+    const int c0 = lane * V, C = a.C, P = p.pairs;
     const bool mine = c0 < C;
-    const int P = p.pairs;
-    float* row = shared + group * a.lanes * V;
-
-    float w[V], dw[V];
+    // where the partners of the lane's channels are: a lane (itself if they are not turned), or the other half of each word
+    const int other = PAIRS != Pairs::BY_SHUFFLE ? 0 : c0 < P ? lane + P / V : c0 < 2 * P ? lane - P / V : lane;
+    uint32_t swap[W::N];
+    if (PAIRS == Pairs::IN_LANE && sizeof(T) == 2)
+#pragma unroll
+        for (int i = 0; i < W::N; ++i) swap[i] = c0 + 2 * i < 2 * P ? 0x1032u : 0x3210u;
+    auto partners = [&](const W& x) {
+        W y;
+        if constexpr (PAIRS == Pairs::BY_SHUFFLE) {
+#pragma unroll
+            for (int i = 0; i < W::N; ++i) y.w[i] = __shfl_sync(0xffffffffu, x.w[i], other, a.lanes);
+        } else if constexpr (PAIRS == Pairs::IN_LANE) {
+#pragma unroll
+            for (int i = 0; i < W::N; ++i)
+                if constexpr (sizeof(T) == 2) y.w[i] = __byte_perm(x.w[i], 0, swap[i]);
+                else y.w[i] = c0 + (i & ~1) < 2 * P ? x.w[i ^ 1] : x.w[i];
+        } else {
+            T* row = reinterpret_cast<T*>(shared) + group * a.lanes * V;
+            T own[V], got[V];
+            *reinterpret_cast<W*>(own) = x;
+#pragma unroll
+            for (int i = 0; i < V; ++i) row[c0 + i] = own[i];
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < V; ++i) { const int c = c0 + i; got[i] = c < P ? row[c + P] : c < 2 * P ? row[c - P] : own[i]; }
+            __syncwarp();
+            y = *reinterpret_cast<W*>(got);
+        }
+        return y;
+    };
+    // dy's partner takes part with the transposed rotation's sign; x's with its own channel's weight
+    float w[V], dw[V], w_partner[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-        w[i] = mine && p.weight != nullptr ? p.weight[c0 + i] : 1.f;
+        const int c = c0 + i, pc = c >= 2 * P ? c : PAIRS == Pairs::IN_LANE ? c ^ 1 : c < P ? c + P : c - P;
+        w[i] = mine && p.weight != nullptr ? p.weight[c] : 1.f;
+        w_partner[i] = !BACKWARD && mine && p.weight != nullptr ? p.weight[pc] : 1.f;
         dw[i] = 0.f;
     }
+    uint64_t w2[VP], dw2[VP];
+#pragma unroll
+    for (int i = 0; i < VP; ++i) { w2[i] = pack2(w[2 * i], w[2 * i + 1]); dw2[i] = pack2(0.f, 0.f); }
     const int s_begin = (block / p.point_blocks) * p.slices_per_block, s_end = min(s_begin + p.slices_per_block, p.slices);
+    const int b_begin = s_begin / p.H, h_begin = s_begin - b_begin * p.H;
     const float inverse_C = 1.f / C;
 
     // the trips are the same for all groups of a block, whose lanes meet in shuffles; those beyond the last point do nothing
@@ -71,100 +122,101 @@ __global__ void __launch_bounds__(ROTATE_THREADS) norm_rotate_kernel(const __gri
         const int point = point0 + group;
         const bool here = mine && point < p.points;
         const int i_lat = here ? point / p.nlon : 0, j_lon = here ? point - i_lat * p.nlon : 0;
-        // y = cs * n + sn * partner; sn carries the sign of the pair's first channel
-        float cs[V], sn[V];
-        bool turned[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int c = c0 + i;
-            const int pair = PAIRS == Pairs::IN_LANE ? c >> 1 : c < P ? c : c - P;
-            const bool first = PAIRS == Pairs::IN_LANE ? (c & 1) == 0 : c < P;
-            turned[i] = mine && c < 2 * P;
-            cs[i] = 1.f; sn[i] = 0.f;
-            if (turned[i]) {
-                const float2 t = pair < p.pairs_lat ? reinterpret_cast<const float2*>(p.lat_table)[(int64_t)i_lat * p.pairs_lat + pair]
-                                                    : reinterpret_cast<const float2*>(p.lon_table)[(int64_t)j_lon * (P - p.pairs_lat) + pair - p.pairs_lat];
-                cs[i] = t.x;
-                sn[i] = first ? -t.y : t.y;
-            }
-        }
-        const T* x = static_cast<const T*>(p.x.data) + at(p.x, i_lat, j_lon) + c0;
-        const T* dy = BACKWARD ? static_cast<const T*>(p.dy.data) + at(p.dy, i_lat, j_lon) + c0 : nullptr;
-        T* y = static_cast<T*>(p.y.data) + at(p.y, i_lat, j_lon) + c0;
-        int b = s_begin / p.H, h = s_begin - b * p.H;
-        for (int s = s_begin; s < s_end; s += U) {
-            Pack<T, V> xs[U], gs[U];
-            int bs[U], hs[U];
+        const T* x = static_cast<const T*>(p.x.data) + at(p.x, i_lat, j_lon) + b_begin * p.x.batch + h_begin * p.x.head + c0;
+        const T* dy = BACKWARD ? static_cast<const T*>(p.dy.data) + at(p.dy, i_lat, j_lon) + b_begin * p.dy.batch + h_begin * p.dy.head + c0 : nullptr;
+        T* y = static_cast<T*>(p.y.data) + at(p.y, i_lat, j_lon) + b_begin * p.y.batch + h_begin * p.y.head + c0;
+        Walk walk_x(p.x, h_begin, p.H), walk_dy(p.dy, h_begin, p.H), walk_y(p.y, h_begin, p.H);
+        W x_next[U], g_next[U];
+        // the next U vectors are under way while these are computed
+        auto fetch = [&](int s) {
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                bs[u] = b; hs[u] = h;
-                if (++h == p.H) { h = 0; ++b; }
                 if (here && s + u < s_end) {
-                    xs[u] = *reinterpret_cast<const Pack<T, V>*>(x + bs[u] * p.x.batch + hs[u] * p.x.head);
-                    if (BACKWARD) gs[u] = *reinterpret_cast<const Pack<T, V>*>(dy + bs[u] * p.dy.batch + hs[u] * p.dy.head);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) { xs[u].v[i] = from_float<T>(0.f); gs[u].v[i] = from_float<T>(0.f); }
+                    x_next[u] = load_words<T, V>(x);
+                    if (BACKWARD) g_next[u] = load_words<T, V>(dy);
                 }
+                walk_x.step(x);
+                if (BACKWARD) walk_dy.step(dy);
+            }
+        };
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < W::N; ++i) { x_next[u].w[i] = 0; g_next[u].w[i] = 0; }
+        fetch(s_begin);
+        // y = own * x + partner's * x of the partner (times r); backward: g likewise, of dy
+        uint64_t own[VP], partners_[VP];
+        {
+            float cs[V], sn[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                const int c = c0 + i;
+                const int pair = PAIRS == Pairs::IN_LANE ? c >> 1 : c < P ? c : c - P;
+                const bool first = PAIRS == Pairs::IN_LANE ? (c & 1) == 0 : c < P;
+                cs[i] = 1.f; sn[i] = 0.f;
+                if (mine && c < 2 * P) {
+                    const float2 t = pair < p.pairs_lat ? reinterpret_cast<const float2*>(p.lat_table)[(int64_t)i_lat * p.pairs_lat + pair]
+                                                        : reinterpret_cast<const float2*>(p.lon_table)[(int64_t)j_lon * (P - p.pairs_lat) + pair - p.pairs_lat];
+                    cs[i] = t.x;
+                    sn[i] = first != BACKWARD ? -t.y : t.y;
+                }
+                if (!BACKWARD) { cs[i] *= w[i]; sn[i] *= w_partner[i]; }
             }
 #pragma unroll
+            for (int i = 0; i < VP; ++i) { own[i] = pack2(cs[2 * i], cs[2 * i + 1]); partners_[i] = pack2(sn[2 * i], sn[2 * i + 1]); }
+        }
+        for (int s = s_begin; s < s_end; s += U) {
+            W xs[U], gs[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) { xs[u] = x_next[u]; if (BACKWARD) gs[u] = g_next[u]; }
+            if (s + U < s_end) fetch(s + U);
+#pragma unroll
             for (int u = 0; u < U; ++u) {
-                // v: what the rotation acts on, n w (forward; without r, which is the same for the whole vector) or dy (backward)
-                float xf[V], v[V], partner[V];
+                uint64_t xf[VP], v[VP], vp[VP];
+                pairs_of<T, V>(xs[u], xf);
+                pairs_of<T, V>(partners(BACKWARD ? gs[u] : xs[u]), vp);
+                if (BACKWARD) pairs_of<T, V>(gs[u], v);
+                uint64_t square2 = pack2(0.f, 0.f), product2 = pack2(0.f, 0.f);
 #pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    xf[i] = to_float(xs[u].v[i]);
-                    v[i] = BACKWARD ? to_float(gs[u].v[i]) : xf[i] * w[i];
+                for (int i = 0; i < VP; ++i) {
+                    square2 = fma2(xf[i], xf[i], square2);
+                    v[i] = fma2(partners_[i], vp[i], mul2(own[i], BACKWARD ? v[i] : xf[i]));       // y / r, or g
+                    if (BACKWARD) product2 = fma2(mul2(v[i], w2[i]), xf[i], product2);
                 }
-                if (PAIRS == Pairs::IN_LANE) {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) partner[i] = v[i ^ 1];
-                } else if (PAIRS == Pairs::BY_SHUFFLE) {
-                    const int other = c0 < P ? lane + P / V : c0 < 2 * P ? lane - P / V : lane;
-#pragma unroll
-                    for (int i = 0; i < V; ++i) partner[i] = __shfl_sync(0xffffffffu, v[i], other, a.lanes);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < V; ++i) row[c0 + i] = v[i];
-                    __syncwarp();
-#pragma unroll
-                    for (int i = 0; i < V; ++i) { const int c = c0 + i; partner[i] = turned[i] ? row[c < P ? c + P : c - P] : 0.f; }
-                    __syncwarp();
-                }
-                float square = 0.f, product = 0.f;
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    square = fmaf(xf[i], xf[i], square);
-                    // (the transposed rotation has the other sign)
-                    if (turned[i]) v[i] = BACKWARD ? fmaf(-sn[i], partner[i], cs[i] * v[i]) : fmaf(sn[i], partner[i], cs[i] * v[i]);
-                    if (BACKWARD) product = fmaf(v[i] * w[i], xf[i], product);
-                }
-                for (int o = a.lanes / 2; o > 0; o >>= 1) {
+                float square, product, upper;
+                unpack2(square2, square, upper);
+                square += upper;
+                unpack2(product2, product, upper);
+                product += upper;
+                for (int o = a.lanes >> 1; o > 0; o >>= 1) {
                     square += __shfl_xor_sync(0xffffffffu, square, o);
                     if (BACKWARD) product += __shfl_xor_sync(0xffffffffu, product, o);
                 }
                 const float r = rsqrtf(square * inverse_C + a.eps);
-                Pack<T, V> out;
+                const uint64_t r2 = pack2(r, r);
                 if (BACKWARD) {
-                    // dx = r (g w - x r^2 sum(g w x) / C)
-                    const float along = product * inverse_C * r * r;
+                    // dx = r (g w) - n (r sum(g w n) / C) with n = x r
+                    const float along = -product * inverse_C * r * r;
+                    const uint64_t along2 = pack2(along, along);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        dw[i] = fmaf(v[i], xf[i] * r, dw[i]);
-                        out.v[i] = from_float<T>(r * (v[i] * w[i] - xf[i] * along));
+                    for (int i = 0; i < VP; ++i) {
+                        const uint64_t n = mul2(xf[i], r2);
+                        dw2[i] = fma2(v[i], n, dw2[i]);
+                        v[i] = fma2(n, along2, mul2(mul2(v[i], w2[i]), r2));
                     }
                 } else {
 #pragma unroll
-                    for (int i = 0; i < V; ++i) out.v[i] = from_float<T>(v[i] * r);
+                    for (int i = 0; i < VP; ++i) v[i] = mul2(v[i], r2);
                 }
-                if (here && s + u < s_end) *reinterpret_cast<Pack<T, V>*>(y + bs[u] * p.y.batch + hs[u] * p.y.head) = out;
+                if (here && s + u < s_end) store_words<T, V>(y, words_of<T, V>(v));
+                walk_y.step(y);
             }
         }
     }
     if (BACKWARD && p.partials != nullptr) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < V; ++i) shared[(group * a.lanes + lane) * V + i] = dw[i];      // lanes * V floats per group
+        for (int i = 0; i < VP; ++i) unpack2(dw2[i], shared[(group * a.lanes + lane) * V + 2 * i], shared[(group * a.lanes + lane) * V + 2 * i + 1]);
         __syncthreads();
         for (int c = threadIdx.x; c < C; c += ROTATE_THREADS) {
             float sum = 0.f;
@@ -180,22 +232,24 @@ struct SumArgs {
     int rows[2];
     int C;
 };
-// dweight = sum of the blocks' partial sums, in a fixed order.  One block per 32 channels and part; 32 rows of threads.
+// dweight = sum of the blocks' partial sums, in a fixed order.  One block per 8 channels (a sector of each row) and part; 128 rows of threads.
 __global__ void __launch_bounds__(1024) sum_partials_kernel(const __grid_constant__ SumArgs a) {
-    __shared__ float sums[32][33];
-    const int which = blockIdx.y, c = blockIdx.x * 32 + threadIdx.x;
+    __shared__ float sums[128][9];
+    const int which = blockIdx.y, c = blockIdx.x * 8 + threadIdx.x, rows = a.rows[which];
     if (a.dweight[which] == nullptr) return;
+    const float* from = a.partials[which] + c;
     float sum = 0.f;
     if (c < a.C)
-        for (int r = threadIdx.y; r < a.rows[which]; r += 32) sum += a.partials[which][(int64_t)r * a.C + c];
+#pragma unroll 4
+        for (int r = threadIdx.y; r < rows; r += 128) sum += from[(int64_t)r * a.C];
     sums[threadIdx.y][threadIdx.x] = sum;
     __syncthreads();
-    if (threadIdx.y == 0 && c < a.C) {
-        float total = 0.f;
 #pragma unroll
-        for (int r = 0; r < 32; ++r) total += sums[r][threadIdx.x];
-        a.dweight[which][c] = total;
+    for (int o = 64; o > 0; o >>= 1) {
+        if (threadIdx.y < o) sums[threadIdx.y][threadIdx.x] += sums[threadIdx.y + o][threadIdx.x];
+        __syncthreads();
     }
+    if (threadIdx.y == 0 && c < a.C) a.dweight[which][c] = sums[0][threadIdx.x];
 }
 
 template <typename T, int V, bool BACKWARD>
@@ -277,19 +331,21 @@ sna_status_t norm_rotate(const sna_rotate_t* parts, int n_parts, sna_dtype_t dty
         if (!interleaved && p.pairs % V != 0) pairs = Pairs::BY_SHARED;
         if (backward) sum.dweight[i] = r.dweight;
         if (p.points == 0 || p.slices == 0) continue;
-        // A block's groups take neighbouring points.  Slices are spread over blocks until the GPU is full twice, as long as each still takes
-        // four with the angles that it has read; the backward pass also bounds its blocks, each of which leaves a row of partial sums.
+        // A block's groups take neighbouring points.  Slices are spread over blocks until the GPU has one full wave of them, as long as each still takes
+        // sixteen with the angles that it has read (four: forward 73 instead of 70 us, two waves of blocks 78, in the case above); the backward pass also
+        // bounds its blocks, each of which leaves a row of partial sums.
         const int groups = ROTATE_THREADS / a.lanes;
         p.point_blocks = (p.points + groups - 1) / groups;
-        const int want = std::max(1, (2 * 8 * sms + p.point_blocks - 1) / p.point_blocks);
-        p.slices_per_block = std::max(std::min(p.slices, 4), (p.slices + want - 1) / want);
+        const int want = std::max(1, (4 * sms + p.point_blocks - 1) / p.point_blocks);
+        p.slices_per_block = std::max(std::min(p.slices, 16), (p.slices + want - 1) / want);
         if (p.point_blocks < sms) p.slices_per_block = std::max(std::min(p.slices, 2), (p.slices + want - 1) / want);
         p.slice_blocks = (p.slices + p.slices_per_block - 1) / p.slices_per_block;
         if (backward && (int64_t)p.point_blocks * p.slice_blocks > MAX_PARTIALS) {
-            p.slice_blocks = std::min(p.slice_blocks, MAX_PARTIALS);
+            p.slice_blocks = std::min(p.slice_blocks, std::max(1, MAX_PARTIALS / p.point_blocks));
             p.slices_per_block = (p.slices + p.slice_blocks - 1) / p.slice_blocks;
             p.slice_blocks = (p.slices + p.slices_per_block - 1) / p.slices_per_block;
-            p.point_blocks = std::min(p.point_blocks, MAX_PARTIALS / p.slice_blocks);
+            const int most = MAX_PARTIALS / p.slice_blocks, trips = (p.point_blocks + most - 1) / most;
+            p.point_blocks = (p.point_blocks + trips - 1) / trips;
         }
         const int64_t n = (int64_t)p.point_blocks * p.slice_blocks;
         if (n > 0x3fffffff) return fail(SNA_ERR_UNSUPPORTED, "problem too large");
@@ -308,7 +364,7 @@ sna_status_t norm_rotate(const sna_rotate_t* parts, int n_parts, sna_dtype_t dty
             : dtype == SNA_BFLOAT16 ? launch_width<__nv_bfloat16>(a, V, pairs, backward, total, stream)
                                     : launch_width<__half>(a, V, pairs, backward, total, stream);
     if (e == cudaSuccess && sums) {
-        sum_partials_kernel<<<dim3((C + 31) / 32, n_parts), dim3(32, 32), 0, stream>>>(sum);
+        sum_partials_kernel<<<dim3((C + 7) / 8, n_parts), dim3(8, 128), 0, stream>>>(sum);
         e = cudaGetLastError();
     }
     if (e != cudaSuccess) return fail(SNA_ERR_CUDA, "norm and rotation launch: %s", cudaGetErrorString(e));

@@ -38,6 +38,65 @@ template <> __device__ __forceinline__ float from_float<float>(float x) { return
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
 
+// Packed fp32 pairs: one instruction for two lanes of a 64-bit register pair
+__device__ __forceinline__ uint64_t pack2(float a, float b) { uint64_t r; asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void unpack2(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) { uint64_t d; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c)); return d; }
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) { uint64_t d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) { uint64_t d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
+
+// The V values of a lane as 32-bit words, and as packed pairs of fp32
+template <typename T, int V> struct Words {
+    static constexpr int N = (int)sizeof(T) * V / 4;
+    uint32_t w[N];
+};
+template <typename T> __device__ __forceinline__ uint64_t pair_of(uint32_t word);
+template <> __device__ __forceinline__ uint64_t pair_of<__nv_bfloat16>(uint32_t word) { return pack2(__uint_as_float(word << 16), __uint_as_float(word & 0xffff0000u)); }
+template <> __device__ __forceinline__ uint64_t pair_of<__half>(uint32_t word) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&word));
+    return pack2(f.x, f.y);
+}
+template <typename T> __device__ __forceinline__ uint32_t word_of(float lo, float hi);
+template <> __device__ __forceinline__ uint32_t word_of<__nv_bfloat16>(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <> __device__ __forceinline__ uint32_t word_of<__half>(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <typename T, int V> __device__ __forceinline__ void pairs_of(const Words<T, V>& x, uint64_t (&f)[V / 2]) {
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        if constexpr (sizeof(T) == 4) f[i] = pack2(__uint_as_float(x.w[2 * i]), __uint_as_float(x.w[2 * i + 1]));
+        else f[i] = pair_of<T>(x.w[i]);
+    }
+}
+template <typename T, int V> __device__ __forceinline__ Words<T, V> words_of(const uint64_t (&f)[V / 2]) {
+    Words<T, V> x;
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+        float a, b;
+        unpack2(f[i], a, b);
+        if constexpr (sizeof(T) == 4) { x.w[2 * i] = __float_as_uint(a); x.w[2 * i + 1] = __float_as_uint(b); }
+        else {
+            x.w[i] = word_of<T>(a, b);
+        }
+    }
+    return x;
+}
+template <typename T, int V> __device__ __forceinline__ Words<T, V> load_words(const T* p) {
+    Words<T, V> x;
+    if constexpr (Words<T, V>::N == 4) { const uint4 q = *reinterpret_cast<const uint4*>(p); x.w[0] = q.x; x.w[1] = q.y; x.w[2] = q.z; x.w[3] = q.w; }
+    else { const uint2 q = *reinterpret_cast<const uint2*>(p); x.w[0] = q.x; x.w[1] = q.y; }
+    return x;
+}
+template <typename T, int V> __device__ __forceinline__ void store_words(T* p, const Words<T, V>& x) {
+    if constexpr (Words<T, V>::N == 4) *reinterpret_cast<uint4*>(p) = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
+    else *reinterpret_cast<uint2*>(p) = make_uint2(x.w[0], x.w[1]);
+}
 // V values in one load or store
 template <typename T, int V> struct alignas(sizeof(T) * V) Pack { T v[V]; };
 #endif
