@@ -55,15 +55,36 @@ sna_status_t check_workspace(const void* workspace, size_t bytes, size_t need) {
 // The tcgen05 kernels take tiles of 128 (forward: two of them) rows and blocks of 128 points.  They find a row's maximum before the scores are scaled, and
 // hold weights divided by the scale: it has to be positive, and not so small that a point left out could be taken for one with a low weight.
 bool on_tensor_memory(const Problem& p) { return p.Nq > 64 && p.Nk >= 128 && p.scale >= 0x1p-20f && p.scale <= 0x1p20f; }
-int splits_of(const Problem& p, int sms) {
-    if (!on_tensor_memory(p)) return forward_splits(p, sms);
-    const int64_t tiles = (int64_t)p.B * p.Hq * ((p.Nq + 255) / 256), blocks = (p.Nk + 127) / 128;
-    return tiles >= sms ? 1 : (int)std::max<int64_t>(1, std::min(blocks / 2, sms / tiles));
+// What the forward pass needs to hold partial results, on either path (the tcgen05 kernels fall back where the driver refuses a tensor).
+size_t forward_bytes(const Problem& p, int sms) {
+    const int splits = forward_splits(p, sms);
+    const size_t simple = splits > 1 ? (size_t)splits * rows_of(p) * (1 + p.C) : 0;
+    return align256(sizeof(float) * (on_tensor_memory(p) ? std::max(simple, partial_floats(p, Kernel::FORWARD, sms)) : simple));
 }
 
-size_t forward_bytes(const Problem& p, int splits) { return splits > 1 ? align256((size_t)splits * rows_of(p) * (1 + p.C) * sizeof(float)) : 0; }
-size_t extra_bytes(const Problem& p) { return (size_t)query_blocks_of(p) * 2 * STATS_BLOCK * sizeof(uint4); }
-size_t backward_bytes(const Problem& p) { return 2 * align256((size_t)rows_of(p) * sizeof(float)) + align256((size_t)p.B * p.Hk * 2 * sizeof(uint32_t)) + extra_bytes(p); }
+struct BackwardWorkspace {
+    Stats stats;
+    float* partials;
+    size_t bytes;
+};
+BackwardWorkspace backward_workspace(const Problem& p, void* workspace, int sms) {
+    BackwardWorkspace w{};
+    char* at = static_cast<char*>(workspace);
+    auto take = [&](size_t bytes) {
+        char* here = at == nullptr ? nullptr : at + w.bytes;
+        w.bytes += align256(bytes);
+        return here;
+    };
+    w.stats.extra = reinterpret_cast<uint4*>(take((size_t)query_blocks_of(p) * 2 * STATS_BLOCK * sizeof(uint4)));
+    w.stats.weights = reinterpret_cast<uint4*>(take((size_t)weight_blocks_of(p) * STATS_BLOCK * sizeof(uint4)));
+    w.stats.gone = reinterpret_cast<uint2*>(take((size_t)weight_blocks_of(p) * sizeof(uint2)));
+    w.stats.lse2 = reinterpret_cast<float*>(take((size_t)rows_of(p) * sizeof(float)));
+    w.stats.D = reinterpret_cast<float*>(take((size_t)rows_of(p) * sizeof(float)));
+    w.stats.norms = reinterpret_cast<uint32_t*>(take((size_t)p.B * p.Hk * 2 * sizeof(uint32_t)));
+    // (one after the other on the stream: dq's are joined before dk's and dv's are written)
+    w.partials = reinterpret_cast<float*>(take(on_tensor_memory(p) ? sizeof(float) * std::max(partial_floats(p, Kernel::DQ, sms), partial_floats(p, Kernel::DKDV, sms)) : 0));
+    return w;
+}
 
 }  // namespace
 }  // namespace attend
@@ -76,7 +97,8 @@ extern "C" {
 size_t sna_attention_forward_workspace_bytes(const sna_attention_t* a, sna_dtype_t dtype) {
     Problem p;
     if (describe(a, dtype, false, p) != SNA_OK) return 0;
-    return forward_bytes(p, splits_of(p, sna::sms_of_current_device()));
+    const int sms = sna::sms_of_current_device();
+    return sms == 0 ? 0 : forward_bytes(p, sms);
 }
 
 sna_status_t sna_attention_forward(const sna_attention_t* a, sna_dtype_t dtype, void* workspace, size_t workspace_bytes, void* cuda_stream) {
@@ -86,14 +108,16 @@ sna_status_t sna_attention_forward(const sna_attention_t* a, sna_dtype_t dtype, 
     if (rows_of(p) == 0) return SNA_OK;
     const int sms = sna::sms_of_current_device();
     if (sms == 0) return sna::fail(SNA_ERR_CUDA, "no CUDA device");
-    const int splits = splits_of(p, sms);
-    st = check_workspace(workspace, workspace_bytes, forward_bytes(p, splits));
+    st = check_workspace(workspace, workspace_bytes, forward_bytes(p, sms));
     if (st != SNA_OK) return st;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     float* partials = static_cast<float*>(workspace);
     cudaError_t e = cudaSuccess;
-    if (!on_tensor_memory(p) || !forward_tc(p, dtype, splits, partials, stream, e)) e = launch_forward(p, dtype, splits, partials, stream);
-    if (e == cudaSuccess && splits > 1) e = launch_join(p, dtype, splits, partials, stream);
+    if (!on_tensor_memory(p) || !forward_tc(p, dtype, sms, partials, stream, e)) {
+        const int splits = forward_splits(p, sms);
+        e = launch_forward(p, dtype, splits, partials, stream);
+        if (e == cudaSuccess && splits > 1) e = launch_join(p, dtype, splits, partials, stream);
+    }
     if (e != cudaSuccess) return sna::fail(SNA_ERR_CUDA, "attention launch: %s", cudaGetErrorString(e));
     return SNA_OK;
 }
@@ -101,7 +125,8 @@ sna_status_t sna_attention_forward(const sna_attention_t* a, sna_dtype_t dtype, 
 size_t sna_attention_backward_workspace_bytes(const sna_attention_t* a, sna_dtype_t dtype) {
     Problem p;
     if (describe(a, dtype, true, p) != SNA_OK) return 0;
-    return backward_bytes(p);
+    const int sms = sna::sms_of_current_device();
+    return sms == 0 ? 0 : backward_workspace(p, nullptr, sms).bytes;
 }
 
 sna_status_t sna_attention_backward(const sna_attention_t* a, sna_dtype_t dtype, void* workspace, size_t workspace_bytes, void* cuda_stream) {
@@ -110,23 +135,17 @@ sna_status_t sna_attention_backward(const sna_attention_t* a, sna_dtype_t dtype,
     if (st != SNA_OK) return st;
     const bool queries = rows_of(p) > 0, keys = (int64_t)p.B * p.Hk * p.Nk > 0;
     if (!queries && !keys) return SNA_OK;
-    if (sna::sms_of_current_device() == 0) return sna::fail(SNA_ERR_CUDA, "no CUDA device");
-    st = check_workspace(workspace, workspace_bytes, backward_bytes(p));
+    const int sms = sna::sms_of_current_device();
+    if (sms == 0) return sna::fail(SNA_ERR_CUDA, "no CUDA device");
+    const BackwardWorkspace w = backward_workspace(p, workspace, sms);
+    st = check_workspace(workspace, workspace_bytes, w.bytes);
     if (st != SNA_OK) return st;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    Stats s;
-    char* at = static_cast<char*>(workspace);
-    s.extra = reinterpret_cast<uint4*>(at);
-    at += extra_bytes(p);
-    s.lse2 = reinterpret_cast<float*>(at);
-    at += align256((size_t)rows_of(p) * sizeof(float));
-    s.D = reinterpret_cast<float*>(at);
-    at += align256((size_t)rows_of(p) * sizeof(float));
-    s.norms = reinterpret_cast<uint32_t*>(at);
+    const Stats& s = w.stats;
     cudaError_t e = launch_statistics(p, s, dtype, stream);
     const bool on_tc = on_tensor_memory(p);
-    if (e == cudaSuccess && queries && (!on_tc || !backward_dq_tc(p, s, dtype, stream, e))) e = launch_backward_dq(p, s, dtype, stream);
-    if (e == cudaSuccess && keys && (!on_tc || !backward_dkdv_tc(p, s, dtype, stream, e))) e = launch_backward_dkdv(p, s, dtype, stream);
+    if (e == cudaSuccess && queries && (!on_tc || !backward_dq_tc(p, s, dtype, sms, w.partials, stream, e))) e = launch_backward_dq(p, s, dtype, stream);
+    if (e == cudaSuccess && keys && (!on_tc || !backward_dkdv_tc(p, s, dtype, sms, w.partials, stream, e))) e = launch_backward_dkdv(p, s, dtype, stream);
     if (e != cudaSuccess) return sna::fail(SNA_ERR_CUDA, "attention backward launch: %s", cudaGetErrorString(e));
     return SNA_OK;
 }

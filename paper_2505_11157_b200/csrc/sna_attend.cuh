@@ -31,8 +31,25 @@ struct Stats {
     float* D;                       // [B][Hq][Nq]
     uint32_t* norms;                // [B][Hk][2]: of dout's rows, of v's rows (float16 only)
     uint4* extra;                   // [B][Hq][blocks of 64 queries][2][64]: what the tcgen05 dk/dv kernel adds to S and T per query (see there)
+    uint4* weights;                 // [B or 1][blocks of 64 points][64]: what the tcgen05 dq kernel adds to S per point, if there are weights
+    uint2* gone;                    // [B or 1][blocks of 64 points]: bits of the points left out
 };
 constexpr int STATS_BLOCK = 64;
+__host__ __device__ inline int64_t weight_blocks_of(const Problem& p) {
+    return p.log_weights == nullptr ? 0 : (int64_t)(p.log_weights_batch == 0 ? 1 : p.B) * ((p.Nk + STATS_BLOCK - 1) / STATS_BLOCK);
+}
+
+// How a tcgen05 kernel's tiles become thread blocks, of which an SM runs one at a time: the first `full` tiles whole, the others in `parts` pieces of the
+// streamed side, whose partial results (fp32) a second kernel joins.
+struct Split {
+    int64_t tiles, full;
+    int parts;
+    __host__ __device__ int64_t blocks() const { return full + (tiles - full) * parts; }
+    __host__ __device__ int64_t rest() const { return tiles - full; }
+};
+// The whole waves stay whole.  The last, partial wave is cut so that its pieces end early: R tiles in k pieces take ceil(R k / SMs) / k of a wave (256 tiles on 148
+// SMs: 1.75 waves with four pieces each instead of 2).  Not for many waves, which gain little, nor into pieces of fewer than `least` streamed blocks.
+Split split_tiles(int64_t tiles, int64_t streamed, int64_t least, int sms);
 __host__ __device__ inline int64_t query_blocks_of(const Problem& p) { return (int64_t)p.B * p.Hq * ((p.Nq + STATS_BLOCK - 1) / STATS_BLOCK); }
 
 // Powers of two that keep float16 operands of the second products away from the numbers that its exponent has no room for: softmax
@@ -66,9 +83,13 @@ inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 __host__ __device__ inline int64_t rows_of(const Problem& p) { return (int64_t)p.B * p.Hq * p.Nq; }
 
 // tcgen05 kernels (sna_kernels_attend_tc.cu).  False: the driver refuses a map of one of the tensors (heads that share memory, say).
-bool forward_tc(const Problem& p, sna_dtype_t dtype, int splits, float* partials, cudaStream_t stream, cudaError_t& e);
-bool backward_dq_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream, cudaError_t& e);
-bool backward_dkdv_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream, cudaError_t& e);
+// partials: room for partial_floats of the kernel.
+enum class Kernel { FORWARD, DQ, DKDV };
+Split split_of(const Problem& p, Kernel kernel, int sms);
+size_t partial_floats(const Problem& p, Kernel kernel, int sms);
+bool forward_tc(const Problem& p, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
+bool backward_dq_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
+bool backward_dkdv_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
 cudaError_t read_status(int* status);
 
 // mma.sync kernels (sna_kernels_attend.cu)

@@ -132,11 +132,16 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
     const int blocks = (p.Nk + BN - 1) / BN;
     const int first = (int)((int64_t)blocks * split / splits), last = (int)((int64_t)blocks * (split + 1) / splits);
 
-    auto load_bias = [&](int j) {
+    // a weight is read one step before it is stored, so that no step waits for it
+    float weight = -INFINITY;
+    auto fetch_bias = [&](int j) {
         if (tid < BN) {
             const int n = j * BN + tid;
-            bias[j & 3][tid] = j < last && n < p.Nk ? weight2(weights, n) : -INFINITY;
+            weight = j < last && n < p.Nk ? weight2(weights, n) : -INFINITY;
         }
+    };
+    auto store_bias = [&](int j) {
+        if (tid < BN) bias[j & 3][tid] = weight;
     };
     auto load_block = [&](int j) {
         if (j < last) {
@@ -149,7 +154,8 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
     };
     load_stacked<CP>(tq, static_cast<const T*>(p.q.data) + b * p.q.batch + (int64_t)hk * p.G * p.q.head, p.q.head, p.q.point, row0, rows, p.Nq, BM, p.C);
 #pragma unroll
-    for (int i = 0; i < STAGES; ++i) load_bias(first + i);
+    for (int i = 0; i < STAGES; ++i) { fetch_bias(first + i); store_bias(first + i); }
+    fetch_bias(first + STAGES);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) load_block(first + i);
@@ -161,7 +167,8 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
         for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
 
     for (int j = first; j < last; ++j) {
-        load_bias(j + STAGES);
+        store_bias(j + STAGES);
+        fetch_bias(j + STAGES + 1);
         load_block(j + STAGES - 1);
         wait_group<STAGES - 1>();
         __syncthreads();
@@ -357,16 +364,30 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) attend_join_kernel(const __gr
 // ---- backward: statistics -----------------------------------------------------------------------------------------------------
 
 // Per query: D = dout . out, log2 of the sum of weights, and both as the extra rows that the tcgen05 dk/dv kernel copies.  float16: also the largest norm
-// of a row of dout and of v per key head, which bound |t - D| <= 2 |dout| |v| (the blocks behind the queries' take v's rows); a maximum does not depend on the
+// of a row of dout and of v per key head, which bound |t - D| <= 2 |dout| |v| (the last blocks take v's rows); a maximum does not depend on the
 // order of its atomics, of which there is one per block (one per row took ten times as long as the rest).  A block takes 64 points of one head,
-// four lanes each.
+// four lanes each.  The first blocks prepare the points' weights for the tcgen05 dq kernel.
 template <typename T>
-__global__ void __launch_bounds__(256) attend_statistics_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats s, int64_t query_blocks) {
+__global__ void __launch_bounds__(256) attend_statistics_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats s, int64_t query_blocks, int64_t weight_blocks) {
     constexpr bool SCALED = SHIFT<T> != 0.f;
     __shared__ uint32_t most;
     const int part = threadIdx.x & 3, place = threadIdx.x >> 2;
-    const bool queries = blockIdx.x < query_blocks;
-    const int64_t block = (int64_t)blockIdx.x - (queries ? 0 : query_blocks);
+    if (blockIdx.x < weight_blocks) {
+        // one thread per point: its weight in parts, and who is left out
+        const int per_row = (p.Nk + STATS_BLOCK - 1) / STATS_BLOCK, row = blockIdx.x / per_row, first = (blockIdx.x - row * per_row) * STATS_BLOCK;
+        if (threadIdx.x >= STATS_BLOCK) return;
+        const int n = first + threadIdx.x;
+        const float weight = n < p.Nk ? p.log_weights[row * p.log_weights_batch + n] : -INFINITY;
+        const bool out = weight <= EXCLUDED;
+        const uint2 parts = out ? make_uint2(EXTRA_OUT, 0) : extra_parts(weight / p.scale);
+        s.weights[(int64_t)blockIdx.x * STATS_BLOCK + threadIdx.x] = make_uint4(parts.x, parts.y, 0, 0);
+        const uint32_t gone = __ballot_sync(0xffffffffu, out && n < p.Nk);
+        if ((threadIdx.x & 31) == 0) reinterpret_cast<uint32_t*>(s.gone)[(int64_t)blockIdx.x * 2 + (threadIdx.x >> 5)] = gone;
+        return;
+    }
+    const int64_t index = (int64_t)blockIdx.x - weight_blocks;
+    const bool queries = index < query_blocks;
+    const int64_t block = index - (queries ? 0 : query_blocks);
     const int N = queries ? p.Nq : p.Nk, H = queries ? p.Hq : p.Hk, per_head = (N + STATS_BLOCK - 1) / STATS_BLOCK;
     const int64_t bh = block / per_head, b = bh / H, h = bh - b * H;
     const int n = (int)(block - bh * per_head) * STATS_BLOCK + place;
@@ -435,11 +456,16 @@ __global__ void __launch_bounds__(THREADS) attend_dq_kernel(const __grid_constan
     const T* vh = static_cast<const T*>(p.v.data) + b * p.v.batch + hk * p.v.head;
     const float* weights = p.log_weights == nullptr ? nullptr : p.log_weights + b * p.log_weights_batch;
     const int last = (p.Nk + BN - 1) / BN;
-    auto load_bias = [&](int j) {
+    // a weight is read one step before it is stored, so that no step waits for it
+    float weight = -INFINITY;
+    auto fetch_bias = [&](int j) {
         if (tid < BN) {
             const int n = j * BN + tid;
-            bias[j & 3][tid] = j < last && n < p.Nk ? weight2(weights, n) : -INFINITY;
+            weight = j < last && n < p.Nk ? weight2(weights, n) : -INFINITY;
         }
+    };
+    auto store_bias = [&](int j) {
+        if (tid < BN) bias[j & 3][tid] = weight;
     };
     auto load_block = [&](int j) {
         if (j < last) {
@@ -452,8 +478,11 @@ __global__ void __launch_bounds__(THREADS) attend_dq_kernel(const __grid_constan
     };
     load_stacked<CP>(tq, static_cast<const T*>(p.q.data) + b * p.q.batch + (int64_t)hk * p.G * p.q.head, p.q.head, p.q.point, row0, rows, p.Nq, BM, p.C);
     load_stacked<CP>(ty, static_cast<const T*>(p.dout.data) + b * p.dout.batch + (int64_t)hk * p.G * p.dout.head, p.dout.head, p.dout.point, row0, rows, p.Nq, BM, p.C);
-    load_bias(0);
-    load_bias(1);
+    fetch_bias(0);
+    store_bias(0);
+    fetch_bias(1);
+    store_bias(1);
+    fetch_bias(2);
     __syncthreads();
     load_block(0);
 
@@ -473,7 +502,8 @@ __global__ void __launch_bounds__(THREADS) attend_dq_kernel(const __grid_constan
         for (int i = 0; i < 4; ++i) dq[n][i] = 0.f;
 
     for (int j = 0; j < last; ++j) {
-        load_bias(j + 2);
+        store_bias(j + 2);
+        fetch_bias(j + 3);
         load_block(j + 1);
         wait_group<1>();
         __syncthreads();
@@ -732,13 +762,14 @@ cudaError_t launch_forward(const Problem& p, sna_dtype_t dtype, int splits, floa
 
 cudaError_t launch_statistics(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream) {
     const int64_t query_blocks = query_blocks_of(p), key_blocks = (int64_t)p.B * p.Hk * ((p.Nk + STATS_BLOCK - 1) / STATS_BLOCK);
+    const int64_t weight_blocks = weight_blocks_of(p), blocks = weight_blocks + query_blocks + (dtype == SNA_FLOAT16 ? key_blocks : 0);
+    if (blocks == 0) return cudaSuccess;
     if (dtype == SNA_BFLOAT16) {
-        if (query_blocks == 0) return cudaSuccess;
-        attend_statistics_kernel<__nv_bfloat16><<<(unsigned)query_blocks, 256, 0, stream>>>(p, s, query_blocks);
+        attend_statistics_kernel<__nv_bfloat16><<<(unsigned)blocks, 256, 0, stream>>>(p, s, query_blocks, weight_blocks);
     } else {
         const cudaError_t e = cudaMemsetAsync(s.norms, 0, (size_t)p.B * p.Hk * 2 * sizeof(uint32_t), stream);
         if (e != cudaSuccess) return e;
-        attend_statistics_kernel<__half><<<(unsigned)(query_blocks + key_blocks), 256, 0, stream>>>(p, s, query_blocks);
+        attend_statistics_kernel<__half><<<(unsigned)blocks, 256, 0, stream>>>(p, s, query_blocks, weight_blocks);
     }
     return cudaGetLastError();
 }

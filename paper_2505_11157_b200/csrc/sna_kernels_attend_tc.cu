@@ -6,6 +6,7 @@
 // Every accumulator has one issuing thread and all sums are taken in a fixed order: results are reproducible bit for bit.  Every wait is
 // bounded; one that runs out sets the device's status word (sna_layer_check), and the block leaves after another bounded wait for the copies
 // and MMAs that it has under way.
+#include <algorithm>
 #include <type_traits>
 
 #include "sna_attend_tc.cuh"
@@ -15,6 +16,21 @@ namespace attend {
 namespace {
 
 __device__ int g_status;        // non-zero: a bounded wait has run out since the last check
+
+// A thread block's tile and its piece of the streamed side.
+struct Piece {
+    int tile, bh, part, parts;
+    int64_t local;          // of a tile in pieces: its number among them
+    __device__ __forceinline__ Piece(const Split& cut, int tiles) {
+        const int64_t over = (int64_t)blockIdx.x - cut.full;
+        parts = over < 0 ? 1 : cut.parts;
+        local = over < 0 ? 0 : over / parts;
+        part = over < 0 ? 0 : (int)(over - local * parts);
+        const int64_t index = over < 0 ? (int64_t)blockIdx.x : cut.full + local;
+        bh = (int)(index / tiles);
+        tile = (int)(index - (int64_t)bh * tiles);
+    }
+};
 
 constexpr int TILE = 128;       // rows of a tile, points of a block
 constexpr int SLAB = TILE * 128;        // bytes of 128 points x 64 channels
@@ -65,7 +81,7 @@ constexpr float NOTHING = -1e31f;       // scores below belong to points left ou
 template <typename T, int D, bool WEIGHTS>
 __global__ void __launch_bounds__(FWD_THREADS, 1)
 attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                         const __grid_constant__ CUtensorMap map_v, int tiles, int splits, float* partials) {
+                         const __grid_constant__ CUtensorMap map_v, int tiles, const __grid_constant__ Split cut, float* partials) {
     using F = Forward<D>;
     extern __shared__ unsigned char raw[];
     unsigned char* base = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
@@ -73,11 +89,12 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
     __shared__ uint32_t tmem_s;
     __shared__ int fail_s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int split = blockIdx.x % splits, rest = blockIdx.x / splits, tile = rest % tiles, bh = rest / tiles;
+    const Piece piece(cut, tiles);
+    const int part = piece.part, parts = piece.parts, tile = piece.tile, bh = piece.bh;
     const int b = bh / p.Hq, h = bh - b * p.Hq, hk = h / p.G;
     const int row0 = tile * 2 * TILE, halves = row0 + TILE < p.Nq ? 2 : 1;
     const int blocks = (p.Nk + TILE - 1) / TILE;
-    const int first = (int)((int64_t)blocks * split / splits), count = (int)((int64_t)blocks * (split + 1) / splits) - first;
+    const int first = (int)((int64_t)blocks * part / parts), count = (int)((int64_t)blocks * (part + 1) / parts) - first;
     const int steps = (p.C + 15) / 16, slabs = (p.C + 63) / 64;
     auto bar = [&](int i) { return s32(&bars[i]); };
 
@@ -324,11 +341,12 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
                 tm_after();
                 const int row = row0 + t * TILE + (warp & 3) * 32 + lane;
                 const int64_t at = ((int64_t)b * p.Hq + h) * p.Nq + row;
+                const int64_t rest = cut.rest() * 2 * TILE, local = piece.local * 2 * TILE + t * TILE + (warp & 3) * 32 + lane;
                 const bool there = row < p.Nq;
                 const float inverse = ref == -INFINITY ? 0.f : 1.f / l;
                 if (there) {
                     const float lse2 = ref == -INFINITY ? -INFINITY : ref + log2f(l) - FORWARD_SHIFT<T>;
-                    if (splits > 1) partials[splits * rows_of(p) * p.C + split * rows_of(p) + at] = lse2;
+                    if (parts > 1) partials[parts * rest * p.C + part * rest + local] = lse2;
                     else if (p.lse != nullptr) p.lse[at] = lse2 * LN2;
                 }
                 for (int c = 0; c < p.C; c += 32) {
@@ -341,8 +359,8 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
                         for (int i = 0; i < 32; ++i) o[i] = 0;
                     }
                     if (!there) continue;
-                    if (splits > 1) {
-                        float* out = partials + ((int64_t)split * rows_of(p) + at) * p.C + c;
+                    if (parts > 1) {
+                        float* out = partials + (part * rest + local) * p.C + c;
 #pragma unroll
                         for (int i = 0; i < 32; i += 4)
                             if (c + i < p.C)
@@ -398,9 +416,9 @@ template <int D, bool DKDV> struct Backward {
     // Extra steps of the first products (see the forward kernel): one tile of 16 channels for each operand that takes part.
     //   dq      S: ones x weights of the block's points
     //   dk, dv  S: (weight of the row, ones) x (ones, -lse / scale of the block's queries), so that p = exp2(scale_log2 S); T: ones x -D, so that it is t - D
-    // (the queries' are written by the statistics kernel and copied with the block; with a warp of this kernel that made them, it was that warp's 1180 cycles
-    // per block that the others waited for)
-    static constexpr int EXTRA_A = TILE * 32, EXTRA_B = DKDV ? BLOCK * 16 : BLOCK * 32, EXTRAS = DKDV ? 2 : 1;
+    // (the streamed side's are written by the statistics kernel and copied with the block; with a warp of this kernel that made them, it was that warp's 1180
+    // cycles per block that the others waited for)
+    static constexpr int EXTRA_A = TILE * 32, EXTRA_B = BLOCK * 16, EXTRAS = DKDV ? 2 : 1;
     static constexpr int OFF_XA = A_BYTES + STAGES * STAGE_BYTES, OFF_XB = OFF_XA + EXTRAS * EXTRA_A;
     static constexpr size_t SMEM = OFF_XB + STAGES * EXTRAS * EXTRA_B + 1024;
     // TMEM columns: buffers of (S, T), sums, operands
@@ -413,7 +431,7 @@ template <int D, bool DKDV> struct Backward {
 template <typename T, int D, bool DKDV, bool WEIGHTS>
 __global__ void __launch_bounds__(BWD_THREADS, 1)
 attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats stats, const __grid_constant__ CUtensorMap map_a1, const __grid_constant__ CUtensorMap map_a2,
-                          const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_b2, int tiles) {
+                          const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_b2, int tiles, const __grid_constant__ Split cut, float* partials) {
     using K = Backward<D, DKDV>;
     constexpr bool CLEARED = !DKDV && WEIGHTS;          // streamed points may be left out
     constexpr bool EXTRA = DKDV || WEIGHTS;
@@ -424,10 +442,13 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     __shared__ uint32_t tmem_s;
     __shared__ int fail_s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int tile = blockIdx.x % tiles, bh = blockIdx.x / tiles;
+    const Piece piece(cut, tiles);
+    const int tile = piece.tile, bh = piece.bh;
     const int heads = DKDV ? p.Hk : p.Hq, b = bh / heads, head = bh - b * heads, hk = DKDV ? head : head / p.G;
     const int row0 = tile * TILE, N = DKDV ? p.Nk : p.Nq, M = DKDV ? p.Nq : p.Nk;       // rows, streamed points
-    const int per_head = (M + BLOCK - 1) / BLOCK, count = DKDV ? p.G * per_head : per_head;
+    const int per_head = (M + BLOCK - 1) / BLOCK, total = DKDV ? p.G * per_head : per_head;
+    // blocks of the streamed side: `begin` and on, numbered from 0 in the pipeline
+    const int begin = (int)((int64_t)total * piece.part / piece.parts), count = (int)((int64_t)total * (piece.part + 1) / piece.parts) - begin;
     const int steps = (p.C + 15) / 16, slabs = (p.C + 63) / 64;
     const float* weights = p.log_weights == nullptr ? nullptr : p.log_weights + b * p.log_weights_batch;
     auto bar = [&](int i) { return s32(&bars[i]); };
@@ -443,14 +464,21 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
     }
     if (EXTRA) {
-        // ones (the tile of S for dk, dv gets its rows' weights later), and zeros behind what is written per block
+        // ones (the tile of S for dk, dv gets its rows' weights later), and zeros behind them
         for (int e = tid; e < K::EXTRAS * K::EXTRA_A / 16; e += BWD_THREADS)
             *reinterpret_cast<uint4*>(base + K::OFF_XA + e * 16) = (e & 8) ? make_uint4(0, 0, 0, 0) : make_uint4(EXTRA_ONES_0, EXTRA_ONES_1, 0, 0);
-        for (int e = tid; !DKDV && e < K::STAGES * K::EXTRAS * K::EXTRA_B / 16; e += BWD_THREADS) *reinterpret_cast<uint4*>(base + K::OFF_XB + e * 16) = make_uint4(0, 0, 0, 0);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
+    // whether a streamed point of this piece is left out: only then do the blocks pass through the warp that clears rows
+    const int64_t weight_row = p.log_weights_batch == 0 ? 0 : b;
+    int any = 0;
+    if (CLEARED)
+        for (int i = tid; i < count; i += BWD_THREADS) {
+            const uint2 gone = stats.gone[weight_row * per_head + begin + i];
+            any |= (gone.x | gone.y) != 0;
+        }
     tm_before();
-    __syncthreads();
+    const bool clearing = __syncthreads_or(any) != 0;
     tm_after();
     const uint32_t tm = tmem_s;
     bool ok = true;
@@ -471,10 +499,12 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                 const int st = it % K::STAGES, turn = it / K::STAGES;
                 if (turn > 0) ok = mb_wait(bar(K::FREE + st), (turn - 1) & 1, ok);
                 if (!ok) break;
-                const int g = DKDV ? it / per_head : 0, point = (it - g * per_head) * BLOCK, h = DKDV ? head * p.G + g : hk;
-                mb_expect(bar(K::FULL + st), 2 * slabs * BSLAB + (DKDV ? 2 * K::EXTRA_B : 0));
+                const int g = DKDV ? (begin + it) / per_head : 0, point = (begin + it - g * per_head) * BLOCK, h = DKDV ? head * p.G + g : hk;
+                mb_expect(bar(K::FULL + st), 2 * slabs * BSLAB + (EXTRA ? K::EXTRAS * K::EXTRA_B : 0));
                 if (DKDV)
                     bulk_load(s32(base) + K::OFF_XB + st * 2 * K::EXTRA_B, stats.extra + (((int64_t)b * p.Hq + h) * per_head + point / BLOCK) * 2 * BLOCK, 2 * K::EXTRA_B, bar(K::FULL + st));
+                else if (EXTRA)
+                    bulk_load(s32(base) + K::OFF_XB + st * K::EXTRA_B, stats.weights + (weight_row * per_head + point / BLOCK) * BLOCK, K::EXTRA_B, bar(K::FULL + st));
                 for (int s = 0; s < slabs; ++s) {
                     tma_load(stage(st) + s * BSLAB, &map_b1, s * 64, point, h, b, bar(K::FULL + st));
                     tma_load(stage(st) + (K::SLABS + s) * BSLAB, &map_b2, s * 64, point, h, b, bar(K::FULL + st));
@@ -490,12 +520,12 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             const uint32_t da = desc_channels(s32(base) + which * K::SLABS * SLAB), db = desc_channels(stage(0) + which * K::SLABS * BSLAB);
             const uint32_t dp = desc_points(stage(0) + (which == 0 ? K::SLABS * BSLAB : 0), BSLAB), ta = tm + K::T_A + which * (D / 2);
             const uint32_t dxa = desc_extra(s32(base) + K::OFF_XA + which * K::EXTRA_A);
-            const uint32_t dxb = (DKDV ? desc_dense(s32(base) + K::OFF_XB) : desc_extra(s32(base) + K::OFF_XB)) + which * (K::EXTRA_B >> 4);
+            const uint32_t dxb = desc_dense(s32(base) + K::OFF_XB + which * K::EXTRA_B);
             const bool sums = DKDV || which == 1, extra = EXTRA && which < K::EXTRAS;
             const int done = (which == 0 ? K::S_DONE : K::D_READY), full = (which == 0 ? K::S_FULL : K::T_FULL);
             auto first = [&](int it) {
                 const int st = it % K::STAGES;
-                if (!mb_wait(bar((CLEARED ? K::READY : K::FULL) + st), (it / K::STAGES) & 1, true)) return false;
+                if (!mb_wait(bar((clearing ? K::READY : K::FULL) + st), (it / K::STAGES) & 1, true)) return false;
                 const uint32_t to = tm + K::T_BUF + (it & 1) * 2 * BLOCK + which * BLOCK, bd = db + st * (K::STAGE_BYTES >> 4);
 #pragma unroll
                 for (int ks = 0; ks < D / 16; ++ks)
@@ -503,7 +533,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                         if constexpr (K::A_IN_TMEM) mma_ts(to, ta + ks * 8, bd + (ks >> 2) * (BSLAB >> 4) + (ks & 3) * 2, ids, ks > 0);
                         else mma_ss(to, da + (ks >> 2) * (SLAB >> 4) + (ks & 3) * 2, bd + (ks >> 2) * (BSLAB >> 4) + (ks & 3) * 2, ids, ks > 0);
                     }
-                if (extra) mma_ss<DESC_EXTRA_HIGH, DKDV ? DESC_DENSE_HIGH : DESC_EXTRA_HIGH>(to, dxa, dxb + st * (K::EXTRAS * K::EXTRA_B >> 4), idw, 1);
+                if (extra) mma_ss<DESC_EXTRA_HIGH, DESC_DENSE_HIGH>(to, dxa, dxb + st * (K::EXTRAS * K::EXTRA_B >> 4), idw, 1);
                 mma_commit(bar(full + (it & 1)));
                 return true;
             };
@@ -536,46 +566,26 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mb_arrive(bar(K::A_READY));
-        } else if (CLEARED && warp == 18) {
-            // ---------------------------------------------------------------- weights of the streamed points, two blocks ahead
-            const float unscale = 1.f / p.scale;
-            float x[2][2];
-            auto fetch = [&](int it, float (&xs)[2]) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int n = it * BLOCK + i * 32 + lane;
-                    xs[i] = n >= M ? -INFINITY : weights[n];
-                }
-            };
-            auto write = [&](int it, const float (&xs)[2]) {
+        } else if (clearing && warp == 18) {
+            // ---------------------------------------------------------------- rows of streamed points left out
+            const uint2* gone = stats.gone + weight_row * per_head + begin;
+            uint2 next = gone[0];
+            for (int it = 0; it < count && ok; ++it) {
                 const int st = it % K::STAGES;
-                uint2 parts[2];
-                uint32_t gone[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const bool out = xs[i] <= EXCLUDED;
-                    gone[i] = __ballot_sync(0xffffffffu, out && it * BLOCK + i * 32 + lane < M);
-                    parts[i] = out ? make_uint2(EXTRA_OUT, 0) : extra_parts(xs[i] * unscale);
+                const uint2 now = next;
+                if (it + 1 < count) next = gone[it + 1];
+                ok = all_lanes(mb_wait(bar(K::FULL + st), (it / K::STAGES) & 1, ok));
+                if (!ok) break;
+                if (now.x | now.y) {
+                    for (int which = 0; which < 2; ++which) {
+                        unsigned char* at = base + K::A_BYTES + st * K::STAGE_BYTES + which * K::SLABS * BSLAB;
+                        zero_rows(at, slabs, BSLAB, 0, now.x, lane);
+                        zero_rows(at, slabs, BSLAB, 1, now.y, lane);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 }
-                ok = all_lanes(mb_wait(bar(K::FULL + st), (it / K::STAGES) & 1, ok));       // (then the stage's last readers are done, too)
-                if (!ok) return;
-#pragma unroll
-                for (int i = 0; i < 2; ++i) *reinterpret_cast<uint2*>(base + K::OFF_XB + st * K::EXTRA_B + extra_at(i * 32 + lane)) = parts[i];
-                if (gone[0] | gone[1])
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        for (int which = 0; which < 2; ++which) zero_rows(base + K::A_BYTES + st * K::STAGE_BYTES + which * K::SLABS * BSLAB, slabs, BSLAB, i, gone[i], lane);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0) mb_arrive(bar(K::READY + st));
-            };
-            fetch(0, x[0]);
-            if (count > 1) fetch(1, x[1]);
-            for (int it = 0; it < count && ok; it += 2) {
-                write(it, x[0]);
-                if (it + 2 < count) fetch(it + 2, x[0]);
-                if (it + 1 < count && ok) write(it + 1, x[1]);
-                if (it + 3 < count) fetch(it + 3, x[1]);
             }
         }
     } else {
@@ -628,9 +638,9 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             tm_ld32(s, from);
             tm_ld_wait();
             if (!DKDV) warp_arrive(bar(K::S_DONE + group), lane);
-            if (!DKDV && !WEIGHTS && (it + 1) * BLOCK > M) {
+            if (!DKDV && !WEIGHTS && (begin + it + 1) * BLOCK > M) {
                 // points that are not there: zero rows, whose probability must not overflow (the scale is positive)
-                const int left = M - it * BLOCK - half * 32;
+                const int left = M - (begin + it) * BLOCK - half * 32;
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
                     if (i >= left) s[i] = 0xff800000u;
@@ -685,6 +695,18 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                 tm_ld32(o, tm + K::T_ACC + (DKDV ? group * D : 0) + c + lanes);
                 tm_ld_wait();
                 if (!there) continue;
+                if (piece.parts > 1) {
+                    // [dk, dv][part][row][channel]
+                    const int64_t rest = cut.rest() * TILE, local = piece.local * TILE + (warp & 3) * 32 + lane;
+                    float* to = partials + ((DKDV && group == 1 ? piece.parts * rest : 0) + piece.part * rest + local) * p.C + c;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4)
+                        if (c + i < p.C)
+                            *reinterpret_cast<float4*>(to + i) = zero ? make_float4(0.f, 0.f, 0.f, 0.f)
+                                                                      : make_float4(__uint_as_float(o[i]) * back, __uint_as_float(o[i + 1]) * back, __uint_as_float(o[i + 2]) * back,
+                                                                                    __uint_as_float(o[i + 3]) * back);
+                    continue;
+                }
 #pragma unroll
                 for (int i = 0; i < 32; i += 8)
                     if (c + i < p.C) {
@@ -703,6 +725,54 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "r"(512));
 }
 
+// ---- joins of tiles in pieces ---------------------------------------------------------------------------------------------------
+//
+// A thread takes eight channels of a row; the pieces are taken in their order.  forward: out = sum_s 2^(lse2_s - lse2) out_s; backward: a plain sum.
+constexpr int JOIN_THREADS = 256;
+template <typename T, bool SOFTMAX>
+__global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const __grid_constant__ View out, float* lse_out, const __grid_constant__ Split cut, int tiles, int rows_per_tile,
+                                                                         int N, int H, int C, const float* __restrict__ partials) {
+    const int chunks = C / 8;
+    const int64_t rest = cut.rest() * rows_per_tile, index = (int64_t)blockIdx.x * JOIN_THREADS + threadIdx.x, local = index / chunks;
+    const int c = (int)(index - local * chunks) * 8;
+    if (local >= rest) return;
+    const int64_t tile = cut.full + local / rows_per_tile, bh = tile / tiles, b = bh / H, h = bh - b * H;
+    const int n = (int)(tile - bh * tiles) * rows_per_tile + (int)(local % rows_per_tile);
+    if (n >= N) return;
+    const float* statistics = partials + cut.parts * rest * C + local;
+    float top = -INFINITY, total = 0.f;
+    if (SOFTMAX)
+#pragma unroll 4
+        for (int s = 0; s < cut.parts; ++s) top = fmaxf(top, statistics[s * rest]);
+    const float base = top == -INFINITY ? 0.f : top;
+    float sum[8] = {};
+#pragma unroll 4
+    for (int s = 0; s < cut.parts; ++s) {
+        float w = 1.f;
+        if (SOFTMAX) {
+            w = ex2(statistics[s * rest] - base);
+            total += w;
+        }
+        const float4* from = reinterpret_cast<const float4*>(partials + (s * rest + local) * C + c);
+        const float4 x = from[0], y = from[1];
+        const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
+    }
+    const float factor = !SOFTMAX ? 1.f : total == 0.f ? 0.f : 1.f / total;
+    uint32_t x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = pack16<T>(sum[2 * i] * factor, sum[2 * i + 1] * factor);
+    *reinterpret_cast<uint4*>(static_cast<T*>(out.data) + b * out.batch + h * out.head + n * out.point + c) = make_uint4(x[0], x[1], x[2], x[3]);
+    if (SOFTMAX && c == 0 && lse_out != nullptr) lse_out[bh * N + n] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
+}
+template <typename T, bool SOFTMAX>
+cudaError_t join_tiles(const View& out, float* lse, const Split& cut, int tiles, int rows_per_tile, int N, int H, int C, const float* partials, cudaStream_t stream) {
+    const int64_t threads = cut.rest() * rows_per_tile * (C / 8);
+    attend_join_tiles_kernel<T, SOFTMAX><<<(unsigned)((threads + JOIN_THREADS - 1) / JOIN_THREADS), JOIN_THREADS, 0, stream>>>(out, lse, cut, tiles, rows_per_tile, N, H, C, partials);
+    return cudaGetLastError();
+}
+
 using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
                             CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 Encode encoder() {
@@ -719,26 +789,33 @@ template <typename K>
 cudaError_t allow(K kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); }
 
 template <typename T, int D, bool WEIGHTS>
-cudaError_t forward_as(const Problem& p, const CUtensorMap (&maps)[3], int splits, float* partials, cudaStream_t stream) {
+cudaError_t forward_as(const Problem& p, const CUtensorMap (&maps)[3], const Split& cut, float* partials, cudaStream_t stream) {
     const int tiles = (p.Nq + 2 * TILE - 1) / (2 * TILE);
     const auto kernel = attend_forward_tc_kernel<T, D, WEIGHTS>;
-    const cudaError_t e = allow(kernel, Forward<D>::SMEM);
+    cudaError_t e = allow(kernel, Forward<D>::SMEM);
     if (e != cudaSuccess) return e;
-    kernel<<<(unsigned)((int64_t)p.B * p.Hq * tiles * splits), FWD_THREADS, Forward<D>::SMEM, stream>>>(p, maps[0], maps[1], maps[2], tiles, splits, partials);
-    return cudaGetLastError();
+    kernel<<<(unsigned)cut.blocks(), FWD_THREADS, Forward<D>::SMEM, stream>>>(p, maps[0], maps[1], maps[2], tiles, cut, partials);
+    e = cudaGetLastError();
+    if (e != cudaSuccess || cut.rest() == 0) return e;
+    return join_tiles<T, true>(p.out, p.lse, cut, tiles, 2 * TILE, p.Nq, p.Hq, p.C, partials, stream);
 }
 
 template <typename T, int D, bool DKDV, bool WEIGHTS>
-cudaError_t backward_as(const Problem& p, const Stats& s, const CUtensorMap (&maps)[4], cudaStream_t stream) {
-    const int tiles = ((DKDV ? p.Nk : p.Nq) + TILE - 1) / TILE;
+cudaError_t backward_as(const Problem& p, const Stats& s, const CUtensorMap (&maps)[4], const Split& cut, float* partials, cudaStream_t stream) {
+    const int N = DKDV ? p.Nk : p.Nq, H = DKDV ? p.Hk : p.Hq, tiles = (N + TILE - 1) / TILE;
     const auto kernel = attend_backward_tc_kernel<T, D, DKDV, WEIGHTS>;
-    const cudaError_t e = allow(kernel, Backward<D, DKDV>::SMEM);
+    cudaError_t e = allow(kernel, Backward<D, DKDV>::SMEM);
     if (e != cudaSuccess) return e;
-    kernel<<<(unsigned)((int64_t)p.B * (DKDV ? p.Hk : p.Hq) * tiles), BWD_THREADS, Backward<D, DKDV>::SMEM, stream>>>(p, s, maps[0], maps[1], maps[2], maps[3], tiles);
-    return cudaGetLastError();
+    kernel<<<(unsigned)cut.blocks(), BWD_THREADS, Backward<D, DKDV>::SMEM, stream>>>(p, s, maps[0], maps[1], maps[2], maps[3], tiles, cut, partials);
+    e = cudaGetLastError();
+    if (e != cudaSuccess || cut.rest() == 0) return e;
+    e = join_tiles<T, false>(DKDV ? p.dk : p.dq, nullptr, cut, tiles, TILE, N, H, p.C, partials, stream);
+    if (e == cudaSuccess && DKDV) e = join_tiles<T, false>(p.dv, nullptr, cut, tiles, TILE, N, H, p.C, partials + cut.parts * cut.rest() * TILE * p.C, stream);
+    return e;
 }
 template <bool DKDV>
-bool backward_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream, cudaError_t& e) {
+bool backward_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
+    const Split cut = split_of(p, DKDV ? Kernel::DKDV : Kernel::DQ, sms);
     CUtensorMap maps[4];        // A1, A2 (boxes of a tile), B1, B2 (of a block)
     const int q_rows = DKDV ? BLOCK : TILE, k_rows = DKDV ? TILE : BLOCK, q_at = DKDV ? 2 : 0, k_at = 2 - q_at;
     if (!make_map(&maps[q_at], p.q, dtype, p.C, p.Nq, p.Hq, p.B, q_rows) || !make_map(&maps[q_at + 1], p.dout, dtype, p.C, p.Nq, p.Hq, p.B, q_rows) ||
@@ -748,7 +825,7 @@ bool backward_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream
     auto run = [&](auto t, auto width) {
         using T = decltype(t);
         constexpr int D = decltype(width)::value;
-        return weights ? backward_as<T, D, DKDV, true>(p, s, maps, stream) : backward_as<T, D, DKDV, false>(p, s, maps, stream);
+        return weights ? backward_as<T, D, DKDV, true>(p, s, maps, cut, partials, stream) : backward_as<T, D, DKDV, false>(p, s, maps, cut, partials, stream);
     };
     using W64 = std::integral_constant<int, 64>;
     using W128 = std::integral_constant<int, 128>;
@@ -759,8 +836,38 @@ bool backward_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream
 
 }  // namespace
 
-bool backward_dq_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream, cudaError_t& e) { return backward_tc<false>(p, s, dtype, stream, e); }
-bool backward_dkdv_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream, cudaError_t& e) { return backward_tc<true>(p, s, dtype, stream, e); }
+bool backward_dq_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
+    return backward_tc<false>(p, s, dtype, sms, partials, stream, e);
+}
+bool backward_dkdv_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
+    return backward_tc<true>(p, s, dtype, sms, partials, stream, e);
+}
+
+Split split_tiles(int64_t tiles, int64_t streamed, int64_t least, int sms) {
+    const int64_t rest = tiles % sms;
+    Split cut{tiles, tiles, 1};
+    if (rest == 0 || tiles >= 8 * (int64_t)sms) return cut;
+    double best = 0.97;        // of the partial wave; less than a tenth of a wave is not worth a second kernel, nor is a finer cut for a hundredth
+    const int64_t most = std::min(streamed / least, std::max<int64_t>(8, sms / rest));        // (few tiles: one piece per SM)
+    for (int64_t k = 2; k <= most; ++k) {
+        const double wave = (double)((rest * k + sms - 1) / sms) / (double)k + 0.01 * (double)(k < 8 ? k : 8);
+        if (wave < best) { best = wave; cut = Split{tiles, tiles - rest, (int)k}; }
+    }
+    return cut;
+}
+
+Split split_of(const Problem& p, Kernel kernel, int sms) {
+    auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
+    if (kernel == Kernel::FORWARD) return split_tiles((int64_t)p.B * p.Hq * up(p.Nq, 2 * TILE), up(p.Nk, TILE), 2, sms);
+    if (kernel == Kernel::DQ) return split_tiles((int64_t)p.B * p.Hq * up(p.Nq, TILE), up(p.Nk, BLOCK), 4, sms);
+    return split_tiles((int64_t)p.B * p.Hk * up(p.Nk, TILE), p.G * up(p.Nq, BLOCK), 4, sms);
+}
+
+size_t partial_floats(const Problem& p, Kernel kernel, int sms) {
+    const Split cut = split_of(p, kernel, sms);
+    const size_t rows = (size_t)cut.rest() * cut.parts * TILE;
+    return kernel == Kernel::FORWARD ? rows * 2 * (p.C + 1) : rows * p.C * (kernel == Kernel::DKDV ? 2 : 1);
+}
 
 bool make_map(CUtensorMap* map, const View& v, sna_dtype_t dtype, int C, int N, int H, int B, int rows) {
     const Encode fn = encoder();
@@ -774,7 +881,8 @@ bool make_map(CUtensorMap* map, const View& v, sna_dtype_t dtype, int C, int N, 
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool forward_tc(const Problem& p, sna_dtype_t dtype, int splits, float* partials, cudaStream_t stream, cudaError_t& e) {
+bool forward_tc(const Problem& p, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
+    const Split cut = split_of(p, Kernel::FORWARD, sms);
     CUtensorMap maps[3];
     if (!make_map(&maps[0], p.q, dtype, p.C, p.Nq, p.Hq, p.B, TILE) || !make_map(&maps[1], p.k, dtype, p.C, p.Nk, p.Hk, p.B, TILE) ||
         !make_map(&maps[2], p.v, dtype, p.C, p.Nk, p.Hk, p.B, TILE))
@@ -783,7 +891,7 @@ bool forward_tc(const Problem& p, sna_dtype_t dtype, int splits, float* partials
     auto run = [&](auto t, auto width) {
         using T = decltype(t);
         constexpr int D = decltype(width)::value;
-        return weights ? forward_as<T, D, true>(p, maps, splits, partials, stream) : forward_as<T, D, false>(p, maps, splits, partials, stream);
+        return weights ? forward_as<T, D, true>(p, maps, cut, partials, stream) : forward_as<T, D, false>(p, maps, cut, partials, stream);
     };
     using W64 = std::integral_constant<int, 64>;
     using W128 = std::integral_constant<int, 128>;
