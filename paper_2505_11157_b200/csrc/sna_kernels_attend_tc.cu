@@ -51,7 +51,9 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
 //   warp 10      weights of the next block's points; zeroes k and v rows of points left out
 //   warps 0-3 and 4-7  softmax of tile 0 and 1, thread = row: S from TMEM, P back.  The row's reference moves (and O is scaled in TMEM)
 //                only when its maximum has grown by 2^8: then the sums are still far from overflow, and most blocks skip the correction.
-// Narrow heads leave TMEM columns for P beside S: S of the next block is then computed during this block's softmax.  Wide ones keep P
+// Narrow heads leave TMEM columns for P beside S: S of the next block is then computed during this block's softmax.  (Tried and not kept, 64x128, B = 2, four
+// heads of 32, 193 us: the two tiles taking turns with their exponentials 225; four groups with half a row per thread, whose scores do not fit their
+// 104 registers, 240.)  Wide ones keep P
 // in S's columns; while one tile's products run, the other tile's softmax does.
 // A point's weight is one more step of the first product: its parts against ones.  (Added per element, with the weights read from shared memory, it
 // cost 40 % of the time: 64x128, B = 2, eight heads of 128, 683 us against 486 without weights.)
@@ -785,14 +787,25 @@ Encode encoder() {
     return fn;
 }
 
+// Opts a kernel in to its shared memory, once per device (`done`: one bit each; a kernel's own).
 template <typename K>
-cudaError_t allow(K kernel, size_t bytes) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); }
+cudaError_t allow(K kernel, size_t bytes, std::atomic<uint64_t>& done) {
+    int device = -1;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = device < 64 ? (uint64_t)1 << device : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 template <typename T, int D, bool WEIGHTS>
 cudaError_t forward_as(const Problem& p, const CUtensorMap (&maps)[3], const Split& cut, float* partials, cudaStream_t stream) {
     const int tiles = (p.Nq + 2 * TILE - 1) / (2 * TILE);
     const auto kernel = attend_forward_tc_kernel<T, D, WEIGHTS>;
-    cudaError_t e = allow(kernel, Forward<D>::SMEM);
+    static std::atomic<uint64_t> allowed{0};
+    cudaError_t e = allow(kernel, Forward<D>::SMEM, allowed);
     if (e != cudaSuccess) return e;
     kernel<<<(unsigned)cut.blocks(), FWD_THREADS, Forward<D>::SMEM, stream>>>(p, maps[0], maps[1], maps[2], tiles, cut, partials);
     e = cudaGetLastError();
@@ -804,7 +817,8 @@ template <typename T, int D, bool DKDV, bool WEIGHTS>
 cudaError_t backward_as(const Problem& p, const Stats& s, const CUtensorMap (&maps)[4], const Split& cut, float* partials, cudaStream_t stream) {
     const int N = DKDV ? p.Nk : p.Nq, H = DKDV ? p.Hk : p.Hq, tiles = (N + TILE - 1) / TILE;
     const auto kernel = attend_backward_tc_kernel<T, D, DKDV, WEIGHTS>;
-    cudaError_t e = allow(kernel, Backward<D, DKDV>::SMEM);
+    static std::atomic<uint64_t> allowed{0};
+    cudaError_t e = allow(kernel, Backward<D, DKDV>::SMEM, allowed);
     if (e != cudaSuccess) return e;
     kernel<<<(unsigned)cut.blocks(), BWD_THREADS, Backward<D, DKDV>::SMEM, stream>>>(p, s, maps[0], maps[1], maps[2], maps[3], tiles, cut, partials);
     e = cudaGetLastError();
