@@ -79,14 +79,22 @@ template <int CP> __device__ __forceinline__ void load_bt(uint32_t (&b)[4], uint
     ldsm_t(b, tile + piece<CP>(k0 + (lane & 7) + (((lane >> 3) & 1) << 3), n * 2 + (lane >> 4)));
 }
 
-// rows [first, first + R) of a head's points (stride `point`); a row that is not there, or for which take(row in tile) is false, is zero
-template <int CP, typename T, typename Take>
-__device__ __forceinline__ void load_rows(uint32_t tile, const T* head, int64_t point, int first, int rows, int R, int C, Take take) {
-    constexpr int CH = CP / 8;
-    for (int e = threadIdx.x; e < R * CH; e += THREADS) {
-        const int r = e / CH, c = e - r * CH;
-        const bool there = first + r < rows && c * 8 < C && take(r);
-        copy16(tile + piece<CP>(r, c), there ? head + (int64_t)(first + r) * point + c * 8 : head, there);
+// rows [first, first + R) of a head's points (stride `point`); a row that is not there, or for which take(row in tile) is false, is zero.
+// A thread's pieces lie RP rows apart, which is a multiple of the permutation's period: one address each way, and steps.  take also sees to rows
+// behind the last point.
+template <int CP, int R, typename T, typename Take>
+__device__ __forceinline__ void load_rows(uint32_t tile, const T* head, int64_t point, int first, int C, Take take) {
+    constexpr int CH = CP / 8, RP = THREADS / CH;
+    static_assert(RP % 8 == 0 && R % RP == 0, "steps of whole periods");
+    const int r0 = threadIdx.x / CH, c = threadIdx.x - r0 * CH;
+    const T* src = head + (first + r0) * point + c * 8;
+    const uint32_t dst = tile + piece<CP>(r0, c);
+    const bool channel = c * 8 < C;
+#pragma unroll
+    for (int i = 0; i < R / RP; ++i) {
+        const bool there = channel && take(r0 + i * RP);
+        copy16(dst + i * RP * CP * 2, there ? src : head, there);
+        src += RP * point;
     }
 }
 // the same for the stacked rows of the query heads of a group: row = head in the group * Nq + query
@@ -147,8 +155,8 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
         if (j < last) {
             auto take = [&](int r) { return bias[j & 3][r] != -INFINITY; };
             const uint32_t stage = tkv + ((j - first) % STAGES) * 2 * BN * CP * 2;
-            load_rows<CP>(stage, kh, p.k.point, j * BN, p.Nk, BN, p.C, take);
-            load_rows<CP>(stage + BN * CP * 2, vh, p.v.point, j * BN, p.Nk, BN, p.C, take);
+            load_rows<CP, BN>(stage, kh, p.k.point, j * BN, p.C, take);
+            load_rows<CP, BN>(stage + BN * CP * 2, vh, p.v.point, j * BN, p.C, take);
         }
         commit();
     };
@@ -166,6 +174,13 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
 
+    uint32_t q[WM == 1 ? CP / 16 : 1][4];        // few rows: the queries' operands stay in registers
+    if (WM == 1) {
+        wait_group<STAGES - 2>();
+        __syncthreads();
+#pragma unroll
+        for (int ks = 0; ks < CP / 16; ++ks) load_a<CP>(q[WM == 1 ? ks : 0], tq, 0, ks, lane);
+    }
     for (int j = first; j < last; ++j) {
         store_bias(j + STAGES);
         fetch_bias(j + STAGES + 1);
@@ -181,8 +196,8 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
             for (int i = 0; i < 4; ++i) s[n][i] = 0.f;
 #pragma unroll
         for (int ks = 0; ks < CP / 16; ++ks) {
-            uint32_t a[4];
-            load_a<CP>(a, tq, wm * 16, ks, lane);
+            uint32_t (&a)[4] = q[WM == 1 ? ks : 0];
+            if (WM != 1) load_a<CP>(a, tq, wm * 16, ks, lane);
 #pragma unroll
             for (int n = 0; n < NT; n += 2) {
                 uint32_t kb[4];
@@ -208,11 +223,13 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
             top[r] = fmaxf(top[r], __shfl_xor_sync(0xffffffffu, top[r], 2));
             const float now = fmaxf(m[r], top[r]);
             base[r] = now == -INFINITY ? 0.f : now;                 // (no point so far: every weight is exp2(-infinity))
-            const float correction = ex2(m[r] - base[r]);
-            m[r] = now;
-            l[r] *= correction;
+            if (__any_sync(0xffffffffu, now != m[r])) {         // (a new maximum gets rare)
+                const float correction = ex2(m[r] - base[r]);
+                l[r] *= correction;
 #pragma unroll
-            for (int n = 0; n < CN; ++n) { o[n][2 * r] *= correction; o[n][2 * r + 1] *= correction; }
+                for (int n = 0; n < CN; ++n) { o[n][2 * r] *= correction; o[n][2 * r + 1] *= correction; }
+            }
+            m[r] = now;
         }
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -471,8 +488,8 @@ __global__ void __launch_bounds__(THREADS) attend_dq_kernel(const __grid_constan
         if (j < last) {
             auto take = [&](int r) { return bias[j & 3][r] != -INFINITY; };
             const uint32_t stage = tkv + (j & 1) * 2 * BN * CP * 2;
-            load_rows<CP>(stage, kh, p.k.point, j * BN, p.Nk, BN, p.C, take);
-            load_rows<CP>(stage + BN * CP * 2, vh, p.v.point, j * BN, p.Nk, BN, p.C, take);
+            load_rows<CP, BN>(stage, kh, p.k.point, j * BN, p.C, take);
+            load_rows<CP, BN>(stage + BN * CP * 2, vh, p.v.point, j * BN, p.C, take);
         }
         commit();
     };
@@ -601,9 +618,9 @@ __global__ void __launch_bounds__(THREADS) attend_dkdv_kernel(const __grid_const
         }
         commit();
     };
-    auto take = [&](int r) { return weight2(weights, min(key0 + r, p.Nk - 1)) != -INFINITY; };
-    load_rows<CP>(tk, static_cast<const T*>(p.k.data) + b * p.k.batch + hk * p.k.head, p.k.point, key0, p.Nk, BM, p.C, take);
-    load_rows<CP>(tv, static_cast<const T*>(p.v.data) + b * p.v.batch + hk * p.v.head, p.v.point, key0, p.Nk, BM, p.C, take);
+    auto take = [&](int r) { return key0 + r < p.Nk && weight2(weights, key0 + r) != -INFINITY; };
+    load_rows<CP, BM>(tk, static_cast<const T*>(p.k.data) + b * p.k.batch + hk * p.k.head, p.k.point, key0, p.C, take);
+    load_rows<CP, BM>(tv, static_cast<const T*>(p.v.data) + b * p.v.batch + hk * p.v.head, p.v.point, key0, p.C, take);
     load_block(0);
     float w2[2];
 #pragma unroll
