@@ -11,6 +11,7 @@ around them.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 from typing import Optional
 
@@ -299,6 +300,7 @@ class Plan:
         self.nlat_in, self.nlon_in, self.nlat_out, self.nlon_out = nlat_in, nlon_in, nlat_out, nlon_out
         self.grid_in, self.grid_out, self.theta_cutoff = grid_in, grid_out, float(theta_cutoff)
         self.host_only = host_only
+        self.global_attention = bool(global_attention) or self.theta_cutoff >= math.pi      # every point attends to every point
         self.handle = None
         self.native = None      # the autograd function's owner of the handle, once there is one
         if global_attention:

@@ -99,3 +99,31 @@ def rotate(parts, dtype=0, B=1, C=8, eps=1e-6, backward=False, workspace=None, w
 def test_the_c_abi_refuses(status, call):
     assert call() == status
     assert status == 0 or lib.sna_last_error_message() != b""
+
+
+def attention(**kw):
+    t = sna.SnaTensor(4096, 8, 8, 32, 8)
+    a = sna.SnaAttention(B=1, Hq=2, Hk=1, C=8, nlat_q=2, nlon_q=4, nlat_k=2, nlon_k=4, q=t, k=t, v=t, out=t, dout=t, dq=t, dk=t, dv=t, lse=4096, scale=0.3)
+    for name, value in kw.items():
+        setattr(a, name, value)
+    return a
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("status, a, dtype", [
+    (2, attention(), 0), (2, attention(), 3), (2, attention(C=12), 1), (2, attention(C=136), 1), (1, attention(Hq=3, Hk=2), 1), (1, attention(Hq=3, Hk=0), 1),
+    (1, attention(B=-1), 1), (1, attention(nlat_k=-1), 1), (1, attention(scale=math.inf), 1), (1, attention(scale=math.nan), 1),
+    (2, attention(nlat_q=1 << 15, nlon_q=1 << 15), 1), (2, attention(B=1 << 30, Hq=1 << 4, Hk=1), 1), (1, attention(lse=4098), 1), (1, attention(log_weights=4098), 1),
+    (1, attention(q=sna.SnaTensor(4104, 8, 8, 32, 8)), 1), (1, attention(k=sna.SnaTensor(4096, 8, 8, 32, 4)), 1), (1, attention(v=sna.SnaTensor(4096, 8, 8, 40, 8)), 2),
+    (1, attention(out=sna.SnaTensor(None, 8, 8, 32, 8)), 2),
+], ids=lambda v: None)
+def test_the_c_abi_refuses_attention(status, a, dtype, backward):
+    call, size = (lib.sna_attention_backward, lib.sna_attention_backward_workspace_bytes) if backward else (lib.sna_attention_forward, lib.sna_attention_forward_workspace_bytes)
+    assert call(a, dtype, 4096, 1 << 40, None) == status
+    assert size(a, dtype) == 0
+
+
+def test_attention_of_nothing_and_a_missing_problem():
+    assert lib.sna_attention_forward(None, 1, None, 0, None) == 1 and lib.sna_attention_backward(None, 1, None, 0, None) == 1
+    assert lib.sna_attention_forward(attention(B=0), 1, None, 0, None) == 0 and lib.sna_attention_backward(attention(B=0), 1, None, 0, None) == 0
+    assert lib.sna_attention_backward(attention(lse=None), 1, 4096, 1 << 40, None) == 1
