@@ -33,7 +33,8 @@ sna_status_t describe(const sna_attention_t* a, sna_dtype_t dtype, bool backward
     if (((uintptr_t)a->lse | (uintptr_t)a->log_weights) & 3u) return fail(SNA_ERR_INVALID_ARG, "lse and log_weights must be 4-byte aligned");
     struct { const sna_tensor_t& t; View& view; bool used, query; } tensors[] = {
         {a->q, p.q, true, true},          {a->k, p.k, true, false},       {a->v, p.v, true, false},       {a->out, p.out, true, true},
-        {a->dout, p.dout, backward, true}, {a->dq, p.dq, backward, true}, {a->dk, p.dk, backward, false}, {a->dv, p.dv, backward, false}};
+        {a->out_rest, p.rest, a->out_rest.data != nullptr, true},
+                {a->dout, p.dout, backward, true}, {a->dq, p.dq, backward, true}, {a->dk, p.dk, backward, false}, {a->dv, p.dv, backward, false}};
     for (const auto& x : tensors) {
         if (!x.used) continue;
         if (!multiple_of_8(x.t)) return fail(SNA_ERR_INVALID_ARG, "data pointers and strides must be multiples of 8 elements");

@@ -17,7 +17,7 @@ struct View {
 };
 
 struct Problem {
-    View q, k, v, out, dout, dq, dk, dv;
+    View q, k, v, out, rest, dout, dq, dk, dv;      // rest: what rounding took from out; its data may be null
     float* lse;                     // [B][Hq][Nq], natural logarithm; may be null in the forward pass
     const float* log_weights;       // [B or 1][Nk], or null
     int64_t log_weights_batch;      // 0: shared

@@ -118,6 +118,14 @@ __device__ __forceinline__ float weight2(const float* weights, int n) {
 
 // ---- forward ---------------------------------------------------------------------------------------------------------------
 
+// One value of out, and what its rounding leaves.
+template <typename T>
+__device__ __forceinline__ void store_out(const Problem& p, int64_t b, int64_t h, int64_t n, int c, float x) {
+    const T rounded = from_float<T>(x);
+    static_cast<T*>(p.out.data)[b * p.out.batch + h * p.out.head + n * p.out.point + c] = rounded;
+    if (p.rest.data != nullptr) static_cast<T*>(p.rest.data)[b * p.rest.batch + h * p.rest.head + n * p.rest.point + c] = from_float<T>(x - to_float(rounded));
+}
+
 // Stages of (K, V): a memory-bound walk wants two under way (one station over 361x720, B = 2, 2 key heads of 64, bf16: 71 us with one)
 template <int WM> constexpr int FORWARD_STAGES = WM == 1 ? 3 : 2;
 template <int CP, int WM> constexpr int forward_smem() { return WM * 16 * CP * 2 + FORWARD_STAGES<WM> * 2 * BN * CP * 2; }
@@ -294,7 +302,7 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
 #pragma unroll
                 for (int w = 0; w < WARPS; ++w) sum += factor[w] * join[(w * 16 + r) * PITCH + c];
                 if (partials != nullptr) partials[((int64_t)split * rows_of(p) + at) * p.C + c] = sum * inverse;
-                else static_cast<T*>(p.out.data)[b * p.out.batch + (int64_t)(hk * p.G + g) * p.out.head + (int64_t)(row - g * p.Nq) * p.out.point + c] = from_float<T>(sum * inverse);
+                else store_out<T>(p, b, hk * p.G + g, row - g * p.Nq, c, sum * inverse);
             }
             if (lane == 0) {
                 if (partials != nullptr) partials[splits * rows_of(p) * p.C + split * rows_of(p) + at] = lse2;
@@ -317,7 +325,16 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
                 if (c >= p.C) continue;
                 const float x = o[n][2 * r] * inverse, y = o[n][2 * r + 1] * inverse;
                 if (partials != nullptr) *reinterpret_cast<float2*>(partials + ((int64_t)split * rows_of(p) + at) * p.C + c) = make_float2(x, y);
-                else *reinterpret_cast<uint32_t*>(out + c) = pack<T>(x, y);
+                else {
+                    const uint32_t word = pack<T>(x, y);
+                    *reinterpret_cast<uint32_t*>(out + c) = word;
+                    if (p.rest.data != nullptr) {
+                        float hi_x, hi_y;
+                        unpack2(pair_of<T>(word), hi_x, hi_y);
+                        T* rest = static_cast<T*>(p.rest.data) + b * p.rest.batch + (int64_t)(hk * p.G + g) * p.rest.head + (int64_t)(row - g * p.Nq) * p.rest.point;
+                        *reinterpret_cast<uint32_t*>(rest + c) = pack<T>(x - hi_x, y - hi_y);
+                    }
+                }
             }
             if ((lane & 3) == 0) {
                 if (partials != nullptr) partials[splits * rows_of(p) * p.C + split * rows_of(p) + at] = lse2;
@@ -370,11 +387,10 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) attend_join_kernel(const __gr
     }
     const int n = (int)(at % p.Nq);
     const int64_t bh = at / p.Nq, b = bh / p.Hq, h = bh - b * p.Hq;
-    T* out = static_cast<T*>(p.out.data) + b * p.out.batch + h * p.out.head + n * p.out.point;
     const float inverse = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        if (lane + 32 * i < p.C) out[lane + 32 * i] = from_float<T>(sum[i] * inverse);
+        if (lane + 32 * i < p.C) store_out<T>(p, b, h, n, lane + 32 * i, sum[i] * inverse);
     if (lane == 0 && p.lse != nullptr) p.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
 }
 
@@ -414,6 +430,7 @@ __global__ void __launch_bounds__(256) attend_statistics_kernel(const __grid_con
         const View& x = queries ? p.dout : p.v;
         const T* px = static_cast<const T*>(x.data) + b * x.batch + h * x.head + n * x.point;
         const T* py = queries ? static_cast<const T*>(p.out.data) + b * p.out.batch + h * p.out.head + n * p.out.point : px;
+        const T* pr = queries && p.rest.data != nullptr ? static_cast<const T*>(p.rest.data) + b * p.rest.batch + h * p.rest.head + n * p.rest.point : nullptr;
         for (int c = part * 8; c < p.C; c += 32) {
             const Pack<T, 8> a = *reinterpret_cast<const Pack<T, 8>*>(px + c), o = *reinterpret_cast<const Pack<T, 8>*>(py + c);
 #pragma unroll
@@ -421,6 +438,11 @@ __global__ void __launch_bounds__(256) attend_statistics_kernel(const __grid_con
                 const float f = to_float(a.v[i]);
                 dot = fmaf(f, to_float(o.v[i]), dot);
                 if (SCALED) square = fmaf(f, f, square);
+            }
+            if (pr != nullptr) {
+                const Pack<T, 8> r = *reinterpret_cast<const Pack<T, 8>*>(pr + c);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dot = fmaf(to_float(a.v[i]), to_float(r.v[i]), dot);
             }
         }
     }

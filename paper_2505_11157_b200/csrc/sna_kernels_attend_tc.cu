@@ -70,6 +70,23 @@ template <int D> struct Forward {
            V_READY = K_READY + STAGES, S_FULL = V_READY + STAGES, S_FREE = S_FULL + 2, P_READY = S_FREE + 2 /* [tile][half] */, O_DONE = P_READY + 4, DRAIN = O_DONE + 2, COUNT = DRAIN + 2 };
 };
 
+// Eight values rounded to 16 bits, and what rounding took from them.
+template <typename T>
+__device__ __forceinline__ void store8(T* out, T* rest, const float (&y)[8]) {
+    uint32_t x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = pack16<T>(y[2 * k], y[2 * k + 1]);
+    *reinterpret_cast<uint4*>(out) = make_uint4(x[0], x[1], x[2], x[3]);
+    if (rest == nullptr) return;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        float a, b;
+        unpack2(pair_of<T>(x[k]), a, b);
+        x[k] = pack16<T>(y[2 * k] - a, y[2 * k + 1] - b);
+    }
+    *reinterpret_cast<uint4*>(rest) = make_uint4(x[0], x[1], x[2], x[3]);
+}
+
 // Rounded to float16, weights up to 2^8 times the reference's must stay finite: 2^(8 + 7) < 65504.
 template <typename T> constexpr float FORWARD_SHIFT = 0.f;
 template <> constexpr float FORWARD_SHIFT<__half> = 7.f;
@@ -370,13 +387,14 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
                                                                                   __uint_as_float(o[i + 2]) * inverse, __uint_as_float(o[i + 3]) * inverse);
                     } else {
                         T* out = static_cast<T*>(p.out.data) + b * p.out.batch + h * p.out.head + row * p.out.point + c;
+                        T* rest_out = p.rest.data == nullptr ? nullptr : static_cast<T*>(p.rest.data) + b * p.rest.batch + h * p.rest.head + row * p.rest.point;
 #pragma unroll
                         for (int i = 0; i < 32; i += 8)
                             if (c + i < p.C) {
-                                uint32_t x[4];
+                                float y[8];
 #pragma unroll
-                                for (int k = 0; k < 4; ++k) x[k] = pack16<T>(__uint_as_float(o[i + 2 * k]) * inverse, __uint_as_float(o[i + 2 * k + 1]) * inverse);
-                                *reinterpret_cast<uint4*>(out + i) = make_uint4(x[0], x[1], x[2], x[3]);
+                                for (int k = 0; k < 8; ++k) y[k] = __uint_as_float(o[i + k]) * inverse;
+                                store8<T>(out + i, rest_out == nullptr ? nullptr : rest_out + c + i, y);
                             }
                     }
                 }
@@ -453,6 +471,44 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     const int begin = (int)((int64_t)total * piece.part / piece.parts), count = (int)((int64_t)total * (piece.part + 1) / piece.parts) - begin;
     const int steps = (p.C + 15) / 16, slabs = (p.C + 63) / 64;
     const float* weights = p.log_weights == nullptr ? nullptr : p.log_weights + b * p.log_weights_batch;
+    // Whether points are left out.  dq: only then do the streamed blocks pass through the warp that clears rows.  Either side all of whose points are left out
+    // gets zeros at once.
+    const int64_t weight_row = p.log_weights_batch == 0 ? 0 : b;
+    bool clearing = false;
+    if (WEIGHTS) {
+        int gone_here = 0, present = 0;
+        if (DKDV) {
+            if (tid < TILE && row0 + tid < N) present = !(weights[row0 + tid] <= EXCLUDED);
+        } else {
+            for (int i = tid; i < count; i += BWD_THREADS) {
+                const uint2 gone = stats.gone[weight_row * per_head + begin + i];
+                const int left = M - (begin + i) * BLOCK;
+                const uint32_t low = left >= 32 ? ~0u : (1u << left) - 1u, high = left >= 64 ? ~0u : left <= 32 ? 0u : (1u << (left - 32)) - 1u;
+                gone_here |= (gone.x | gone.y) != 0;
+                present |= ((~gone.x & low) | (~gone.y & high)) != 0;
+            }
+            clearing = __syncthreads_or(gone_here) != 0;
+        }
+        if (__syncthreads_or(present) == 0) {
+            const int chunks = p.C / 8;
+            for (int e = tid; e < TILE * chunks; e += BWD_THREADS) {
+                const int r = e / chunks, c = (e - r * chunks) * 8, row = row0 + r;
+                if (row >= N) continue;
+#pragma unroll
+                for (int which = 0; which < (DKDV ? 2 : 1); ++which) {
+                    if (piece.parts > 1) {
+                        const int64_t rest = cut.rest() * TILE;
+                        float4* to = reinterpret_cast<float4*>(partials + (which * piece.parts * rest + piece.part * rest + piece.local * TILE + r) * p.C + c);
+                        to[0] = to[1] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    } else {
+                        const View& v = DKDV ? (which == 0 ? p.dk : p.dv) : p.dq;
+                        *reinterpret_cast<uint4*>(static_cast<T*>(v.data) + b * v.batch + head * v.head + row * v.point + c) = make_uint4(0, 0, 0, 0);
+                    }
+                }
+            }
+            return;
+        }
+    }
     auto bar = [&](int i) { return s32(&bars[i]); };
     auto stage = [&](int st) { return s32(base) + K::A_BYTES + st * K::STAGE_BYTES; };
 
@@ -471,16 +527,8 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             *reinterpret_cast<uint4*>(base + K::OFF_XA + e * 16) = (e & 8) ? make_uint4(0, 0, 0, 0) : make_uint4(EXTRA_ONES_0, EXTRA_ONES_1, 0, 0);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    // whether a streamed point of this piece is left out: only then do the blocks pass through the warp that clears rows
-    const int64_t weight_row = p.log_weights_batch == 0 ? 0 : b;
-    int any = 0;
-    if (CLEARED)
-        for (int i = tid; i < count; i += BWD_THREADS) {
-            const uint2 gone = stats.gone[weight_row * per_head + begin + i];
-            any |= (gone.x | gone.y) != 0;
-        }
     tm_before();
-    const bool clearing = __syncthreads_or(any) != 0;
+    __syncthreads();
     tm_after();
     const uint32_t tm = tmem_s;
     bool ok = true;
@@ -732,7 +780,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
 // A thread takes eight channels of a row; the pieces are taken in their order.  forward: out = sum_s 2^(lse2_s - lse2) out_s; backward: a plain sum.
 constexpr int JOIN_THREADS = 256;
 template <typename T, bool SOFTMAX>
-__global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const __grid_constant__ View out, float* lse_out, const __grid_constant__ Split cut, int tiles, int rows_per_tile,
+__global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const __grid_constant__ View out, const __grid_constant__ View rest_out, float* lse_out, const __grid_constant__ Split cut, int tiles, int rows_per_tile,
                                                                          int N, int H, int C, const float* __restrict__ partials) {
     const int chunks = C / 8;
     const int64_t rest = cut.rest() * rows_per_tile, index = (int64_t)blockIdx.x * JOIN_THREADS + threadIdx.x, local = index / chunks;
@@ -762,16 +810,16 @@ __global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const _
         for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
     }
     const float factor = !SOFTMAX ? 1.f : total == 0.f ? 0.f : 1.f / total;
-    uint32_t x[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = pack16<T>(sum[2 * i] * factor, sum[2 * i + 1] * factor);
-    *reinterpret_cast<uint4*>(static_cast<T*>(out.data) + b * out.batch + h * out.head + n * out.point + c) = make_uint4(x[0], x[1], x[2], x[3]);
+    for (int i = 0; i < 8; ++i) sum[i] *= factor;
+    store8<T>(static_cast<T*>(out.data) + b * out.batch + h * out.head + n * out.point + c,
+              rest_out.data == nullptr ? nullptr : static_cast<T*>(rest_out.data) + b * rest_out.batch + h * rest_out.head + n * rest_out.point + c, sum);
     if (SOFTMAX && c == 0 && lse_out != nullptr) lse_out[bh * N + n] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
 }
 template <typename T, bool SOFTMAX>
-cudaError_t join_tiles(const View& out, float* lse, const Split& cut, int tiles, int rows_per_tile, int N, int H, int C, const float* partials, cudaStream_t stream) {
+cudaError_t join_tiles(const View& out, const View& rest_out, float* lse, const Split& cut, int tiles, int rows_per_tile, int N, int H, int C, const float* partials, cudaStream_t stream) {
     const int64_t threads = cut.rest() * rows_per_tile * (C / 8);
-    attend_join_tiles_kernel<T, SOFTMAX><<<(unsigned)((threads + JOIN_THREADS - 1) / JOIN_THREADS), JOIN_THREADS, 0, stream>>>(out, lse, cut, tiles, rows_per_tile, N, H, C, partials);
+    attend_join_tiles_kernel<T, SOFTMAX><<<(unsigned)((threads + JOIN_THREADS - 1) / JOIN_THREADS), JOIN_THREADS, 0, stream>>>(out, rest_out, lse, cut, tiles, rows_per_tile, N, H, C, partials);
     return cudaGetLastError();
 }
 
@@ -810,7 +858,7 @@ cudaError_t forward_as(const Problem& p, const CUtensorMap (&maps)[3], const Spl
     kernel<<<(unsigned)cut.blocks(), FWD_THREADS, Forward<D>::SMEM, stream>>>(p, maps[0], maps[1], maps[2], tiles, cut, partials);
     e = cudaGetLastError();
     if (e != cudaSuccess || cut.rest() == 0) return e;
-    return join_tiles<T, true>(p.out, p.lse, cut, tiles, 2 * TILE, p.Nq, p.Hq, p.C, partials, stream);
+    return join_tiles<T, true>(p.out, p.rest, p.lse, cut, tiles, 2 * TILE, p.Nq, p.Hq, p.C, partials, stream);
 }
 
 template <typename T, int D, bool DKDV, bool WEIGHTS>
@@ -823,8 +871,8 @@ cudaError_t backward_as(const Problem& p, const Stats& s, const CUtensorMap (&ma
     kernel<<<(unsigned)cut.blocks(), BWD_THREADS, Backward<D, DKDV>::SMEM, stream>>>(p, s, maps[0], maps[1], maps[2], maps[3], tiles, cut, partials);
     e = cudaGetLastError();
     if (e != cudaSuccess || cut.rest() == 0) return e;
-    e = join_tiles<T, false>(DKDV ? p.dk : p.dq, nullptr, cut, tiles, TILE, N, H, p.C, partials, stream);
-    if (e == cudaSuccess && DKDV) e = join_tiles<T, false>(p.dv, nullptr, cut, tiles, TILE, N, H, p.C, partials + cut.parts * cut.rest() * TILE * p.C, stream);
+    e = join_tiles<T, false>(DKDV ? p.dk : p.dq, View{}, nullptr, cut, tiles, TILE, N, H, p.C, partials, stream);
+    if (e == cudaSuccess && DKDV) e = join_tiles<T, false>(p.dv, View{}, nullptr, cut, tiles, TILE, N, H, p.C, partials + cut.parts * cut.rest() * TILE * p.C, stream);
     return e;
 }
 template <bool DKDV>

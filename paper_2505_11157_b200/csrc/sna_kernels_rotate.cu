@@ -172,6 +172,7 @@ __global__ void __launch_bounds__(ROTATE_THREADS, BACKWARD ? 3 : 4) norm_rotate_
             if (s + U < s_end) fetch(s + U);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                if (s + u >= s_end) break;          // (the same for the whole block; what is in the registers then is an earlier vector)
                 uint64_t xf[VP], v[VP], vp[VP];
                 pairs_of<T, V>(xs[u], xf);
                 pairs_of<T, V>(partners(BACKWARD ? gs[u] : xs[u]), vp);
@@ -208,7 +209,7 @@ __global__ void __launch_bounds__(ROTATE_THREADS, BACKWARD ? 3 : 4) norm_rotate_
 #pragma unroll
                     for (int i = 0; i < VP; ++i) v[i] = mul2(v[i], r2);
                 }
-                if (here && s + u < s_end) store_words<T, V>(y, words_of<T, V>(v));
+                if (here) store_words<T, V>(y, words_of<T, V>(v));
                 walk_y.step(y);
             }
         }

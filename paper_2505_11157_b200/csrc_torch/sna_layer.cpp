@@ -81,7 +81,7 @@ void check_part(const RotatePart& p, const char* name, const at::Tensor& q) {
     check_like(p.x, name, q, "q");
     TORCH_CHECK_VALUE(p.x.dim() == 5 && p.x.size(0) == q.size(0) && p.x.size(4) == q.size(4), name, " must be [B, H, nlat, nlon, C] with B = ", q.size(0), " and C = ",
                       q.size(4), ", got ", p.x.sizes());
-    for (int i = 0; i < 4; ++i) TORCH_CHECK_VALUE(p.x.size(i) < (1 << 30), name, " is too large: ", p.x.sizes());
+    for (int i = 0; i < 5; ++i) TORCH_CHECK_VALUE(p.x.size(i) < (1 << 30), name, " is too large: ", p.x.sizes());
     if (p.weight.defined()) {
         check_cuda(p.weight, (n + "_weight").c_str(), q, "q");
         TORCH_CHECK_VALUE(p.weight.scalar_type() == at::kFloat && p.weight.dim() == 1 && p.weight.size(0) == q.size(4), name, "_weight must be float32 of shape [", q.size(4), "]");
@@ -227,7 +227,7 @@ void check_attention(const AttentionInputs& in) {
                       ", got ", in.k.sizes());
     TORCH_CHECK_VALUE(in.v.sizes() == in.k.sizes(), "v has shape ", in.v.sizes(), ", expected ", in.k.sizes());
     for (const at::Tensor* t : {&in.q, &in.k})
-        for (int i = 0; i < 4; ++i) TORCH_CHECK_VALUE(t->size(i) < (1 << 30), "a tensor is too large: ", t->sizes());
+        for (int i = 0; i < 5; ++i) TORCH_CHECK_VALUE(t->size(i) < (1 << 30), "a tensor is too large: ", t->sizes());
     TORCH_CHECK_VALUE(in.k.size(1) > 0 ? q.size(1) % in.k.size(1) == 0 : q.size(1) == 0, "q's heads (", q.size(1), ") must be a multiple of k's (", in.k.size(1), ")");
     if (!in.log_weights.defined()) return;
     const at::Tensor& w = in.log_weights;
@@ -253,7 +253,7 @@ sna_attention_t described(const AttentionInputs& in) {
 }
 
 // (the inputs become what the kernels read)
-std::tuple<at::Tensor, at::Tensor> attention_forward(AttentionInputs& in) {
+std::tuple<at::Tensor, at::Tensor, at::Tensor> attention_forward(AttentionInputs& in, bool for_backward) {
     const c10::cuda::CUDAGuard guard(in.q.device());
     for (at::Tensor* t : {&in.q, &in.k, &in.v}) *t = attendable(*t);
     if (in.log_weights.defined() && in.log_weights.size(-1) > 1 && in.log_weights.stride(-1) != 1) in.log_weights = in.log_weights.contiguous();
@@ -261,20 +261,25 @@ std::tuple<at::Tensor, at::Tensor> attention_forward(AttentionInputs& in) {
     const sna_dtype_t dtype = dtype_of(in.q, "q");
     sna_attention_t a = described(in);
     a.out = described(out);
+    at::Tensor rest;
+    if (for_backward) {
+        rest = attention_result_like(in.q);
+        a.out_rest = described(rest);
+    }
     a.lse = lse.data_ptr<float>();
     const size_t bytes = sna_attention_forward_workspace_bytes(&a, dtype);
     at::Tensor workspace;
     if (bytes > 0) workspace = at::empty({(int64_t)bytes}, in.q.options().dtype(at::kByte));
     check(sna_attention_forward(&a, dtype, bytes ? workspace.data_ptr() : nullptr, bytes, stream_of(in.q)));
-    return {out, lse};
+    return {out, lse, rest};
 }
 
 class WeightedAttention : public torch::autograd::Function<WeightedAttention> {
 public:
     static variable_list forward(AutogradContext* ctx, at::Tensor q, at::Tensor k, at::Tensor v, std::optional<at::Tensor> log_weights, double scale) {
         AttentionInputs in{q, k, v, or_undefined(log_weights), scale};
-        auto [out, lse] = attention_forward(in);
-        ctx->save_for_backward({in.q, in.k, in.v, in.log_weights, out, lse});
+        auto [out, lse, rest] = attention_forward(in, true);
+        ctx->save_for_backward({in.q, in.k, in.v, in.log_weights, out, lse, rest});
         ctx->saved_data["scale"] = scale;
         ctx->mark_non_differentiable({lse});
         return {out, lse};
@@ -286,19 +291,21 @@ public:
         // (what hooks on saved tensors return is checked like arguments)
         check_attention(in);
         const at::Tensor& lse = saved[5];
-        check_like(saved[4], "out", in.q, "q");
-        TORCH_CHECK_VALUE(saved[4].sizes() == in.q.sizes(), "out has shape ", saved[4].sizes(), ", expected ", in.q.sizes());
+        for (int i : {4, 6}) {
+            check_like(saved[i], "out", in.q, "q");
+            TORCH_CHECK_VALUE(saved[i].sizes() == in.q.sizes(), "out has shape ", saved[i].sizes(), ", expected ", in.q.sizes());
+        }
         TORCH_CHECK_VALUE(grads[0].sizes() == in.q.sizes() && grads[0].device() == in.q.device(), "the gradient has shape ", grads[0].sizes(), ", expected ", in.q.sizes());
         check_cuda(lse, "lse", in.q, "q");
         TORCH_CHECK_VALUE(lse.scalar_type() == at::kFloat && lse.sizes() == in.q.sizes().slice(0, 4) && lse.is_contiguous(), "lse must be float32 and contiguous, of shape ",
                           in.q.sizes().slice(0, 4));
         const c10::cuda::CUDAGuard guard(in.q.device());
         for (at::Tensor* t : {&in.q, &in.k, &in.v}) *t = attendable(*t);
-        const at::Tensor out = attendable(saved[4]), dout = attendable(grads[0].to(in.q.scalar_type()));
+        const at::Tensor out = attendable(saved[4]), rest = attendable(saved[6]), dout = attendable(grads[0].to(in.q.scalar_type()));
         at::Tensor dq = attention_result_like(in.q), dk = attention_result_like(in.k), dv = attention_result_like(in.v);
         const sna_dtype_t dtype = dtype_of(in.q, "q");
         sna_attention_t a = described(in);
-        a.out = described(out); a.dout = described(dout);
+        a.out = described(out); a.out_rest = described(rest); a.dout = described(dout);
         a.dq = described(dq); a.dk = described(dk); a.dv = described(dv);
         a.lse = const_cast<float*>(lse.const_data_ptr<float>());
         const size_t bytes = sna_attention_backward_workspace_bytes(&a, dtype);
@@ -316,7 +323,8 @@ std::tuple<at::Tensor, at::Tensor> weighted_attention(const at::Tensor& q, const
         const variable_list r = WeightedAttention::apply(q, k, v, log_weights, scale);
         return {r[0], r[1]};
     }
-    return attention_forward(in);
+    auto [out, lse, rest] = attention_forward(in, false);
+    return {out, lse};
 }
 
 // ---- dropout --------------------------------------------------------------------------------------------------------------

@@ -69,9 +69,9 @@ def weighted_attention(q, k, v, log_weights=None, scale: float | None = None, re
     q [B, Hq, nlat, nlon, C], k and v [B, Hk, nlat', nlon', C], bfloat16 or float16, C a multiple of 8 up to 128, Hq a multiple of Hk:
     query head h reads key head h // (Hq // Hk).  ``log_weights``: float32, [nlat' * nlon'] or one such row per batch; with the logarithms of
     quadrature weights (:func:`log_quadrature_weights`) this is global spherical attention.  A point at -1e30 or below (-inf, the lowest number of any
-    type) is left out, whatever k and v hold there; a row without points gives zeros, and no gradient.  ``scale``: 1 / sqrt(C) if None.
+    type) is left out, whatever k and v hold there (others must be below 1e30); a row without points gives zeros, and no gradient.  ``scale``: 1 / sqrt(C) if None.
     Returns out, or with ``return_lse`` (out, lse): the logarithm of each row's sum, float32 [B, Hq, nlat, nlon], not differentiable.
-    Differentiable in q, k and v: the backward pass keeps out and lse and recomputes the probabilities."""
+    Differentiable in q, k and v: what is kept for the backward pass is lse, and out with what its rounding took; the probabilities are recomputed."""
     _check_plain(q, k, v, log_weights)
     if scale is None:
         scale = q.shape[-1] ** -0.5 if q.dim() and q.shape[-1] else 1.0

@@ -56,7 +56,7 @@ class SnaTensor(ctypes.Structure):
 class SnaAttention(ctypes.Structure):
     """sna_attention_t: a problem of sna_attention_forward / _backward."""
     _fields_ = ([(n, _i) for n in ("B", "Hq", "Hk", "C", "nlat_q", "nlon_q", "nlat_k", "nlon_k")]
-                + [(n, SnaTensor) for n in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")]
+                + [(n, SnaTensor) for n in ("q", "k", "v", "out", "out_rest", "dout", "dq", "dk", "dv")]
                 + [("lse", _vp), ("log_weights", _vp), ("log_weights_batch", _i64), ("scale", _f)])
 
 

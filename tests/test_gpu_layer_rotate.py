@@ -117,6 +117,45 @@ def definition_transposed_size(g, rotation, interleaved):
     return size
 
 
+@pytest.mark.parametrize("B, H, grid, C, dtype", [(1, 3, (64, 128), 32, torch.float32), (1, 1, (91, 181), 8, torch.bfloat16), (3, 7, (45, 90), 64, torch.float16),
+                                                  (5, 5, (7, 9), 128, torch.bfloat16), (1, 17, (30, 61), 16, torch.float32), (3, 1, (180, 361), 24, torch.float32)])
+def test_gradients_of_the_weights_closely(B, H, grid, C, dtype):
+    """Odd numbers of slices, several points per thread.  A sum passes a thread's vectors (at most 64 here), up to 256 threads of a block, and up to 10 + 7 partial
+    sums: no more than 400 roundings to 32 bits, of which each is of a part of the sum of the terms' magnitudes."""
+    torch.manual_seed(C)
+    q, k = heads(B, H, *grid, C, dtype), heads(B, 1, *grid, C, dtype)
+    weights = [torch.randn(C, device="cuda").requires_grad_() for _ in range(2)]
+    rotation = tables(*grid, C // 4, C // 4)
+    out = layer.qk_norm_rotate(q, k, *weights, rotation, rotation)
+    grads_out = [torch.randn(o.shape, device="cuda").to(dtype) for o in out]
+    got = torch.autograd.grad(out, weights, grads_out)
+    for x, weight, g, dw in zip((q, k), weights, grads_out, got):
+        w = weight.detach().double().requires_grad_()
+        ref = torch.autograd.grad(definition(x, w, rotation, 1e-6, False)[0], w, g.double())[0]
+        n = x.double().abs() / (x.double().square().mean(-1, keepdim=True) + 1e-6).sqrt()
+        near(dw, ref, (definition_transposed_size(g.double(), rotation, False) * n).sum((0, 1, 2, 3)), C + 416, torch.float32, "dw")
+
+
+def test_results_in_place_of_inputs():
+    """Through the C ABI: y is x, and dx is dy."""
+    torch.manual_seed(11)
+    x, w = heads(2, 3, 5, 7, 24, torch.bfloat16), torch.randn(24, device="cuda")
+    rotation = tables(5, 7, 5, 6)
+    xr = x.clone().requires_grad_()
+    y = layer.qk_norm_rotate(xr, xr.detach(), w, w, rotation, rotation, eps=0.5)[0]
+    g = heads(2, 3, 5, 7, 24, torch.bfloat16)
+    dx = torch.autograd.grad(y, xr, g)[0]
+    t = lambda a: sna.SnaTensor(a.data_ptr(), a.stride(0), a.stride(1), a.stride(2), a.stride(3))
+    stream = torch.cuda.current_stream().cuda_stream
+    a, b = x.clone(), g.clone()
+    part = sna.SnaRotate(nlat=5, nlon=7, H=3, x=t(a), y=t(a), weight=w.data_ptr(), lat_table=rotation[0].data_ptr(), lon_table=rotation[1].data_ptr(), pairs_lat=5, pairs_lon=6)
+    assert sna._lib.sna_norm_rotate_forward(part, 1, sna.SNA_BFLOAT16, 2, 24, 0.5, 0, stream) == 0
+    assert torch.equal(a, y)
+    part.x, part.dy, part.dx = t(x), t(b), t(b)
+    assert sna._lib.sna_norm_rotate_backward(part, 1, sna.SNA_BFLOAT16, 2, 24, 0.5, 0, None, 0, stream) == 0
+    assert torch.equal(b, dx)
+
+
 def test_gradient_against_differences():
     torch.manual_seed(3)
     q, k = (torch.randn(1, 2, 3, 4, 8, device="cuda") for _ in range(2))
