@@ -53,9 +53,13 @@ sna_status_t check_workspace(const void* workspace, size_t bytes, size_t need) {
     return SNA_OK;
 }
 
-// The tcgen05 kernels take tiles of 128 (forward: two of them) rows and blocks of 128 points.  They find a row's maximum before the scores are scaled, and
-// hold weights divided by the scale: it has to be positive, and not so small that a point left out could be taken for one with a low weight.
-bool on_tensor_memory(const Problem& p) { return p.Nq > 64 && p.Nk >= 128 && p.scale >= 0x1p-20f && p.scale <= 0x1p20f; }
+// Which kernels: those on tcgen05 unless there are few queries (whose tiles of 128 and 256 rows per head would be nearly empty, while the mma.sync kernels stack
+// the heads of a group) or few points.  us, mma.sync : tcgen05, bf16, C = 64, forward and (in brackets) with the backward pass: 32 heads, 32 x 1024
+// 15.8 : 12.1 (56 : 41), 17 x 8192 41.8 : 27.0 (280 : 148), 65 x 128 7.7 : 6.9 (27 : 26); 128 heads, 512 x 64 20 : 16 (77 : 61), 128 x 64 7.5 : 7.9 (28 : 27);
+// 4 heads, 64 x 8192 14.6 : 20.2 (193 : 57).
+// The tcgen05 kernels find a row's maximum before the scores are scaled, and hold weights divided by the scale: it has to be positive, and not so small that
+// a point left out could be taken for one with a low weight.
+bool on_tensor_memory(const Problem& p) { return p.Nq > 16 && p.Nk >= 64 && p.scale >= 0x1p-20f && p.scale <= 0x1p20f; }
 // What the forward pass needs to hold partial results, on either path (the tcgen05 kernels fall back where the driver refuses a tensor).
 size_t forward_bytes(const Problem& p, int sms) {
     const int splits = forward_splits(p, sms);

@@ -6,8 +6,9 @@
 //   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij dout_i
 //
 // These are the kernels for any size, on mma.sync (m16n8k16): a warp owns 16 rows, scores stay in registers and become the next product's
-// operand there.  Products are accumulated in 32 bits, the softmax and all statistics are in 32 bits; p and ds are rounded to the tensors'
-// type as operands of the second products (to nearest, so that the roundings of a sum's terms cancel on average).
+// operand there.  Products are accumulated in 32 bits, the softmax and all statistics are in 32 bits.  p and ds are operands of
+// the second products in two 16-bit parts, except for few rows in the forward pass, where p is rounded once, to nearest, so that the roundings of a
+// sum's terms cancel on average (one station over 361x720: 55 us with two parts, 51 with one).
 //
 // A key head serves G query heads: their rows are stacked, so that the head's keys are read once for all of them, and so that its
 // gradients are summed within one block.  Few rows: a tile of 16 rows, the block's four warps sharing each 64 keys, and the keys split
@@ -58,6 +59,20 @@ template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi)
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
+}
+
+// The A operand of a second product from 16 x 16 numbers in a product's layout (two 16 x 8 accumulators), rounded to 16 bits, and what rounding leaves: with
+// both, p and ds count with twice the digits.  These kernels take the small problems, whose time is not the tensor cores'; the tcgen05 kernels round once.
+template <typename T>
+__device__ __forceinline__ void operands(const float (&x)[4], const float (&y)[4], uint32_t (&hi)[4], uint32_t (&lo)[4]) {
+    const float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        hi[i] = pack<T>(v[2 * i], v[2 * i + 1]);
+        float a, b;
+        unpack2(pair_of<T>(hi[i]), a, b);
+        lo[i] = pack<T>(v[2 * i] - a, v[2 * i + 1] - b);
+    }
 }
 
 // A tile in shared memory: rows of CP 16-bit channels in pieces of 16 bytes, which are permuted within a row so that the eight rows of an
@@ -248,12 +263,16 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
             }
 #pragma unroll
         for (int ks = 0; ks < KW / 16; ++ks) {
-            const uint32_t a[4] = {pack<T>(s[2 * ks][0], s[2 * ks][1]), pack<T>(s[2 * ks][2], s[2 * ks][3]), pack<T>(s[2 * ks + 1][0], s[2 * ks + 1][1]),
-                                   pack<T>(s[2 * ks + 1][2], s[2 * ks + 1][3])};
+            uint32_t a[4], a_lo[4];
+            operands<T>(s[2 * ks], s[2 * ks + 1], a, a_lo);
 #pragma unroll
             for (int n = 0; n < CN; n += 2) {
                 uint32_t vb[4];
                 load_bt<CP>(vb, tv, key0 + ks * 16, n / 2, lane);
+                if (WM != 1) {
+                    mma<T>(o[n], a_lo, vb[0], vb[1]);
+                    mma<T>(o[n + 1], a_lo, vb[2], vb[3]);
+                }
                 mma<T>(o[n], a, vb[0], vb[1]);
                 mma<T>(o[n + 1], a, vb[2], vb[3]);
             }
@@ -579,12 +598,14 @@ __global__ void __launch_bounds__(THREADS) attend_dq_kernel(const __grid_constan
         }
 #pragma unroll
         for (int ks = 0; ks < BN / 16; ++ks) {
-            const uint32_t a[4] = {pack<T>(s[2 * ks][0], s[2 * ks][1]), pack<T>(s[2 * ks][2], s[2 * ks][3]), pack<T>(s[2 * ks + 1][0], s[2 * ks + 1][1]),
-                                   pack<T>(s[2 * ks + 1][2], s[2 * ks + 1][3])};
+            uint32_t a[4], a_lo[4];
+            operands<T>(s[2 * ks], s[2 * ks + 1], a, a_lo);
 #pragma unroll
             for (int n = 0; n < CN; n += 2) {
                 uint32_t kb[4];
                 load_bt<CP>(kb, tk, ks * 16, n / 2, lane);
+                mma<T>(dq[n], a_lo, kb[0], kb[1]);
+                mma<T>(dq[n + 1], a_lo, kb[2], kb[3]);
                 mma<T>(dq[n], a, kb[0], kb[1]);
                 mma<T>(dq[n + 1], a, kb[2], kb[3]);
             }
@@ -694,17 +715,21 @@ __global__ void __launch_bounds__(THREADS) attend_dkdv_kernel(const __grid_const
         }
 #pragma unroll
         for (int ks = 0; ks < QB / 16; ++ks) {
-            const uint32_t a[4] = {pack<T>(s[2 * ks][0], s[2 * ks][1]), pack<T>(s[2 * ks][2], s[2 * ks][3]), pack<T>(s[2 * ks + 1][0], s[2 * ks + 1][1]),
-                                   pack<T>(s[2 * ks + 1][2], s[2 * ks + 1][3])};
-            const uint32_t d[4] = {pack<T>(t[2 * ks][0], t[2 * ks][1]), pack<T>(t[2 * ks][2], t[2 * ks][3]), pack<T>(t[2 * ks + 1][0], t[2 * ks + 1][1]),
-                                   pack<T>(t[2 * ks + 1][2], t[2 * ks + 1][3])};
+            uint32_t a[4], a_lo[4];
+            operands<T>(s[2 * ks], s[2 * ks + 1], a, a_lo);
+            uint32_t d[4], d_lo[4];
+            operands<T>(t[2 * ks], t[2 * ks + 1], d, d_lo);
 #pragma unroll
             for (int n = 0; n < CN; n += 2) {
                 uint32_t yb[4], qb[4];
                 load_bt<CP>(yb, ty, ks * 16, n / 2, lane);
+                mma<T>(dv[n], a_lo, yb[0], yb[1]);
+                mma<T>(dv[n + 1], a_lo, yb[2], yb[3]);
                 mma<T>(dv[n], a, yb[0], yb[1]);
                 mma<T>(dv[n + 1], a, yb[2], yb[3]);
                 load_bt<CP>(qb, tq, ks * 16, n / 2, lane);
+                mma<T>(dk[n], d_lo, qb[0], qb[1]);
+                mma<T>(dk[n + 1], d_lo, qb[2], qb[3]);
                 mma<T>(dk[n], d, qb[0], qb[1]);
                 mma<T>(dk[n + 1], d, qb[2], qb[3]);
             }
