@@ -69,7 +69,7 @@ size_t forward_bytes(const Problem& p, int sms) {
 
 struct BackwardWorkspace {
     Stats stats;
-    float* partials;
+    float *dq_partials, *dkdv_partials;
     size_t bytes;
 };
 BackwardWorkspace backward_workspace(const Problem& p, void* workspace, int sms) {
@@ -86,8 +86,8 @@ BackwardWorkspace backward_workspace(const Problem& p, void* workspace, int sms)
     w.stats.lse2 = reinterpret_cast<float*>(take((size_t)rows_of(p) * sizeof(float)));
     w.stats.D = reinterpret_cast<float*>(take((size_t)rows_of(p) * sizeof(float)));
     w.stats.norms = reinterpret_cast<uint32_t*>(take((size_t)p.B * p.Hk * 2 * sizeof(uint32_t)));
-    // (one after the other on the stream: dq's are joined before dk's and dv's are written)
-    w.partials = reinterpret_cast<float*>(take(on_tensor_memory(p) ? sizeof(float) * std::max(partial_floats(p, Kernel::DQ, sms), partial_floats(p, Kernel::DKDV, sms)) : 0));
+    w.dq_partials = reinterpret_cast<float*>(take(on_tensor_memory(p) ? sizeof(float) * partial_floats(p, Kernel::DQ, sms) : 0));
+    w.dkdv_partials = reinterpret_cast<float*>(take(on_tensor_memory(p) ? sizeof(float) * partial_floats(p, Kernel::DKDV, sms) : 0));
     return w;
 }
 
@@ -148,9 +148,14 @@ sna_status_t sna_attention_backward(const sna_attention_t* a, sna_dtype_t dtype,
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     const Stats& s = w.stats;
     cudaError_t e = launch_statistics(p, s, dtype, stream);
-    const bool on_tc = on_tensor_memory(p);
-    if (e == cudaSuccess && queries && (!on_tc || !backward_dq_tc(p, s, dtype, sms, w.partials, stream, e))) e = launch_backward_dq(p, s, dtype, stream);
-    if (e == cudaSuccess && keys && (!on_tc || !backward_dkdv_tc(p, s, dtype, sms, w.partials, stream, e))) e = launch_backward_dkdv(p, s, dtype, stream);
+    // (on_tensor_memory: there are queries and keys)
+    if (e == cudaSuccess && on_tensor_memory(p) && backward_dq_tc(p, s, dtype, sms, w.dq_partials, stream, e)) {
+        if (e == cudaSuccess && !backward_dkdv_tc(p, s, dtype, sms, w.dkdv_partials, stream, e)) e = cudaErrorInvalidValue;      // (the same tensors, in other boxes)
+        if (e == cudaSuccess) e = join_backward(p, dtype, sms, w.dq_partials, w.dkdv_partials, stream);
+    } else {
+        if (e == cudaSuccess && queries) e = launch_backward_dq(p, s, dtype, stream);
+        if (e == cudaSuccess && keys) e = launch_backward_dkdv(p, s, dtype, stream);
+    }
     if (e != cudaSuccess) return sna::fail(SNA_ERR_CUDA, "attention backward launch: %s", cudaGetErrorString(e));
     return SNA_OK;
 }

@@ -48,8 +48,7 @@ struct Split {
     __host__ __device__ int64_t rest() const { return tiles - full; }
 };
 // The whole waves stay whole.  The last, partial wave is cut so that its pieces end early: R tiles in k pieces take ceil(R k / SMs) / k of a wave (256 tiles on 148
-// SMs: 1.75 waves with four pieces each instead of 2).  Not for many waves, which gain little, nor into pieces of fewer than `least` streamed blocks.
-Split split_tiles(int64_t tiles, int64_t streamed, int64_t least, int sms);
+// SMs: 1.75 waves with four pieces each instead of 2).  Not for many waves, which gain little, nor into pieces of a few streamed blocks.
 __host__ __device__ inline int64_t query_blocks_of(const Problem& p) { return (int64_t)p.B * p.Hq * ((p.Nq + STATS_BLOCK - 1) / STATS_BLOCK); }
 
 // Powers of two that keep float16 operands of the second products away from the numbers that its exponent has no room for: softmax
@@ -90,6 +89,7 @@ size_t partial_floats(const Problem& p, Kernel kernel, int sms);
 bool forward_tc(const Problem& p, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
 bool backward_dq_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
 bool backward_dkdv_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
+cudaError_t join_backward(const Problem& p, sna_dtype_t dtype, int sms, const float* dq_partials, const float* dkdv_partials, cudaStream_t stream);
 cudaError_t read_status(int* status);
 
 // mma.sync kernels (sna_kernels_attend.cu)

@@ -153,6 +153,7 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(16) float bias[4][BN];
     const uint32_t tq = s32(smem), tkv = tq + BM * CP * 2;      // stages of (K, V)
+    allow_dependents();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wm = warp % WM, wk = warp / WM;
     const int split = blockIdx.x % splits, rest = blockIdx.x / splits, tile = rest % tiles, bh = rest / tiles;
     const int b = bh / p.Hk, hk = bh - b * p.Hk;
@@ -373,6 +374,7 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) attend_join_kernel(const __gr
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t rows = rows_of(p), at = BLOCK_PER_ROW ? blockIdx.x : (int64_t)blockIdx.x * JOIN_WARPS + warp;
     if (at >= rows) return;         // (whole warps; whole blocks where they meet)
+    wait_for_previous();
     const float* statistics = partials + splits * rows * p.C;
     float top = -INFINITY;
     for (int s = lane; s < splits; s += 32) top = fmaxf(top, statistics[s * rows + at]);
@@ -423,6 +425,7 @@ template <typename T>
 __global__ void __launch_bounds__(256) attend_statistics_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats s, int64_t query_blocks, int64_t weight_blocks) {
     constexpr bool SCALED = SHIFT<T> != 0.f;
     __shared__ uint32_t most;
+    allow_dependents();
     const int part = threadIdx.x & 3, place = threadIdx.x >> 2;
     if (blockIdx.x < weight_blocks) {
         // one thread per point: its weight in parts, and who is left out
@@ -808,12 +811,9 @@ cudaError_t launch_join(const Problem& p, sna_dtype_t dtype, int splits, const f
     const unsigned blocks = (unsigned)(block_per_row ? rows : (rows + JOIN_WARPS - 1) / JOIN_WARPS);
     auto run = [&](auto t) {
         using T = decltype(t);
-        if (block_per_row) attend_join_kernel<T, true><<<blocks, 32 * JOIN_WARPS, 0, stream>>>(p, splits, partials);
-        else attend_join_kernel<T, false><<<blocks, 32 * JOIN_WARPS, 0, stream>>>(p, splits, partials);
+        return launch_dependent(block_per_row ? attend_join_kernel<T, true> : attend_join_kernel<T, false>, blocks, 32 * JOIN_WARPS, 0, stream, p, splits, partials);
     };
-    if (dtype == SNA_BFLOAT16) run(__nv_bfloat16());
-    else run(__half());
-    return cudaGetLastError();
+    return dtype == SNA_BFLOAT16 ? run(__nv_bfloat16()) : run(__half());
 }
 
 cudaError_t launch_forward(const Problem& p, sna_dtype_t dtype, int splits, float* partials, cudaStream_t stream) {

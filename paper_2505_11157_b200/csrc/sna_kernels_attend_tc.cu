@@ -102,6 +102,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1)
 attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                          const __grid_constant__ CUtensorMap map_v, int tiles, const __grid_constant__ Split cut, float* partials) {
     using F = Forward<D>;
+    allow_dependents();
     extern __shared__ unsigned char raw[];
     unsigned char* base = (unsigned char*)(((uintptr_t)raw + 1023) & ~(uintptr_t)1023);
     __shared__ unsigned long long bars[F::COUNT];
@@ -453,7 +454,6 @@ __global__ void __launch_bounds__(BWD_THREADS, 1)
 attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats stats, const __grid_constant__ CUtensorMap map_a1, const __grid_constant__ CUtensorMap map_a2,
                           const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_b2, int tiles, const __grid_constant__ Split cut, float* partials) {
     using K = Backward<D, DKDV>;
-    constexpr bool CLEARED = !DKDV && WEIGHTS;          // streamed points may be left out
     constexpr bool EXTRA = DKDV || WEIGHTS;
     static_assert(BLOCK == STATS_BLOCK, "the statistics kernel's blocks");
     extern __shared__ unsigned char raw[];
@@ -471,6 +471,12 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     const int begin = (int)((int64_t)total * piece.part / piece.parts), count = (int)((int64_t)total * (piece.part + 1) / piece.parts) - begin;
     const int steps = (p.C + 15) / 16, slabs = (p.C + 63) / 64;
     const float* weights = p.log_weights == nullptr ? nullptr : p.log_weights + b * p.log_weights_batch;
+    // The order on the stream is statistics, dq, dk and dv, joins.  dk and dv need nothing of dq: their blocks fill the SMs that its last blocks leave idle, and wait
+    // for them at their end alone; by the time that they may start, every block of dq has seen the statistics complete.
+    if (!DKDV) {
+        wait_for_previous();
+        allow_dependents();
+    }
     // Whether points are left out.  dq: only then do the streamed blocks pass through the warp that clears rows.  Either side all of whose points are left out
     // gets zeros at once.
     const int64_t weight_row = p.log_weights_batch == 0 ? 0 : b;
@@ -506,6 +512,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                     }
                 }
             }
+            if (DKDV) wait_for_previous();
             return;
         }
     }
@@ -773,6 +780,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     __syncthreads();
     if (fail_s && tid == 0) atomicExch(&g_status, 1);
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "r"(512));
+    if (DKDV) wait_for_previous();
 }
 
 // ---- joins of tiles in pieces ---------------------------------------------------------------------------------------------------
@@ -786,6 +794,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const _
     const int64_t rest = cut.rest() * rows_per_tile, index = (int64_t)blockIdx.x * JOIN_THREADS + threadIdx.x, local = index / chunks;
     const int c = (int)(index - local * chunks) * 8;
     if (local >= rest) return;
+    wait_for_previous();
     const int64_t tile = cut.full + local / rows_per_tile, bh = tile / tiles, b = bh / H, h = bh - b * H;
     const int n = (int)(tile - bh * tiles) * rows_per_tile + (int)(local % rows_per_tile);
     if (n >= N) return;
@@ -819,8 +828,8 @@ __global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const _
 template <typename T, bool SOFTMAX>
 cudaError_t join_tiles(const View& out, const View& rest_out, float* lse, const Split& cut, int tiles, int rows_per_tile, int N, int H, int C, const float* partials, cudaStream_t stream) {
     const int64_t threads = cut.rest() * rows_per_tile * (C / 8);
-    attend_join_tiles_kernel<T, SOFTMAX><<<(unsigned)((threads + JOIN_THREADS - 1) / JOIN_THREADS), JOIN_THREADS, 0, stream>>>(out, rest_out, lse, cut, tiles, rows_per_tile, N, H, C, partials);
-    return cudaGetLastError();
+    return launch_dependent(attend_join_tiles_kernel<T, SOFTMAX>, (unsigned)((threads + JOIN_THREADS - 1) / JOIN_THREADS), JOIN_THREADS, 0, stream, out, rest_out, lse, cut, tiles,
+                            rows_per_tile, N, H, C, partials);
 }
 
 using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
@@ -863,17 +872,12 @@ cudaError_t forward_as(const Problem& p, const CUtensorMap (&maps)[3], const Spl
 
 template <typename T, int D, bool DKDV, bool WEIGHTS>
 cudaError_t backward_as(const Problem& p, const Stats& s, const CUtensorMap (&maps)[4], const Split& cut, float* partials, cudaStream_t stream) {
-    const int N = DKDV ? p.Nk : p.Nq, H = DKDV ? p.Hk : p.Hq, tiles = (N + TILE - 1) / TILE;
+    const int tiles = ((DKDV ? p.Nk : p.Nq) + TILE - 1) / TILE;
     const auto kernel = attend_backward_tc_kernel<T, D, DKDV, WEIGHTS>;
     static std::atomic<uint64_t> allowed{0};
     cudaError_t e = allow(kernel, Backward<D, DKDV>::SMEM, allowed);
     if (e != cudaSuccess) return e;
-    kernel<<<(unsigned)cut.blocks(), BWD_THREADS, Backward<D, DKDV>::SMEM, stream>>>(p, s, maps[0], maps[1], maps[2], maps[3], tiles, cut, partials);
-    e = cudaGetLastError();
-    if (e != cudaSuccess || cut.rest() == 0) return e;
-    e = join_tiles<T, false>(DKDV ? p.dk : p.dq, View{}, nullptr, cut, tiles, TILE, N, H, p.C, partials, stream);
-    if (e == cudaSuccess && DKDV) e = join_tiles<T, false>(p.dv, View{}, nullptr, cut, tiles, TILE, N, H, p.C, partials + cut.parts * cut.rest() * TILE * p.C, stream);
-    return e;
+    return launch_dependent(kernel, (unsigned)cut.blocks(), BWD_THREADS, Backward<D, DKDV>::SMEM, stream, p, s, maps[0], maps[1], maps[2], maps[3], tiles, cut, partials);
 }
 template <bool DKDV>
 bool backward_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
@@ -905,24 +909,44 @@ bool backward_dkdv_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int s
     return backward_tc<true>(p, s, dtype, sms, partials, stream, e);
 }
 
-Split split_tiles(int64_t tiles, int64_t streamed, int64_t least, int sms) {
-    const int64_t rest = tiles % sms;
-    Split cut{tiles, tiles, 1};
-    if (rest == 0 || tiles >= 8 * (int64_t)sms) return cut;
-    double best = 0.97;        // of the partial wave; less than a tenth of a wave is not worth a second kernel, nor is a finer cut for a hundredth
+// Pieces of each of `rest` tiles, where the SMs have a partial wave of them (see Split).
+static int pieces(int64_t rest, int64_t streamed, int64_t least, int sms) {
+    double best = 0.97;        // of the partial wave: what gains less is not worth a second kernel, nor is a finer cut for a hundredth
+    int parts = 1;
     const int64_t most = std::min(streamed / least, std::max<int64_t>(8, sms / rest));        // (few tiles: one piece per SM)
     for (int64_t k = 2; k <= most; ++k) {
         const double wave = (double)((rest * k + sms - 1) / sms) / (double)k + 0.01 * (double)(k < 8 ? k : 8);
-        if (wave < best) { best = wave; cut = Split{tiles, tiles - rest, (int)k}; }
+        if (wave < best) { best = wave; parts = (int)k; }
     }
-    return cut;
+    return parts;
 }
 
 Split split_of(const Problem& p, Kernel kernel, int sms) {
     auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
-    if (kernel == Kernel::FORWARD) return split_tiles((int64_t)p.B * p.Hq * up(p.Nq, 2 * TILE), up(p.Nk, TILE), 2, sms);
-    if (kernel == Kernel::DQ) return split_tiles((int64_t)p.B * p.Hq * up(p.Nq, TILE), up(p.Nk, BLOCK), 4, sms);
-    return split_tiles((int64_t)p.B * p.Hk * up(p.Nk, TILE), p.G * up(p.Nq, BLOCK), 4, sms);
+    const int64_t forward = (int64_t)p.B * p.Hq * up(p.Nq, 2 * TILE), dq = (int64_t)p.B * p.Hq * up(p.Nq, TILE), dkdv = (int64_t)p.B * p.Hk * up(p.Nk, TILE);
+    const int64_t keys = up(p.Nk, BLOCK), queries = p.G * up(p.Nq, BLOCK);
+    // dq's and dk/dv's blocks run side by side, so theirs is one last wave, dk's and dv's; dq is cut only if both together are less than a wave
+    const int64_t tiles = kernel == Kernel::FORWARD ? forward : kernel == Kernel::DQ ? dq : dkdv, all = kernel == Kernel::FORWARD ? forward : dq + dkdv;
+    const int64_t rest = std::min(all % sms, tiles);
+    Split cut{tiles, tiles, 1};
+    if (rest == 0 || all >= 8 * (int64_t)sms || (kernel == Kernel::DQ && all >= sms)) return cut;
+    const int parts = kernel == Kernel::FORWARD ? pieces(rest, up(p.Nk, TILE), 2, sms) : pieces(all < sms ? all : rest, all < sms ? std::min(keys, queries) : queries, 4, sms);
+    if (parts > 1) cut = Split{tiles, tiles - rest, parts};
+    return cut;
+}
+
+cudaError_t join_backward(const Problem& p, sna_dtype_t dtype, int sms, const float* dq_partials, const float* dkdv_partials, cudaStream_t stream) {
+    const Split q = split_of(p, Kernel::DQ, sms), k = split_of(p, Kernel::DKDV, sms);
+    const int q_tiles = (p.Nq + TILE - 1) / TILE, k_tiles = (p.Nk + TILE - 1) / TILE;
+    auto run = [&](auto t) {
+        using T = decltype(t);
+        cudaError_t e = cudaSuccess;
+        if (q.parts > 1) e = join_tiles<T, false>(p.dq, View{}, nullptr, q, q_tiles, TILE, p.Nq, p.Hq, p.C, dq_partials, stream);
+        if (e == cudaSuccess && k.parts > 1) e = join_tiles<T, false>(p.dk, View{}, nullptr, k, k_tiles, TILE, p.Nk, p.Hk, p.C, dkdv_partials, stream);
+        if (e == cudaSuccess && k.parts > 1) e = join_tiles<T, false>(p.dv, View{}, nullptr, k, k_tiles, TILE, p.Nk, p.Hk, p.C, dkdv_partials + k.parts * k.rest() * TILE * p.C, stream);
+        return e;
+    };
+    return dtype == SNA_BFLOAT16 ? run(__nv_bfloat16()) : run(__half());
 }
 
 size_t partial_floats(const Problem& p, Kernel kernel, int sms) {

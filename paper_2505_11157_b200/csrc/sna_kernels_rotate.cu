@@ -65,6 +65,7 @@ __global__ void __launch_bounds__(ROTATE_THREADS, BACKWARD ? 3 : 4) norm_rotate_
     constexpr int VP = V / 2, U = 2;        // pairs per lane; vectors of a group under way
     // (the last sum over threads needs room for a block's partial dw, the exchange for a block's vectors)
     __shared__ __align__(16) float shared[BACKWARD || PAIRS == Pairs::BY_SHARED ? ROTATE_THREADS * V : 4];
+    if (BACKWARD) allow_dependents();
     const int which = (int)blockIdx.x >= a.first_blocks;
     const Part& p = a.part[which];
     const int block = (int)blockIdx.x - (which ? a.first_blocks : 0);
@@ -240,6 +241,7 @@ __global__ void __launch_bounds__(1024) sum_partials_kernel(const __grid_constan
     if (a.dweight[which] == nullptr) return;
     const float* from = a.partials[which] + c;
     float sum = 0.f;
+    wait_for_previous();
     if (c < a.C)
 #pragma unroll 4
         for (int r = threadIdx.y; r < rows; r += 128) sum += from[(int64_t)r * a.C];
@@ -365,8 +367,7 @@ sna_status_t norm_rotate(const sna_rotate_t* parts, int n_parts, sna_dtype_t dty
             : dtype == SNA_BFLOAT16 ? launch_width<__nv_bfloat16>(a, V, pairs, backward, total, stream)
                                     : launch_width<__half>(a, V, pairs, backward, total, stream);
     if (e == cudaSuccess && sums) {
-        sum_partials_kernel<<<dim3((C + 7) / 8, n_parts), dim3(8, 128), 0, stream>>>(sum);
-        e = cudaGetLastError();
+        e = launch_dependent(sum_partials_kernel, dim3((C + 7) / 8, n_parts), dim3(8, 128), 0, stream, sum);
     }
     if (e != cudaSuccess) return fail(SNA_ERR_CUDA, "norm and rotation launch: %s", cudaGetErrorString(e));
     return SNA_OK;
