@@ -51,10 +51,12 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
 //   warp 10      weights of the next block's points; zeroes k and v rows of points left out
 //   warps 0-3 and 4-7  softmax of tile 0 and 1, thread = row: S from TMEM, P back.  The row's reference moves (and O is scaled in TMEM)
 //                only when its maximum has grown by 2^8: then the sums are still far from overflow, and most blocks skip the correction.
-// Narrow heads leave TMEM columns for P beside S: S of the next block is then computed during this block's softmax.  (Tried and not kept, 64x128, B = 2, four
-// heads of 32, 193 us: the two tiles taking turns with their exponentials 225; four groups with half a row per thread, whose scores do not fit their
-// 104 registers, 240.)  Wide ones keep P
+// Narrow heads leave TMEM columns for P beside S: S of the next block is then computed during this block's softmax.  Wide ones keep P
 // in S's columns; while one tile's products run, the other tile's softmax does.
+// What bounds them: latencies.  Eight softmax warps keep the special-function unit 57 %, the tensor pipe 43 % and the issue slots 54 % busy (heads of 64); with heads of
+// 128 it is the chain of a tile's softmax and products, 3200 cycles per block and pair of tiles, of which the tensor pipe works 2200.  Tried and not kept (64x128, B = 2,
+// four heads of 32, 193 us): the two tiles taking turns with their exponentials 225; four groups with half a row per thread, whose scores do not fit
+// their 104 registers, 240; the next block's scores loaded and their maxima found between this block's exponentials 213.
 // A point's weight is one more step of the first product: its parts against ones.  (Added per element, with the weights read from shared memory, it
 // cost 40 % of the time: 64x128, B = 2, eight heads of 128, 683 us against 486 without weights.)
 constexpr int FWD_THREADS = 384;
@@ -91,10 +93,7 @@ __device__ __forceinline__ void store8(T* out, T* rest, const float (&y)[8]) {
 template <typename T> constexpr float FORWARD_SHIFT = 0.f;
 template <> constexpr float FORWARD_SHIFT<__half> = 7.f;
 constexpr float GROWTH = 8.f;
-#ifndef V0
-#define V0 4
-#endif
-constexpr int BY_FMA = V0;               // one pair of this many takes its exponentials on the FMA pipe
+constexpr int BY_FMA = 4;               // one pair of this many takes its exponentials on the FMA pipe (us in the case above: none 204, 1 in 3 196, 1 in 4 194, 1 in 2 213)
 constexpr float NOTHING = -1e31f;       // scores below belong to points left out
 
 template <typename T, int D, bool WEIGHTS>
@@ -424,11 +423,6 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
 // Blocks of 64 points need two buffers of S and T to keep both sides busy: 256 of the 512 columns.  An MMA of 64 columns that reads its
 // A operand from shared memory is bound by that (6 KB at 128 bytes per clock: 48 cycles instead of 32), so A1 and A2 are kept in TMEM; only for dk, dv of wide
 // heads, whose two sums take the other 256 columns, are they in shared memory.
-#ifndef V1
-#define V1 4
-#define V2 4
-#endif
-constexpr int BY_FMA_DKDV = V1, BY_FMA_DQ = V2;
 constexpr int BWD_THREADS = 640, BLOCK = 64, BSLAB = BLOCK * 128;
 
 template <int D, bool DKDV> struct Backward {
@@ -706,7 +700,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             for (int i = 0; i < 16; ++i) {
                 const uint64_t s2 = pack2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), x2 = DKDV ? mul2(s2, scale2) : fma2(s2, scale2, row_x);
                 float e0, e1;
-                if (i % (DKDV ? BY_FMA_DKDV : BY_FMA_DQ) == 1) {
+                if (i % BY_FMA == BY_FMA - 1) {
                     exp2_by_fma(x2, e0, e1);
                 } else {
                     unpack2(x2, e0, e1);
