@@ -779,34 +779,47 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
 
 // ---- joins of tiles in pieces ---------------------------------------------------------------------------------------------------
 //
-// A thread takes eight channels of a row; the pieces are taken in their order.  forward: out = sum_s 2^(lse2_s - lse2) out_s; backward: a plain sum.
+// A thread takes eight channels of a row; the pieces are taken in their order.  forward: out = sum_s 2^(lse2_s - lse2) out_s; backward: plain sums, of dq, dk and dv
+// in one launch.
 constexpr int JOIN_THREADS = 256;
+struct Join {
+    View out, rest;             // rest: what rounding takes from out, forward only; its data may be null
+    const float* partials;
+    Split cut;
+    int64_t threads;
+    int tiles, rows_per_tile, N, H;
+};
+struct Joins {
+    Join join[3];
+    float* lse;                 // forward
+    int C;
+};
 template <typename T, bool SOFTMAX>
-__global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const __grid_constant__ View out, const __grid_constant__ View rest_out, float* lse_out, const __grid_constant__ Split cut, int tiles, int rows_per_tile,
-                                                                         int N, int H, int C, const float* __restrict__ partials) {
-    const int chunks = C / 8;
-    const int64_t rest = cut.rest() * rows_per_tile, index = (int64_t)blockIdx.x * JOIN_THREADS + threadIdx.x, local = index / chunks;
+__global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const __grid_constant__ Joins a) {
+    const Join& j = a.join[SOFTMAX ? 0 : blockIdx.y];
+    const int C = a.C, chunks = C / 8, parts = j.cut.parts;
+    const int64_t rest = j.cut.rest() * j.rows_per_tile, index = (int64_t)blockIdx.x * JOIN_THREADS + threadIdx.x, local = index / chunks;
     const int c = (int)(index - local * chunks) * 8;
-    if (local >= rest) return;
+    if (index >= j.threads) return;
+    const int64_t tile = j.cut.full + local / j.rows_per_tile, bh = tile / j.tiles, b = bh / j.H, h = bh - b * j.H;
+    const int n = (int)(tile - bh * j.tiles) * j.rows_per_tile + (int)(local % j.rows_per_tile);
     wait_for_previous();
-    const int64_t tile = cut.full + local / rows_per_tile, bh = tile / tiles, b = bh / H, h = bh - b * H;
-    const int n = (int)(tile - bh * tiles) * rows_per_tile + (int)(local % rows_per_tile);
-    if (n >= N) return;
-    const float* statistics = partials + cut.parts * rest * C + local;
+    if (n >= j.N) return;
+    const float* statistics = j.partials + parts * rest * C + local;
     float top = -INFINITY, total = 0.f;
     if (SOFTMAX)
 #pragma unroll 4
-        for (int s = 0; s < cut.parts; ++s) top = fmaxf(top, statistics[s * rest]);
+        for (int s = 0; s < parts; ++s) top = fmaxf(top, statistics[s * rest]);
     const float base = top == -INFINITY ? 0.f : top;
     float sum[8] = {};
 #pragma unroll 4
-    for (int s = 0; s < cut.parts; ++s) {
+    for (int s = 0; s < parts; ++s) {
         float w = 1.f;
         if (SOFTMAX) {
             w = ex2(statistics[s * rest] - base);
             total += w;
         }
-        const float4* from = reinterpret_cast<const float4*>(partials + (s * rest + local) * C + c);
+        const float4* from = reinterpret_cast<const float4*>(j.partials + (s * rest + local) * C + c);
         const float4 x = from[0], y = from[1];
         const float v[8] = {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
 #pragma unroll
@@ -815,15 +828,19 @@ __global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const _
     const float factor = !SOFTMAX ? 1.f : total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] *= factor;
-    store8<T>(static_cast<T*>(out.data) + b * out.batch + h * out.head + n * out.point + c,
-              rest_out.data == nullptr ? nullptr : static_cast<T*>(rest_out.data) + b * rest_out.batch + h * rest_out.head + n * rest_out.point + c, sum);
-    if (SOFTMAX && c == 0 && lse_out != nullptr) lse_out[bh * N + n] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
+    store8<T>(static_cast<T*>(j.out.data) + b * j.out.batch + h * j.out.head + n * j.out.point + c,
+              j.rest.data == nullptr ? nullptr : static_cast<T*>(j.rest.data) + b * j.rest.batch + h * j.rest.head + n * j.rest.point + c, sum);
+    if (SOFTMAX && c == 0 && a.lse != nullptr) a.lse[bh * j.N + n] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
+}
+Join join_of(const View& out, const View& rest, const Split& cut, int rows_per_tile, int N, int H, int C, const float* partials) {
+    const int64_t threads = cut.parts > 1 ? cut.rest() * rows_per_tile * (C / 8) : 0;
+    return Join{out, rest, partials, cut, threads, (N + rows_per_tile - 1) / rows_per_tile, rows_per_tile, N, H};
 }
 template <typename T, bool SOFTMAX>
-cudaError_t join_tiles(const View& out, const View& rest_out, float* lse, const Split& cut, int tiles, int rows_per_tile, int N, int H, int C, const float* partials, cudaStream_t stream) {
-    const int64_t threads = cut.rest() * rows_per_tile * (C / 8);
-    return launch_dependent(attend_join_tiles_kernel<T, SOFTMAX>, (unsigned)((threads + JOIN_THREADS - 1) / JOIN_THREADS), JOIN_THREADS, 0, stream, out, rest_out, lse, cut, tiles,
-                            rows_per_tile, N, H, C, partials);
+cudaError_t launch_joins(const Joins& a, cudaStream_t stream) {
+    const int64_t most = std::max({a.join[0].threads, a.join[1].threads, a.join[2].threads});
+    if (most == 0) return cudaSuccess;
+    return launch_dependent(attend_join_tiles_kernel<T, SOFTMAX>, dim3((unsigned)((most + JOIN_THREADS - 1) / JOIN_THREADS), SOFTMAX ? 1 : 3), JOIN_THREADS, 0, stream, a);
 }
 
 using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*, const cuuint32_t*,
@@ -860,8 +877,12 @@ cudaError_t forward_as(const Problem& p, const CUtensorMap (&maps)[3], const Spl
     if (e != cudaSuccess) return e;
     kernel<<<(unsigned)cut.blocks(), FWD_THREADS, Forward<D>::SMEM, stream>>>(p, maps[0], maps[1], maps[2], tiles, cut, partials);
     e = cudaGetLastError();
-    if (e != cudaSuccess || cut.rest() == 0) return e;
-    return join_tiles<T, true>(p.out, p.rest, p.lse, cut, tiles, 2 * TILE, p.Nq, p.Hq, p.C, partials, stream);
+    if (e != cudaSuccess) return e;
+    Joins joins{};
+    joins.join[0] = join_of(p.out, p.rest, cut, 2 * TILE, p.Nq, p.Hq, p.C, partials);
+    joins.lse = p.lse;
+    joins.C = p.C;
+    return launch_joins<T, true>(joins, stream);
 }
 
 template <typename T, int D, bool DKDV, bool WEIGHTS>
@@ -931,16 +952,12 @@ Split split_of(const Problem& p, Kernel kernel, int sms) {
 
 cudaError_t join_backward(const Problem& p, sna_dtype_t dtype, int sms, const float* dq_partials, const float* dkdv_partials, cudaStream_t stream) {
     const Split q = split_of(p, Kernel::DQ, sms), k = split_of(p, Kernel::DKDV, sms);
-    const int q_tiles = (p.Nq + TILE - 1) / TILE, k_tiles = (p.Nk + TILE - 1) / TILE;
-    auto run = [&](auto t) {
-        using T = decltype(t);
-        cudaError_t e = cudaSuccess;
-        if (q.parts > 1) e = join_tiles<T, false>(p.dq, View{}, nullptr, q, q_tiles, TILE, p.Nq, p.Hq, p.C, dq_partials, stream);
-        if (e == cudaSuccess && k.parts > 1) e = join_tiles<T, false>(p.dk, View{}, nullptr, k, k_tiles, TILE, p.Nk, p.Hk, p.C, dkdv_partials, stream);
-        if (e == cudaSuccess && k.parts > 1) e = join_tiles<T, false>(p.dv, View{}, nullptr, k, k_tiles, TILE, p.Nk, p.Hk, p.C, dkdv_partials + k.parts * k.rest() * TILE * p.C, stream);
-        return e;
-    };
-    return dtype == SNA_BFLOAT16 ? run(__nv_bfloat16()) : run(__half());
+    Joins joins{};
+    joins.join[0] = join_of(p.dq, View{}, q, TILE, p.Nq, p.Hq, p.C, dq_partials);
+    joins.join[1] = join_of(p.dk, View{}, k, TILE, p.Nk, p.Hk, p.C, dkdv_partials);
+    joins.join[2] = join_of(p.dv, View{}, k, TILE, p.Nk, p.Hk, p.C, dkdv_partials + k.parts * k.rest() * TILE * p.C);
+    joins.C = p.C;
+    return dtype == SNA_BFLOAT16 ? launch_joins<__nv_bfloat16, false>(joins, stream) : launch_joins<__half, false>(joins, stream);
 }
 
 size_t partial_floats(const Problem& p, Kernel kernel, int sms) {
