@@ -385,6 +385,10 @@ typedef struct {
  * last check (SNA_ERR_CUDA; its outputs would be incomplete), as sna_plan_check does for a plan.  Not expected to happen. */
 sna_status_t sna_layer_check(void);
 
+/* Test aid for that path, as sna_debug_exercise_bounded_wait is for a plan's: one tiny kernel waits, by the same routine and for a few polls, on a barrier that
+ * nothing arrives on; it records that and returns normally. */
+sna_status_t sna_debug_exercise_layer_wait(void* cuda_stream);
+
 /* workspace: device, 256-byte aligned, private to the call until its work has finished; at least the bytes that the query gives for the same
  * problem on the current device (0: it may be NULL).  The queries return 0 for invalid arguments. */
 size_t sna_attention_forward_workspace_bytes(const sna_attention_t* a, sna_dtype_t dtype);

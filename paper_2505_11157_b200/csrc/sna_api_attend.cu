@@ -34,7 +34,7 @@ sna_status_t describe(const sna_attention_t* a, sna_dtype_t dtype, bool backward
     struct { const sna_tensor_t& t; View& view; bool used, query; } tensors[] = {
         {a->q, p.q, true, true},          {a->k, p.k, true, false},       {a->v, p.v, true, false},       {a->out, p.out, true, true},
         {a->out_rest, p.rest, a->out_rest.data != nullptr, true},
-                {a->dout, p.dout, backward, true}, {a->dq, p.dq, backward, true}, {a->dk, p.dk, backward, false}, {a->dv, p.dv, backward, false}};
+        {a->dout, p.dout, backward, true}, {a->dq, p.dq, backward, true}, {a->dk, p.dk, backward, false}, {a->dv, p.dv, backward, false}};
     for (const auto& x : tensors) {
         if (!x.used) continue;
         if (!multiple_of_8(x.t)) return fail(SNA_ERR_INVALID_ARG, "data pointers and strides must be multiples of 8 elements");
@@ -157,6 +157,13 @@ sna_status_t sna_attention_backward(const sna_attention_t* a, sna_dtype_t dtype,
         if (e == cudaSuccess && keys) e = launch_backward_dkdv(p, s, dtype, stream);
     }
     if (e != cudaSuccess) return sna::fail(SNA_ERR_CUDA, "attention backward launch: %s", cudaGetErrorString(e));
+    return SNA_OK;
+}
+
+sna_status_t sna_debug_exercise_layer_wait(void* cuda_stream) {
+    if (sna::sms_of_current_device() == 0) return sna::fail(SNA_ERR_CUDA, "no CUDA device");
+    const cudaError_t e = launch_wait_probe((cudaStream_t)cuda_stream);
+    if (e != cudaSuccess) return sna::fail(SNA_ERR_CUDA, "probe launch: %s", cudaGetErrorString(e));
     return SNA_OK;
 }
 

@@ -41,14 +41,14 @@ __host__ __device__ inline int64_t weight_blocks_of(const Problem& p) {
 
 // How a tcgen05 kernel's tiles become thread blocks, of which an SM runs one at a time: the first `full` tiles whole, the others in `parts` pieces of the
 // streamed side, whose partial results (fp32) a second kernel joins.
+// The whole waves stay whole.  The last, partial wave is cut so that its pieces end early: R tiles in k pieces take ceil(R k / SMs) / k of a wave (256 tiles on 148
+// SMs: 1.75 waves with four pieces each instead of 2).  Not for many waves, which gain little, nor into pieces of a few streamed blocks.
 struct Split {
     int64_t tiles, full;
     int parts;
     __host__ __device__ int64_t blocks() const { return full + (tiles - full) * parts; }
     __host__ __device__ int64_t rest() const { return tiles - full; }
 };
-// The whole waves stay whole.  The last, partial wave is cut so that its pieces end early: R tiles in k pieces take ceil(R k / SMs) / k of a wave (256 tiles on 148
-// SMs: 1.75 waves with four pieces each instead of 2).  Not for many waves, which gain little, nor into pieces of a few streamed blocks.
 __host__ __device__ inline int64_t query_blocks_of(const Problem& p) { return (int64_t)p.B * p.Hq * ((p.Nq + STATS_BLOCK - 1) / STATS_BLOCK); }
 
 // Powers of two that keep float16 operands of the second products away from the numbers that its exponent has no room for: softmax
@@ -57,8 +57,7 @@ template <typename T> constexpr float SHIFT = 0.f;
 template <> constexpr float SHIFT<__half> = 14.f;
 
 #ifdef __CUDACC__
-// A number in three bfloat16 parts (24 bits), whose products with ones a tensor core adds up; the lowest, for a point left out: times a scale of 2^-20
-// or more, below any finite score of a point that takes part.
+// A number in three bfloat16 parts (24 bits), whose products with ones a tensor core adds up.
 constexpr uint32_t EXTRA_ONES_0 = 0x3f803f80u, EXTRA_ONES_1 = 0x00003f80u;
 constexpr uint32_t EXTRA_OUT = 0x0000ff61u;        // -2.99e38: times a scale of 2^-20 or more, below any finite score of a point that takes part
 __device__ __forceinline__ uint2 extra_parts(float x) {
@@ -91,6 +90,7 @@ bool backward_dq_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms
 bool backward_dkdv_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
 cudaError_t join_backward(const Problem& p, sna_dtype_t dtype, int sms, const float* dq_partials, const float* dkdv_partials, cudaStream_t stream);
 cudaError_t read_status(int* status);
+cudaError_t launch_wait_probe(cudaStream_t stream);
 
 // mma.sync kernels (sna_kernels_attend.cu)
 int forward_splits(const Problem& p, int sms);

@@ -416,7 +416,7 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
 //   warp 16  TMA of the blocks
 //   warps 17, 19  MMAs, as soon as block j has left the columns: dv of block j and S of block j + 2 (dq: S alone, when S has been read); dk or dq of
 //            block j and T of block j + 2.  (One thread for all of them was busy all the time: a wait costs it 60 cycles or more even if it need not wait.)
-//   warp 18  dq: weights of the block's points, rows of points left out zeroed
+//   warp 18  dq: if points are left out, zeroes their rows of the block (their weights come with it)
 //   warps 0-15  element-wise: a group of four warps takes one half of the columns of the blocks of even or of odd number, thread = row; p while T is computed;
 //            p and ds go back over S and T, each half over its own.  (Two groups, with whole rows per thread, were bound by latencies: issue slots 39 %,
 //            special-function unit 55 % busy.)
@@ -995,6 +995,18 @@ bool forward_tc(const Problem& p, sna_dtype_t dtype, int sms, float* partials, c
     if (dtype == SNA_BFLOAT16) e = p.C <= 64 ? run(__nv_bfloat16(), W64()) : run(__nv_bfloat16(), W128());
     else e = p.C <= 64 ? run(__half(), W64()) : run(__half(), W128());
     return true;
+}
+
+// A wait on a barrier that nothing arrives on, as long as waits are after one that has run out.
+__global__ void wait_probe_kernel() {
+    __shared__ unsigned long long bar;
+    mb_init(s32(&bar), 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (!mb_wait(s32(&bar), 0, false)) atomicExch(&g_status, 1);
+}
+cudaError_t launch_wait_probe(cudaStream_t stream) {
+    wait_probe_kernel<<<1, 1, 0, stream>>>();
+    return cudaGetLastError();
 }
 
 cudaError_t read_status(int* status) {

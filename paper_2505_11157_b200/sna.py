@@ -103,6 +103,7 @@ _SIGNATURES = {
     "sna_attention_backward_workspace_bytes": (_sz, [ctypes.POINTER(SnaAttention), _i]),
     "sna_attention_backward": (_i, [ctypes.POINTER(SnaAttention), _i, _vp, _sz, _vp]),
     "sna_layer_check": (_i, []),
+    "sna_debug_exercise_layer_wait": (_i, [_vp]),
     "sna_dropout": (_i, [_vp, _vp, _vp, _i, _i64, _d, _vp, _vp]),
     "sna_measure_fp32_fma_peak": (_i, [ctypes.POINTER(ctypes.c_double)]),
     "sna_status_string": (ctypes.c_char_p, [_i]),
@@ -191,6 +192,11 @@ def sna_plan_check(plan: int):
 def sna_layer_check():
     """Synchronise and raise if a kernel of the 16-bit attention gave up on a bounded wait on the current device."""
     _check(_lib.sna_layer_check())
+
+
+def sna_debug_exercise_layer_wait(stream=None) -> None:
+    """Test aid: make one bounded wait run out on the GPU so that ``sna_layer_check`` has a failure to report."""
+    _check(_lib.sna_debug_exercise_layer_wait(_stream(stream)))
 
 
 def sna_plan_get_nnz(plan: int) -> int:

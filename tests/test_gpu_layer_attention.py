@@ -325,3 +325,87 @@ def test_refusals():
 def test_no_kernel_gave_up_on_a_wait():
     """Last in this file: every bounded wait of the calls above came to its end."""
     sna.sna_layer_check()
+
+
+def test_a_wait_that_runs_out_is_reported_once():
+    sna.sna_layer_check()
+    sna.sna_debug_exercise_layer_wait()
+    with pytest.raises(sna.SnaError, match="gave up on a bounded wait"):
+        sna.sna_layer_check()
+    sna.sna_layer_check()
+    after = run(*(heads(1, 1, (1, 200), 32, torch.bfloat16) for _ in range(3)))
+    assert all(bool(torch.isfinite(t).all()) for t in after)
+
+
+@pytest.mark.parametrize("saved", range(7), ids=["q", "k", "v", "log_weights", "out", "lse", "rest"])
+@pytest.mark.parametrize("change, says", [(lambda t: t.cpu(), "CUDA tensor"), (lambda t: t.double(), "must be|type of q"), (lambda t: t[..., :-1], "shape|must be|C ="),
+                                          (lambda t: t + 0, None), (lambda t: t.transpose(0, 1).contiguous().transpose(0, 1) if t.dim() == 5 else t, None)],
+                         ids=["host", "double", "shape", "copy", "strides"])
+def test_saved_tensors_that_hooks_return_are_checked(saved, change, says):
+    torch.manual_seed(12)
+    q, k, v = (heads(2, 2, (1, n), 32, torch.bfloat16).requires_grad_() for n in (20, 70, 70))
+    w = torch.randn(2, 70, device="cuda")
+    g = torch.randn(q.shape, device="cuda").bfloat16()
+    seen = []
+
+    def unpack(t):
+        seen.append(t)
+        return change(t) if len(seen) == saved + 1 else t
+
+    ref = torch.autograd.grad(layer.weighted_attention(q, k, v, w), (q, k, v), g)
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, unpack):
+        out = layer.weighted_attention(q, k, v, w)
+    if says:
+        with pytest.raises(ValueError, match=says):
+            torch.autograd.grad(out, (q, k, v), g)
+    else:
+        assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, (q, k, v), g), ref))
+    assert len(seen) == 7
+
+
+def test_inputs_changed_before_the_backward_pass_and_single_gradients():
+    torch.manual_seed(13)
+    q, k, v = (heads(1, 2, (1, 90), 32, torch.float16) for _ in range(3))
+    ends = [x.clone().requires_grad_() for x in (q, k, v)]
+    g = torch.randn(q.shape, device="cuda").half()
+    ref = torch.autograd.grad(layer.weighted_attention(*ends), ends, g)
+    for i in range(3):
+        ends = [x.clone().requires_grad_(j == i) for j, x in enumerate((q, k, v))]
+        assert torch.equal(torch.autograd.grad(layer.weighted_attention(*ends), ends[i], g)[0], ref[i])
+    ends = [x.clone().requires_grad_() for x in (q, k, v)]
+    w = torch.zeros(90, device="cuda")
+    out = layer.weighted_attention(*ends, w)
+    w += 1
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        out.sum().backward()
+
+
+def test_threads_and_streams_at_once():
+    import threading
+    torch.manual_seed(14)
+    inputs = [[heads(1, 4, (1, n), 64, torch.bfloat16) for _ in range(3)] for n in (200, 700, 90, 8)]
+    refs = []
+    for x in inputs:
+        torch.manual_seed(1)
+        refs.append(run(*x))
+    torch.cuda.synchronize()
+    results = [None] * len(inputs)
+
+    def work(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            gens = [t.detach().requires_grad_() for t in inputs[i]]
+            for _ in range(20):
+                out = layer.weighted_attention(*gens)
+                results[i] = (out.detach(), *torch.autograd.grad(out, gens, torch.ones_like(out)))
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(inputs))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    for x, got, ref in zip(inputs, results, refs):
+        assert torch.equal(got[0], ref[0])
+        gens = [t.detach().requires_grad_() for t in x]
+        out = layer.weighted_attention(*gens)
+        assert all(torch.equal(a, b) for a, b in zip(got[1:], torch.autograd.grad(out, gens, torch.ones_like(out))))

@@ -272,3 +272,31 @@ def test_refusals():
     out = call(q, k)[0]
     with pytest.raises(RuntimeError, match="differentiable once"):
         torch.autograd.grad(out.sum(), q, create_graph=True)
+
+
+@pytest.mark.parametrize("saved", range(8), ids=["q", "k", "q_weight", "k_weight", "q_lat", "q_lon", "k_lat", "k_lon"])
+@pytest.mark.parametrize("change, says", [(lambda t: t.cpu(), "CUDA tensor"), (lambda t: t.double(), "must be|type of"), (lambda t: t[:-1], "shape|must be"), (lambda t: t + 0, None)],
+                         ids=["host", "double", "shape", "copy"])
+def test_saved_tensors_that_hooks_return_are_checked(saved, change, says):
+    torch.manual_seed(15)
+    q, k = heads(2, 2, 3, 4, 16, torch.float32).requires_grad_(), heads(2, 1, 5, 6, 16, torch.float32).requires_grad_()
+    w = [torch.randn(16, device="cuda").requires_grad_() for _ in range(2)]
+    rotations = [tables(3, 4, 2, 3), tables(5, 6, 2, 3)]
+    seen = []
+
+    def unpack(t):
+        seen.append(t)
+        return change(t) if len(seen) == saved + 1 else t
+
+    call = lambda: sum(o.square().sum() for o in layer.qk_norm_rotate(q, k, *w, *rotations))
+    ref = torch.autograd.grad(call(), (q, k, *w))
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t):
+        out = layer.qk_norm_rotate(q, k, *w, *rotations)
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, unpack):
+        out = layer.qk_norm_rotate(q, k, *w, *rotations)
+    total = sum(o.square().sum() for o in out)
+    if says:
+        with pytest.raises(ValueError, match=says):
+            torch.autograd.grad(total, (q, k, *w))
+    else:
+        assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(total, (q, k, *w)), ref))
