@@ -239,6 +239,12 @@ void check_attention(const AttentionInputs& in) {
     TORCH_CHECK_VALUE(!w.requires_grad(), "log_weights: no gradient of the weights is computed");
 }
 
+// (the inputs become what the kernels read)
+void make_readable(AttentionInputs& in) {
+    for (at::Tensor* t : {&in.q, &in.k, &in.v}) *t = attendable(*t);
+    if (in.log_weights.defined() && in.log_weights.size(-1) > 1 && in.log_weights.stride(-1) != 1) in.log_weights = in.log_weights.contiguous();
+}
+
 sna_attention_t described(const AttentionInputs& in) {
     sna_attention_t a{};
     a.B = (int)in.q.size(0); a.Hq = (int)in.q.size(1); a.Hk = (int)in.k.size(1); a.C = (int)in.q.size(4);
@@ -252,11 +258,9 @@ sna_attention_t described(const AttentionInputs& in) {
     return a;
 }
 
-// (the inputs become what the kernels read)
 std::tuple<at::Tensor, at::Tensor, at::Tensor> attention_forward(AttentionInputs& in, bool for_backward) {
     const c10::cuda::CUDAGuard guard(in.q.device());
-    for (at::Tensor* t : {&in.q, &in.k, &in.v}) *t = attendable(*t);
-    if (in.log_weights.defined() && in.log_weights.size(-1) > 1 && in.log_weights.stride(-1) != 1) in.log_weights = in.log_weights.contiguous();
+    make_readable(in);
     at::Tensor out = attention_result_like(in.q), lse = at::empty(in.q.sizes().slice(0, 4), in.q.options().dtype(at::kFloat));
     const sna_dtype_t dtype = dtype_of(in.q, "q");
     sna_attention_t a = described(in);
@@ -300,7 +304,7 @@ public:
         TORCH_CHECK_VALUE(lse.scalar_type() == at::kFloat && lse.sizes() == in.q.sizes().slice(0, 4) && lse.is_contiguous(), "lse must be float32 and contiguous, of shape ",
                           in.q.sizes().slice(0, 4));
         const c10::cuda::CUDAGuard guard(in.q.device());
-        for (at::Tensor* t : {&in.q, &in.k, &in.v}) *t = attendable(*t);
+        make_readable(in);
         const at::Tensor out = attendable(saved[4]), rest = attendable(saved[6]), dout = attendable(grads[0].to(in.q.scalar_type()));
         at::Tensor dq = attention_result_like(in.q), dk = attention_result_like(in.k), dv = attention_result_like(in.v);
         const sna_dtype_t dtype = dtype_of(in.q, "q");

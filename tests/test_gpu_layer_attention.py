@@ -409,3 +409,15 @@ def test_threads_and_streams_at_once():
         gens = [t.detach().requires_grad_() for t in x]
         out = layer.weighted_attention(*gens)
         assert all(torch.equal(a, b) for a, b in zip(got[1:], torch.autograd.grad(out, gens, torch.ones_like(out))))
+
+
+def test_saved_weights_that_hooks_return_with_other_strides():
+    # (every layout below lies within memory of as many values as are read from it)
+    torch.manual_seed(16)
+    q, k, v = (heads(2, 2, (1, n), 32, torch.bfloat16).requires_grad_() for n in (20, 70, 70))
+    w = torch.randn(2, 70, device="cuda")
+    g = torch.randn(q.shape, device="cuda").bfloat16()
+    ref = torch.autograd.grad(layer.weighted_attention(q, k, v, w), (q, k, v), g)
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t.t().contiguous().t() if t.shape == w.shape else t):
+        out = layer.weighted_attention(q, k, v, w)
+    assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, (q, k, v), g), ref))
