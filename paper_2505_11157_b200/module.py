@@ -61,8 +61,9 @@ class SphericalNeighborhoodAttention(torch.nn.Module):
 
     def _tables_on(self, device):
         if device not in self._tables:
-            rotations = layer.plan_rotations(self.plan, self.head_dim, device) if self.rotary else (None, None)
-            self._tables[device] = (*rotations, layer.log_quadrature_weights(self.plan, device) if self.half_attention else None)
+            with torch.inference_mode(False):       # (they outlive the first call, whose mode may not be the next one's)
+                rotations = layer.plan_rotations(self.plan, self.head_dim, device) if self.rotary else (None, None)
+                self._tables[device] = (*rotations, layer.log_quadrature_weights(self.plan, device) if self.half_attention else None)
         return self._tables[device]
 
     def _attend_by_heads(self, q, k, v):

@@ -171,3 +171,15 @@ def test_refusals():
         SphericalNeighborhoodAttention(full, 8, 2, 12, half_attention=True)
     with pytest.raises(ValueError, match="dropout"):
         SphericalNeighborhoodAttention(full, 8, 2, 16, dropout=1.0)
+
+
+def test_training_after_a_first_call_in_inference_mode():
+    torch.manual_seed(6)
+    plan = sna.Plan(6, 12, 6, 12, 0, 0, global_attention=True)
+    m = SphericalNeighborhoodAttention(plan, 8, 2, 16, qk_norm=True, rotary=True, half_attention=True).cuda()
+    x = torch.randn(2, 8, 6, 12, device="cuda")
+    with torch.inference_mode():
+        first = m(x)
+    y = m(x)
+    y.sum().backward()
+    assert torch.equal(first, y) and all(bool(torch.isfinite(p.grad).all()) for p in m.parameters())
