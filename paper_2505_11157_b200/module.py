@@ -100,5 +100,9 @@ class SphericalNeighborhoodAttention(torch.nn.Module):
             y = spherical_neighborhood_attention_cf(self.plan, q.float(), k.float(), v.float(), heads=self.heads)
         y = conv(y.to(x_q.dtype), self.wo, self.bo)
         if self.training and self.dropout > 0.0:
+            if residual is not None:        # (of other types, under autocast say: as the plain sum takes them)
+                dtype = torch.promote_types(y.dtype, residual.dtype)
+                residual = residual.to(dtype).expand_as(y)
+                y = y.to(dtype)
             return layer.residual_dropout(y, layer.dropout_state(y.device), self.dropout, residual)
         return y if residual is None else residual + y

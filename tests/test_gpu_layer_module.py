@@ -183,3 +183,23 @@ def test_training_after_a_first_call_in_inference_mode():
     y = m(x)
     y.sum().backward()
     assert torch.equal(first, y) and all(bool(torch.isfinite(p.grad).all()) for p in m.parameters())
+
+
+@pytest.mark.parametrize("shape", [(2, 8, 12, 24), (1, 8, 1, 1)])
+def test_residuals_of_another_type_or_shape_with_dropout(shape):
+    torch.manual_seed(7)
+    plan = sna.Plan(12, 24, 12, 24, 0, 0, global_attention=True)
+    m = SphericalNeighborhoodAttention(plan, 8, 2, 16, half_attention=True, dropout=0.25).cuda()
+    x, residual = torch.randn(2, 8, 12, 24, device="cuda"), torch.randn(*shape, device="cuda", requires_grad=True)
+    with torch.autocast("cuda", torch.bfloat16):
+        rest = m.eval()(x)
+        kept = m.train()(x, residual=residual)
+    assert rest.dtype == torch.bfloat16 and kept.dtype == torch.float32
+    # a kept value of the attention's result in 16 bits, divided by 0.75 in 32 and added in one rounding; half a unit of the sum and of the quotient
+    y = kept.detach().double() - residual.detach().double()
+    quotient = rest.detach().double() / 0.75
+    room = 2.0 ** -23 * (quotient.abs() + kept.detach().double().abs() + residual.detach().double().abs())
+    dropped = y.abs() <= room
+    assert bool((dropped | ((y - quotient).abs() <= room)).all()) and 0.2 < float(dropped.double().mean()) < 0.3
+    kept.sum().backward()
+    assert torch.equal(residual.grad, torch.full(shape, 2 * 8 * 12 * 24 / residual.numel(), device="cuda"))
