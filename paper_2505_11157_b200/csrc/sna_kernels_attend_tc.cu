@@ -362,9 +362,10 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
                 const int64_t at = ((int64_t)b * p.Hq + h) * p.Nq + row;
                 const int64_t rest = cut.rest() * 2 * TILE, local = piece.local * 2 * TILE + t * TILE + (warp & 3) * 32 + lane;
                 const bool there = row < p.Nq;
-                const float inverse = ref == -INFINITY ? 0.f : 1.f / l;
+                const bool none = ref == -INFINITY && l == l;        // (not a row of NaN)
+                const float inverse = none ? 0.f : 1.f / l;
                 if (there) {
-                    const float lse2 = ref == -INFINITY ? -INFINITY : ref + log2f(l) - FORWARD_SHIFT<T>;
+                    const float lse2 = none ? -INFINITY : ref + log2f(l) - FORWARD_SHIFT<T>;
                     if (parts > 1) partials[parts * rest * p.C + part * rest + local] = lse2;
                     else if (p.lse != nullptr) p.lse[at] = lse2 * LN2;
                 }

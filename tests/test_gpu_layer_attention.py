@@ -421,3 +421,44 @@ def test_saved_weights_that_hooks_return_with_other_strides():
     with torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: t.t().contiguous().t() if t.shape == w.shape else t):
         out = layer.weighted_attention(q, k, v, w)
     assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(out, (q, k, v), g), ref))
+
+
+@pytest.mark.parametrize("n", [8, 200])
+@pytest.mark.parametrize("weighted", [False, True])
+def test_a_row_of_nan_says_so_in_its_lse(n, weighted):
+    torch.manual_seed(17)
+    q, k, v = heads(1, 1, (1, n), 32, torch.bfloat16), heads(1, 1, (1, 200), 32, torch.bfloat16), heads(1, 1, (1, 200), 32, torch.bfloat16)
+    q[0, 0, 0, 3, 5] = math.nan
+    w = torch.randn(200, device="cuda") if weighted else None
+    out, lse = layer.weighted_attention(q, k, v, w, return_lse=True)
+    nan = torch.arange(n, device="cuda") == 3
+    assert torch.equal(lse[0, 0, 0].isnan(), nan) and torch.equal(out[0, 0, 0].isnan().all(-1), nan) and torch.equal(out[0, 0, 0].isnan().any(-1), nan)
+
+
+@pytest.mark.parametrize("axes", [(2, 3), (3,), (0, 2, 3), (1,)])
+def test_gradients_of_means(axes):
+    torch.manual_seed(18)
+    ends = [heads(2, 2, (3, n), 32, torch.bfloat16).requires_grad_() for n in (30, 40, 40)]
+    out = layer.weighted_attention(*ends)
+    g = torch.randn(out.mean(axes, keepdim=True).shape, device="cuda").bfloat16()
+    for got, ref in zip(torch.autograd.grad(out, ends, g.expand_as(out), retain_graph=True), torch.autograd.grad(out, ends, g.expand_as(out).contiguous())):
+        assert torch.equal(got, ref)
+
+
+def test_a_pending_negation_is_refused_and_that_of_a_gradient_taken():
+    torch.manual_seed(19)
+    q, k, v = (heads(1, 1, (1, 100), 32, torch.float16).requires_grad_() for _ in range(3))
+    g = torch.randn(q.shape, device="cuda").half()
+    pending = torch._neg_view(g)
+    assert pending.is_neg()
+    for args in ((pending, k, v), (q, pending, v), (q, k, pending)):
+        with pytest.raises(ValueError, match="pending negation"):
+            layer.weighted_attention(*args)
+    with pytest.raises(ValueError, match="pending negation"):
+        layer.qk_norm_rotate(q, pending)
+    with pytest.raises(ValueError, match="pending negation"):
+        layer.residual_dropout(pending, layer.dropout_state("cuda"), 0.5)
+    w = torch.ones(32, device="cuda")
+    state = layer.dropout_state("cuda")
+    for f in (lambda: layer.weighted_attention(q, k, v), lambda: layer.qk_norm_rotate(q, k, w)[0], lambda: layer.residual_dropout(q, state, 0.5)):
+        assert torch.equal(torch.autograd.grad(f(), q, pending)[0], torch.autograd.grad(f(), q, -g)[0])
