@@ -60,34 +60,66 @@ sna_status_t check_workspace(const void* workspace, size_t bytes, size_t need) {
 // The tcgen05 kernels find a row's maximum before the scores are scaled, and hold weights divided by the scale: it has to be positive, and not so small that
 // a point left out could be taken for one with a low weight.
 bool on_tensor_memory(const Problem& p) { return p.Nq > 16 && p.Nk >= 64 && p.scale >= 0x1p-20f && p.scale <= 0x1p20f; }
+// Pieces of a workspace, or with a null pointer their sizes alone.
+struct Pieces {
+    char* at;
+    size_t bytes = 0;
+    char* take(size_t size) {
+        char* here = at == nullptr ? nullptr : at + bytes;
+        bytes += align256(size);
+        return here;
+    }
+    Selection selection(const Problem& p) {
+        Selection sel{};
+        if (!on_tensor_memory(p) || !selects(p)) return sel;
+        const size_t copies = (size_t)p.B * p.Hk * p.Nk * p.C * 2;
+        sel.taken = reinterpret_cast<int*>(take((size_t)p.B * sizeof(int)));
+        sel.index = reinterpret_cast<int*>(take((size_t)p.B * p.Nk * sizeof(int)));
+        sel.weights = reinterpret_cast<float*>(take((size_t)p.B * p.Nk * sizeof(float)));
+        sel.k = take(copies);
+        sel.v = take(copies);
+        return sel;
+    }
+};
+
 // What the forward pass needs to hold partial results, on either path (the tcgen05 kernels fall back where the driver refuses a tensor).
-size_t forward_bytes(const Problem& p, int sms) {
+struct ForwardWorkspace {
+    float* partials;
+    Selection selection;
+    size_t bytes;
+};
+ForwardWorkspace forward_workspace(const Problem& p, void* workspace, int sms) {
+    Pieces pieces{static_cast<char*>(workspace)};
     const int splits = forward_splits(p, sms);
     const size_t simple = splits > 1 ? (size_t)splits * rows_of(p) * (1 + p.C) : 0;
-    return align256(sizeof(float) * (on_tensor_memory(p) ? std::max(simple, partial_floats(p, Kernel::FORWARD, sms)) : simple));
+    ForwardWorkspace w{};
+    w.partials = reinterpret_cast<float*>(pieces.take(sizeof(float) * (on_tensor_memory(p) ? std::max(simple, partial_floats(p, Kernel::FORWARD, sms)) : simple)));
+    w.selection = pieces.selection(p);
+    w.bytes = pieces.bytes;
+    return w;
 }
 
 struct BackwardWorkspace {
     Stats stats;
+    Selection selection;
     float *dq_partials, *dkdv_partials;
     size_t bytes;
 };
 BackwardWorkspace backward_workspace(const Problem& p, void* workspace, int sms) {
     BackwardWorkspace w{};
-    char* at = static_cast<char*>(workspace);
-    auto take = [&](size_t bytes) {
-        char* here = at == nullptr ? nullptr : at + w.bytes;
-        w.bytes += align256(bytes);
-        return here;
-    };
+    Pieces pieces{static_cast<char*>(workspace)};
+    auto take = [&](size_t bytes) { return pieces.take(bytes); };
+    const int64_t weight_blocks = weight_blocks_of(p, on_tensor_memory(p) && selects(p));
     w.stats.extra = reinterpret_cast<uint4*>(take((size_t)query_blocks_of(p) * 2 * STATS_BLOCK * sizeof(uint4)));
-    w.stats.weights = reinterpret_cast<uint4*>(take((size_t)weight_blocks_of(p) * STATS_BLOCK * sizeof(uint4)));
-    w.stats.gone = reinterpret_cast<uint2*>(take((size_t)weight_blocks_of(p) * sizeof(uint2)));
+    w.stats.weights = reinterpret_cast<uint4*>(take((size_t)weight_blocks * STATS_BLOCK * sizeof(uint4)));
+    w.stats.gone = reinterpret_cast<uint2*>(take((size_t)weight_blocks * sizeof(uint2)));
     w.stats.lse2 = reinterpret_cast<float*>(take((size_t)rows_of(p) * sizeof(float)));
     w.stats.D = reinterpret_cast<float*>(take((size_t)rows_of(p) * sizeof(float)));
     w.stats.norms = reinterpret_cast<uint32_t*>(take((size_t)p.B * p.Hk * 2 * sizeof(uint32_t)));
     w.dq_partials = reinterpret_cast<float*>(take(on_tensor_memory(p) ? sizeof(float) * partial_floats(p, Kernel::DQ, sms) : 0));
     w.dkdv_partials = reinterpret_cast<float*>(take(on_tensor_memory(p) ? sizeof(float) * partial_floats(p, Kernel::DKDV, sms) : 0));
+    w.selection = pieces.selection(p);
+    w.bytes = pieces.bytes;
     return w;
 }
 
@@ -103,7 +135,7 @@ size_t sna_attention_forward_workspace_bytes(const sna_attention_t* a, sna_dtype
     Problem p;
     if (describe(a, dtype, false, p) != SNA_OK) return 0;
     const int sms = sna::sms_of_current_device();
-    return sms == 0 ? 0 : forward_bytes(p, sms);
+    return sms == 0 ? 0 : forward_workspace(p, nullptr, sms).bytes;
 }
 
 sna_status_t sna_attention_forward(const sna_attention_t* a, sna_dtype_t dtype, void* workspace, size_t workspace_bytes, void* cuda_stream) {
@@ -113,12 +145,13 @@ sna_status_t sna_attention_forward(const sna_attention_t* a, sna_dtype_t dtype, 
     if (rows_of(p) == 0) return SNA_OK;
     const int sms = sna::sms_of_current_device();
     if (sms == 0) return sna::fail(SNA_ERR_CUDA, "no CUDA device");
-    st = check_workspace(workspace, workspace_bytes, forward_bytes(p, sms));
+    const ForwardWorkspace w = forward_workspace(p, workspace, sms);
+    st = check_workspace(workspace, workspace_bytes, w.bytes);
     if (st != SNA_OK) return st;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
-    float* partials = static_cast<float*>(workspace);
+    float* partials = w.partials;
     cudaError_t e = cudaSuccess;
-    if (!on_tensor_memory(p) || !forward_tc(p, dtype, sms, partials, stream, e)) {
+    if (!on_tensor_memory(p) || !forward_tc(p, w.selection, dtype, sms, partials, stream, e)) {
         const int splits = forward_splits(p, sms);
         e = launch_forward(p, dtype, splits, partials, stream);
         if (e == cudaSuccess && splits > 1) e = launch_join(p, dtype, splits, partials, stream);
@@ -147,11 +180,11 @@ sna_status_t sna_attention_backward(const sna_attention_t* a, sna_dtype_t dtype,
     if (st != SNA_OK) return st;
     cudaStream_t stream = (cudaStream_t)cuda_stream;
     const Stats& s = w.stats;
-    cudaError_t e = launch_statistics(p, s, dtype, stream);
+    cudaError_t e = launch_statistics(p, s, w.selection, dtype, stream);
     // (on_tensor_memory: there are queries and keys)
-    if (e == cudaSuccess && on_tensor_memory(p) && backward_dq_tc(p, s, dtype, sms, w.dq_partials, stream, e)) {
-        if (e == cudaSuccess && !backward_dkdv_tc(p, s, dtype, sms, w.dkdv_partials, stream, e)) e = cudaErrorInvalidValue;      // (the same tensors, in other boxes)
-        if (e == cudaSuccess) e = join_backward(p, dtype, sms, w.dq_partials, w.dkdv_partials, stream);
+    if (e == cudaSuccess && on_tensor_memory(p) && backward_dq_tc(p, s, w.selection, dtype, sms, w.dq_partials, stream, e)) {
+        if (e == cudaSuccess && !backward_dkdv_tc(p, s, w.selection, dtype, sms, w.dkdv_partials, stream, e)) e = cudaErrorInvalidValue;      // (the same tensors, in other boxes)
+        if (e == cudaSuccess) e = join_backward(p, w.selection, dtype, sms, w.dq_partials, w.dkdv_partials, stream);
     } else {
         if (e == cudaSuccess && queries) e = launch_backward_dq(p, s, dtype, stream);
         if (e == cudaSuccess && keys) e = launch_backward_dkdv(p, s, dtype, stream);

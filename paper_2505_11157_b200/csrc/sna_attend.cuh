@@ -25,18 +25,41 @@ struct Problem {
     float scale, scale_log2;
 };
 
+__host__ __device__ inline int64_t rows_of(const Problem& p) { return (int64_t)p.B * p.Hq * p.Nq; }
+
 // Workspace of the backward pass: statistics per query, and the largest norms per key head (bits of floats)
 struct Stats {
     float* lse2;                    // [B][Hq][Nq]: log2 of the sum of weights, +infinity for rows without any
     float* D;                       // [B][Hq][Nq]
     uint32_t* norms;                // [B][Hk][2]: of dout's rows, of v's rows (float16 only)
     uint4* extra;                   // [B][Hq][blocks of 64 queries][2][64]: what the tcgen05 dk/dv kernel adds to S and T per query (see there)
-    uint4* weights;                 // [B or 1][blocks of 64 points][64]: what the tcgen05 dq kernel adds to S per point, if there are weights
-    uint2* gone;                    // [B or 1][blocks of 64 points]: bits of the points left out
+    uint4* weights;                 // [B or 1; B if there is a selection][blocks of 64 points][64]: what the tcgen05 dq kernel adds to S per point, if there are weights
+    uint2* gone;                    // likewise, [blocks of 64 points]: bits of the points left out
 };
 constexpr int STATS_BLOCK = 64;
-__host__ __device__ inline int64_t weight_blocks_of(const Problem& p) {
-    return p.log_weights == nullptr ? 0 : (int64_t)(p.log_weights_batch == 0 ? 1 : p.B) * ((p.Nk + STATS_BLOCK - 1) / STATS_BLOCK);
+
+// The points that take part, one behind the other, for the tcgen05 kernels (workspace): where at least one point in sixteen of a batch is left out, its other
+// keys and values are copied together first, so that the kernels walk as many points as there are.
+struct Selection {
+    int* taken;                     // [B]: the number of points, or Nk where they are read in place; null: no selection
+    int* index;                     // [B][Nk]: which points they are
+    float* weights;                 // [B][Nk]: their logarithmic weights
+    void *k, *v;                    // [B][Hk][Nk][C]; zeros to the end of a tile of 128
+};
+constexpr int SELECT_POINTS = 256;
+// It costs 3 us if few are left out, and a pass over the keys and values if many are; so not for small problems, nor where few rows share them, nor for so many
+// points that counting them, which every block does, takes long.  us, forward and (in brackets) backward, B = 2, 8192 queries and points, bf16, with the points read
+// in place : with a selection: 4 heads of 32, none left out 184 : 188 (421 : 421), 3 % 197 : 198 (476 : 471), 7 % 206 : 179 (516 : 409), 40 % 212 : 128 (530 : 301);
+// 8 heads of 128 426 : 430 (1405 : 1400), 7 % 559 : 475 (1736 : 1474), 40 % 572 : 349 (1740 : 1086).  B = 1, 4 heads of 32, 2048 queries and points, none 19.5 : 21.7
+// (82 : 85), 40 % 20.5 : 21.0 (80 : 83).
+inline bool selects(const Problem& p) {
+    return p.log_weights != nullptr && (int64_t)p.G * p.Nq >= 2048 && p.Nk <= 65536 && rows_of(p) * p.Nk >= (int64_t)1 << 27;
+}
+inline View selected_view(const Problem& p, void* data) { return View{data, (int64_t)p.Hk * p.Nk * p.C, (int64_t)p.Nk * p.C, p.C}; }
+inline int64_t select_blocks_of(const Problem& p) { return (int64_t)p.B * p.Hk * ((p.Nk + SELECT_POINTS - 1) / SELECT_POINTS); }
+
+__host__ __device__ inline int64_t weight_blocks_of(const Problem& p, bool selected) {
+    return p.log_weights == nullptr ? 0 : (int64_t)(p.log_weights_batch == 0 && !selected ? 1 : p.B) * ((p.Nk + STATS_BLOCK - 1) / STATS_BLOCK);
 }
 
 // How a tcgen05 kernel's tiles become thread blocks, of which an SM runs one at a time: the first `full` tiles whole, the others in `parts` pieces of the
@@ -78,17 +101,16 @@ __device__ __forceinline__ float ds_scale(const Stats& s, int bk) {
 #endif
 
 inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
-__host__ __device__ inline int64_t rows_of(const Problem& p) { return (int64_t)p.B * p.Hq * p.Nq; }
 
 // tcgen05 kernels (sna_kernels_attend_tc.cu).  False: the driver refuses a map of one of the tensors (heads that share memory, say).
 // partials: room for partial_floats of the kernel.
 enum class Kernel { FORWARD, DQ, DKDV };
 Split split_of(const Problem& p, Kernel kernel, int sms);
 size_t partial_floats(const Problem& p, Kernel kernel, int sms);
-bool forward_tc(const Problem& p, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
-bool backward_dq_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
-bool backward_dkdv_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
-cudaError_t join_backward(const Problem& p, sna_dtype_t dtype, int sms, const float* dq_partials, const float* dkdv_partials, cudaStream_t stream);
+bool forward_tc(const Problem& p, const Selection& sel, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
+bool backward_dq_tc(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
+bool backward_dkdv_tc(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
+cudaError_t join_backward(const Problem& p, const Selection& sel, sna_dtype_t dtype, int sms, const float* dq_partials, const float* dkdv_partials, cudaStream_t stream);
 cudaError_t read_status(int* status);
 cudaError_t launch_wait_probe(cudaStream_t stream);
 
@@ -96,7 +118,8 @@ cudaError_t launch_wait_probe(cudaStream_t stream);
 int forward_splits(const Problem& p, int sms);
 cudaError_t launch_join(const Problem& p, sna_dtype_t dtype, int splits, const float* partials, cudaStream_t stream);
 cudaError_t launch_forward(const Problem& p, sna_dtype_t dtype, int splits, float* partials, cudaStream_t stream);
-cudaError_t launch_statistics(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream);
+cudaError_t launch_statistics(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, cudaStream_t stream);      // and the selection
+cudaError_t launch_selection(const Problem& p, const Selection& sel, cudaStream_t stream);
 cudaError_t launch_backward_dq(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream);
 cudaError_t launch_backward_dkdv(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream);
 

@@ -415,19 +415,103 @@ __global__ void __launch_bounds__(32 * JOIN_WARPS) attend_join_kernel(const __gr
     if (lane == 0 && p.lse != nullptr) p.lse[at] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
 }
 
+// ---- points that take part ----------------------------------------------------------------------------------------------------
+
+// A block of 256 threads, for 256 points of one batch and key head; the blocks of the first head write the lists.  Backward (s is there): also the weights that the
+// dq kernel adds to S, and the gradients of the points left out.
+__device__ __forceinline__ void select_points(const Problem& p, const Selection& sel, const Stats* s, int64_t block) {
+    constexpr int N = SELECT_POINTS, NW = N / 32;
+    __shared__ int sums[NW][3];
+    __shared__ int list[N];             // taken points from the front, left-out ones from the back
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, cuts = (p.Nk + N - 1) / N;
+    const int64_t bh = block / cuts, b = bh / p.Hk, hk = bh - b * p.Hk;
+    const int first = (int)(block - bh * cuts) * N, n = first + tid, here = min(N, p.Nk - first);
+    const float* weights = p.log_weights + b * p.log_weights_batch;
+    int before = 0, total = 0;
+#pragma unroll 16
+    for (int i = tid; i < p.Nk; i += N) {
+        const int take = !(weights[i] <= EXCLUDED);
+        total += take;
+        before += i < first ? take : 0;
+    }
+    total = __reduce_add_sync(0xffffffffu, total);
+    before = __reduce_add_sync(0xffffffffu, before);
+    const float weight = n < p.Nk ? weights[n] : -INFINITY;
+    const bool take = n < p.Nk && !(weight <= EXCLUDED);
+    const uint32_t takes = __ballot_sync(0xffffffffu, take);
+    if (lane == 0) { sums[warp][0] = total; sums[warp][1] = before; sums[warp][2] = __popc(takes); }
+    __syncthreads();
+    int rank = __popc(takes & ((1u << lane) - 1u)), m = 0;
+    total = before = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        total += sums[w][0];
+        before += sums[w][1];
+        rank += w < warp ? sums[w][2] : 0;
+        m += sums[w][2];
+    }
+    const bool apart = total <= p.Nk - p.Nk / 16;
+    const int per_row = (p.Nk + STATS_BLOCK - 1) / STATS_BLOCK;
+    if (hk == 0) {
+        if (block == bh * cuts && tid == 0) sel.taken[b] = apart ? total : p.Nk;
+        const int at = apart ? before + rank : n;
+        if (apart && take) {
+            sel.index[b * p.Nk + at] = n;
+            sel.weights[b * p.Nk + at] = weight;
+        }
+        if (s != nullptr) {
+            uint4* extra = s->weights + b * per_row * STATS_BLOCK;
+            const uint2 parts = take ? extra_parts(weight / p.scale) : make_uint2(EXTRA_OUT, 0);
+            if (apart ? take : n < per_row * STATS_BLOCK) extra[at] = make_uint4(parts.x, parts.y, 0, 0);
+            if (!apart && lane == 0 && n < per_row * STATS_BLOCK)
+                reinterpret_cast<uint32_t*>(s->gone + b * per_row)[n >> 5] = ~takes & (p.Nk - n >= 32 ? ~0u : p.Nk > n ? (1u << (p.Nk - n)) - 1u : 0u);
+            if (apart && first + N >= p.Nk && total + tid < (total + STATS_BLOCK - 1) / STATS_BLOCK * STATS_BLOCK) extra[total + tid] = make_uint4(EXTRA_OUT, 0, 0, 0);
+        }
+    }
+    if (!apart) return;
+    if (n < p.Nk) list[take ? rank : here - 1 - (tid - rank)] = n;
+    __syncthreads();
+    const int chunks = p.C / 8;
+    uint4 *k_to = static_cast<uint4*>(sel.k) + bh * p.Nk * chunks, *v_to = static_cast<uint4*>(sel.v) + bh * p.Nk * chunks;
+    auto row = [&](const View& v, int r) { return reinterpret_cast<uint4*>(static_cast<uint16_t*>(v.data) + b * v.batch + hk * v.head + r * v.point); };
+    for (int e = tid; e < m * chunks; e += N) {
+        const int r = e / chunks, c = e - r * chunks;
+        k_to[(before + r) * (int64_t)chunks + c] = row(p.k, list[r])[c];
+        v_to[(before + r) * (int64_t)chunks + c] = row(p.v, list[r])[c];
+    }
+    if (s != nullptr)
+        for (int e = tid; e < (here - m) * chunks; e += N) {
+            const int r = e / chunks, c = e - r * chunks;
+            row(p.dk, list[m + r])[c] = row(p.dv, list[m + r])[c] = make_uint4(0, 0, 0, 0);
+        }
+    if (first + N >= p.Nk) {
+        const int end = min(p.Nk, (total + 127) / 128 * 128);
+        for (int e = tid; e < (end - total) * chunks; e += N) k_to[total * (int64_t)chunks + e] = v_to[total * (int64_t)chunks + e] = make_uint4(0, 0, 0, 0);
+    }
+}
+__global__ void __launch_bounds__(SELECT_POINTS) attend_select_kernel(const __grid_constant__ Problem p, const __grid_constant__ Selection sel) {
+    allow_dependents();
+    select_points(p, sel, nullptr, blockIdx.x);
+}
+
 // ---- backward: statistics -----------------------------------------------------------------------------------------------------
 
 // Per query: D = dout . out, log2 of the sum of weights, and both as the extra rows that the tcgen05 dk/dv kernel copies.  float16: also the largest norm
 // of a row of dout and of v per key head, which bound |t - D| <= 2 |dout| |v| (the last blocks take v's rows); a maximum does not depend on the
 // order of its atomics, of which there is one per block (one per row took ten times as long as the rest).  A block takes 64 points of one head,
-// four lanes each.  The first blocks prepare the points' weights for the tcgen05 dq kernel.
+// four lanes each.  The first blocks prepare the points' weights for the tcgen05 dq kernel, or select them.
 template <typename T>
-__global__ void __launch_bounds__(256) attend_statistics_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats s, int64_t query_blocks, int64_t weight_blocks) {
+__global__ void __launch_bounds__(256) attend_statistics_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats s, const __grid_constant__ Selection sel, int64_t query_blocks,
+                                                                int64_t weight_blocks) {
     constexpr bool SCALED = SHIFT<T> != 0.f;
     __shared__ uint32_t most;
     allow_dependents();
     const int part = threadIdx.x & 3, place = threadIdx.x >> 2;
     if (blockIdx.x < weight_blocks) {
+        if (sel.taken != nullptr) {
+            select_points(p, sel, &s, blockIdx.x);
+            return;
+        }
         // one thread per point: its weight in parts, and who is left out
         const int per_row = (p.Nk + STATS_BLOCK - 1) / STATS_BLOCK, row = blockIdx.x / per_row, first = (blockIdx.x - row * per_row) * STATS_BLOCK;
         if (threadIdx.x >= STATS_BLOCK) return;
@@ -824,16 +908,21 @@ cudaError_t launch_forward(const Problem& p, sna_dtype_t dtype, int splits, floa
     });
 }
 
-cudaError_t launch_statistics(const Problem& p, const Stats& s, sna_dtype_t dtype, cudaStream_t stream) {
+cudaError_t launch_selection(const Problem& p, const Selection& sel, cudaStream_t stream) {
+    attend_select_kernel<<<(unsigned)select_blocks_of(p), SELECT_POINTS, 0, stream>>>(p, sel);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_statistics(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, cudaStream_t stream) {
     const int64_t query_blocks = query_blocks_of(p), key_blocks = (int64_t)p.B * p.Hk * ((p.Nk + STATS_BLOCK - 1) / STATS_BLOCK);
-    const int64_t weight_blocks = weight_blocks_of(p), blocks = weight_blocks + query_blocks + (dtype == SNA_FLOAT16 ? key_blocks : 0);
+    const int64_t weight_blocks = sel.taken != nullptr ? select_blocks_of(p) : weight_blocks_of(p, false), blocks = weight_blocks + query_blocks + (dtype == SNA_FLOAT16 ? key_blocks : 0);
     if (blocks == 0) return cudaSuccess;
     if (dtype == SNA_BFLOAT16) {
-        attend_statistics_kernel<__nv_bfloat16><<<(unsigned)blocks, 256, 0, stream>>>(p, s, query_blocks, weight_blocks);
+        attend_statistics_kernel<__nv_bfloat16><<<(unsigned)blocks, 256, 0, stream>>>(p, s, sel, query_blocks, weight_blocks);
     } else {
         const cudaError_t e = cudaMemsetAsync(s.norms, 0, (size_t)p.B * p.Hk * 2 * sizeof(uint32_t), stream);
         if (e != cudaSuccess) return e;
-        attend_statistics_kernel<__half><<<(unsigned)blocks, 256, 0, stream>>>(p, s, query_blocks, weight_blocks);
+        attend_statistics_kernel<__half><<<(unsigned)blocks, 256, 0, stream>>>(p, s, sel, query_blocks, weight_blocks);
     }
     return cudaGetLastError();
 }

@@ -98,8 +98,9 @@ constexpr float NOTHING = -1e31f;       // scores below belong to points left ou
 
 template <typename T, int D, bool WEIGHTS>
 __global__ void __launch_bounds__(FWD_THREADS, 1)
-attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
-                         const __grid_constant__ CUtensorMap map_v, int tiles, const __grid_constant__ Split cut, float* partials) {
+attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ Selection sel, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+                         const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CUtensorMap map_k_sel, const __grid_constant__ CUtensorMap map_v_sel, int tiles,
+                         const __grid_constant__ Split cut, float* partials) {
     using F = Forward<D>;
     allow_dependents();
     extern __shared__ unsigned char raw[];
@@ -112,8 +113,6 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
     const int part = piece.part, parts = piece.parts, tile = piece.tile, bh = piece.bh;
     const int b = bh / p.Hq, h = bh - b * p.Hq, hk = h / p.G;
     const int row0 = tile * 2 * TILE, halves = row0 + TILE < p.Nq ? 2 : 1;
-    const int blocks = (p.Nk + TILE - 1) / TILE;
-    const int first = (int)((int64_t)blocks * part / parts), count = (int)((int64_t)blocks * (part + 1) / parts) - first;
     const int steps = (p.C + 15) / 16, slabs = (p.C + 63) / 64;
     auto bar = [&](int i) { return s32(&bars[i]); };
 
@@ -140,6 +139,15 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
     const uint32_t tm = tmem_s;
     bool ok = true;
 
+    int Nk = p.Nk;
+    if (WEIGHTS) {
+        wait_for_previous();
+        if (sel.taken != nullptr) Nk = sel.taken[b];
+    }
+    const bool apart = WEIGHTS && Nk != p.Nk;
+    const int blocks = (Nk + TILE - 1) / TILE;
+    const int first = (int)((int64_t)blocks * part / parts), count = (int)((int64_t)blocks * (part + 1) / parts) - first;
+
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         if (warp == 8 && elect_one()) {
@@ -149,16 +157,17 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
                 for (int s = 0; s < slabs; ++s) tma_load(s32(base) + t * F::TILE_BYTES + s * SLAB, &map_q, s * 64, row0 + t * TILE, h, b, bar(F::Q_FULL + t));
             }
             int it = 0;
+            const CUtensorMap *keys = apart ? &map_k_sel : &map_k, *values = apart ? &map_v_sel : &map_v;
             for (; it < count && ok; ++it) {
                 const int st = it % F::STAGES, turn = it / F::STAGES;
                 if (turn > 0) ok = mb_wait(bar(F::K_FREE + st), (turn - 1) & 1, ok);
                 if (!ok) break;
                 mb_expect(bar(F::K_FULL + st), slabs * SLAB);
-                for (int s = 0; s < slabs; ++s) tma_load(s32(base) + F::OFF_K + st * F::TILE_BYTES + s * SLAB, &map_k, s * 64, (first + it) * TILE, hk, b, bar(F::K_FULL + st));
+                for (int s = 0; s < slabs; ++s) tma_load(s32(base) + F::OFF_K + st * F::TILE_BYTES + s * SLAB, keys, s * 64, (first + it) * TILE, hk, b, bar(F::K_FULL + st));
                 if (turn > 0) ok = mb_wait(bar(F::V_FREE + st), (turn - 1) & 1, ok);
                 if (!ok) break;
                 mb_expect(bar(F::V_FULL + st), slabs * SLAB);
-                for (int s = 0; s < slabs; ++s) tma_load(s32(base) + F::OFF_V + st * F::TILE_BYTES + s * SLAB, &map_v, s * 64, (first + it) * TILE, hk, b, bar(F::V_FULL + st));
+                for (int s = 0; s < slabs; ++s) tma_load(s32(base) + F::OFF_V + st * F::TILE_BYTES + s * SLAB, values, s * 64, (first + it) * TILE, hk, b, bar(F::V_FULL + st));
             }
             // the copies under way (all there already if all went well)
             for (int t = 0; t < halves; ++t) mb_wait(bar(F::Q_FULL + t), 0, true);
@@ -222,14 +231,14 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
             mb_wait(bar(F::DRAIN + (warp == 9 ? 0 : 1)), 0, true);
         } else if (WEIGHTS && warp == 10) {
             // ---------------------------------------------------------------- weights
-            const float* weights = p.log_weights == nullptr ? nullptr : p.log_weights + b * p.log_weights_batch;
+            const float* weights = apart ? sel.weights + (int64_t)b * p.Nk : p.log_weights + b * p.log_weights_batch;
             const float unscale = 1.f / p.scale;
             float w[4];
             auto fetch = [&](int it) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int n = (first + it) * TILE + i * 32 + lane;
-                    w[i] = n >= p.Nk ? -INFINITY : weights == nullptr ? 0.f : weights[n];
+                    w[i] = n >= Nk ? -INFINITY : weights[n];
                 }
             };
             if (count > 0) fetch(0);
@@ -241,7 +250,7 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const bool out = w[i] <= EXCLUDED;
-                    gone[i] = __ballot_sync(0xffffffffu, out && (first + it) * TILE + i * 32 + lane < p.Nk);
+                    gone[i] = __ballot_sync(0xffffffffu, out && (first + it) * TILE + i * 32 + lane < Nk);
                     any |= gone[i];
                     parts[i] = out ? make_uint2(EXTRA_OUT, 0) : extra_parts(w[i] * unscale);
                 }
@@ -446,8 +455,9 @@ template <int D, bool DKDV> struct Backward {
 
 template <typename T, int D, bool DKDV, bool WEIGHTS>
 __global__ void __launch_bounds__(BWD_THREADS, 1)
-attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats stats, const __grid_constant__ CUtensorMap map_a1, const __grid_constant__ CUtensorMap map_a2,
-                          const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_b2, int tiles, const __grid_constant__ Split cut, float* partials) {
+attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats stats, const __grid_constant__ Selection sel, const __grid_constant__ CUtensorMap map_a1,
+                          const __grid_constant__ CUtensorMap map_a2, const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_b2,
+                          const __grid_constant__ CUtensorMap map_k_sel, const __grid_constant__ CUtensorMap map_v_sel, int tiles, const __grid_constant__ Split cut, float* partials) {
     using K = Backward<D, DKDV>;
     constexpr bool EXTRA = DKDV || WEIGHTS;
     static_assert(BLOCK == STATS_BLOCK, "the statistics kernel's blocks");
@@ -460,36 +470,40 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     const Piece piece(cut, tiles);
     const int tile = piece.tile, bh = piece.bh;
     const int heads = DKDV ? p.Hk : p.Hq, b = bh / heads, head = bh - b * heads, hk = DKDV ? head : head / p.G;
-    const int row0 = tile * TILE, N = DKDV ? p.Nk : p.Nq, M = DKDV ? p.Nq : p.Nk;       // rows, streamed points
-    const int per_head = (M + BLOCK - 1) / BLOCK, total = DKDV ? p.G * per_head : per_head;
-    // blocks of the streamed side: `begin` and on, numbered from 0 in the pipeline
-    const int begin = (int)((int64_t)total * piece.part / piece.parts), count = (int)((int64_t)total * (piece.part + 1) / piece.parts) - begin;
-    const int steps = (p.C + 15) / 16, slabs = (p.C + 63) / 64;
-    const float* weights = p.log_weights == nullptr ? nullptr : p.log_weights + b * p.log_weights_batch;
     // The order on the stream is statistics, dq, dk and dv, joins.  dk and dv need nothing of dq: their blocks fill the SMs that its last blocks leave idle, and wait
     // for them at their end alone; by the time that they may start, every block of dq has seen the statistics complete.
     if (!DKDV) {
         wait_for_previous();
         allow_dependents();
     }
+    const int Nk = WEIGHTS && sel.taken != nullptr ? sel.taken[b] : p.Nk;
+    const bool apart = WEIGHTS && Nk != p.Nk;
+    const int row0 = tile * TILE, N = DKDV ? Nk : p.Nq, M = DKDV ? p.Nq : Nk;       // rows, streamed points
+    const int per_head = (M + BLOCK - 1) / BLOCK, total = DKDV ? p.G * per_head : per_head;
+    // blocks of the streamed side: `begin` and on, numbered from 0 in the pipeline
+    const int begin = (int)((int64_t)total * piece.part / piece.parts), count = (int)((int64_t)total * (piece.part + 1) / piece.parts) - begin;
+    const int steps = (p.C + 15) / 16, slabs = (p.C + 63) / 64;
+    const float* weights = !WEIGHTS ? nullptr : apart ? sel.weights + (int64_t)b * p.Nk : p.log_weights + b * p.log_weights_batch;
     // Whether points are left out.  dq: only then do the streamed blocks pass through the warp that clears rows.  Either side all of whose points are left out
     // gets zeros at once.
-    const int64_t weight_row = p.log_weights_batch == 0 ? 0 : b;
+    const int64_t weight_row0 = (p.log_weights_batch == 0 && sel.taken == nullptr ? 0 : (int64_t)b) * ((p.Nk + BLOCK - 1) / BLOCK);       // the first of its blocks
     bool clearing = false;
     if (WEIGHTS) {
         int gone_here = 0, present = 0;
         if (DKDV) {
             if (tid < TILE && row0 + tid < N) present = !(weights[row0 + tid] <= EXCLUDED);
+        } else if (apart) {
+            present = count > 0;
         } else {
             for (int i = tid; i < count; i += BWD_THREADS) {
-                const uint2 gone = stats.gone[weight_row * per_head + begin + i];
+                const uint2 gone = stats.gone[weight_row0 + begin + i];
                 const int left = M - (begin + i) * BLOCK;
                 const uint32_t low = left >= 32 ? ~0u : (1u << left) - 1u, high = left >= 64 ? ~0u : left <= 32 ? 0u : (1u << (left - 32)) - 1u;
                 gone_here |= (gone.x | gone.y) != 0;
                 present |= ((~gone.x & low) | (~gone.y & high)) != 0;
             }
-            clearing = __syncthreads_or(gone_here) != 0;
         }
+        if (!DKDV) clearing = __syncthreads_or(gone_here) != 0;
         if (__syncthreads_or(present) == 0) {
             const int chunks = p.C / 8;
             for (int e = tid; e < TILE * chunks; e += BWD_THREADS) {
@@ -503,7 +517,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                         to[0] = to[1] = make_float4(0.f, 0.f, 0.f, 0.f);
                     } else {
                         const View& v = DKDV ? (which == 0 ? p.dk : p.dv) : p.dq;
-                        *reinterpret_cast<uint4*>(static_cast<T*>(v.data) + b * v.batch + head * v.head + row * v.point + c) = make_uint4(0, 0, 0, 0);
+                        *reinterpret_cast<uint4*>(static_cast<T*>(v.data) + b * v.batch + head * v.head + row * v.point + c) = make_uint4(0, 0, 0, 0);       // (in place: not apart)
                     }
                 }
             }
@@ -538,12 +552,14 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     if (warp >= 16) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == 16 && elect_one()) {
+            const CUtensorMap *a1 = DKDV && apart ? &map_k_sel : &map_a1, *a2 = DKDV && apart ? &map_v_sel : &map_a2;
+            const CUtensorMap *b1 = !DKDV && apart ? &map_k_sel : &map_b1, *b2 = !DKDV && apart ? &map_v_sel : &map_b2;
             // ---------------------------------------------------------------- TMA
             if (!K::A_IN_TMEM) {
                 mb_expect(bar(K::A_FULL), 2 * slabs * SLAB);
                 for (int s = 0; s < slabs; ++s) {
-                    tma_load(s32(base) + s * SLAB, &map_a1, s * 64, row0, head, b, bar(K::A_FULL));
-                    tma_load(s32(base) + (K::SLABS + s) * SLAB, &map_a2, s * 64, row0, head, b, bar(K::A_FULL));
+                    tma_load(s32(base) + s * SLAB, a1, s * 64, row0, head, b, bar(K::A_FULL));
+                    tma_load(s32(base) + (K::SLABS + s) * SLAB, a2, s * 64, row0, head, b, bar(K::A_FULL));
                 }
             }
             int it = 0;
@@ -556,10 +572,10 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                 if (DKDV)
                     bulk_load(s32(base) + K::OFF_XB + st * 2 * K::EXTRA_B, stats.extra + (((int64_t)b * p.Hq + h) * per_head + point / BLOCK) * 2 * BLOCK, 2 * K::EXTRA_B, bar(K::FULL + st));
                 else if (EXTRA)
-                    bulk_load(s32(base) + K::OFF_XB + st * K::EXTRA_B, stats.weights + (weight_row * per_head + point / BLOCK) * BLOCK, K::EXTRA_B, bar(K::FULL + st));
+                    bulk_load(s32(base) + K::OFF_XB + st * K::EXTRA_B, stats.weights + (weight_row0 + point / BLOCK) * BLOCK, K::EXTRA_B, bar(K::FULL + st));
                 for (int s = 0; s < slabs; ++s) {
-                    tma_load(stage(st) + s * BSLAB, &map_b1, s * 64, point, h, b, bar(K::FULL + st));
-                    tma_load(stage(st) + (K::SLABS + s) * BSLAB, &map_b2, s * 64, point, h, b, bar(K::FULL + st));
+                    tma_load(stage(st) + s * BSLAB, b1, s * 64, point, h, b, bar(K::FULL + st));
+                    tma_load(stage(st) + (K::SLABS + s) * BSLAB, b2, s * 64, point, h, b, bar(K::FULL + st));
                 }
             }
             // the copies under way (all there already if all went well)
@@ -612,7 +628,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             ok = all_lanes(mb_wait(bar(K::A_FULL), 0, ok));
             for (int r = 0; r < 4 && ok; ++r) {
                 const int n = row0 + r * 32 + lane;
-                const uint32_t gone = __ballot_sync(0xffffffffu, n < p.Nk && weight2(weights, n) == -INFINITY);
+                const uint32_t gone = __ballot_sync(0xffffffffu, n < Nk && weight2(weights, n) == -INFINITY);
                 for (int which = 0; which < 2; ++which) zero_rows(base + which * K::SLABS * SLAB, slabs, SLAB, r, gone, lane);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -620,7 +636,7 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             if (lane == 0) mb_arrive(bar(K::A_READY));
         } else if (clearing && warp == 18) {
             // ---------------------------------------------------------------- rows of streamed points left out
-            const uint2* gone = stats.gone + weight_row * per_head + begin;
+            const uint2* gone = stats.gone + weight_row0 + begin;
             uint2 next = gone[0];
             for (int it = 0; it < count && ok; ++it) {
                 const int st = it % K::STAGES;
@@ -658,7 +674,8 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
         }
         if (K::A_IN_TMEM) {
             const View& v = DKDV ? (group == 0 ? p.k : p.v) : (group == 0 ? p.q : p.dout);
-            const uint4* from = reinterpret_cast<const uint4*>(static_cast<const T*>(v.data) + b * v.batch + head * v.head + (there ? row : 0) * v.point);
+            const int point = !there ? 0 : DKDV && apart ? sel.index[(int64_t)b * p.Nk + row] : row;
+            const uint4* from = reinterpret_cast<const uint4*>(static_cast<const T*>(v.data) + b * v.batch + head * v.head + point * v.point);
 #pragma unroll
             for (int part = 0; part < D / 64; ++part) {
                 const int c = half * (D / 2) + part * 32;
@@ -741,7 +758,8 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
             const float unshift = ex2(-SHIFT<T>), back = DKDV && group == 1 ? unshift : p.scale * unshift / factor;
             const bool zero = DKDV && !taken;       // (exponentials on the FMA pipe end at 2^-126)
             const View& v = DKDV ? (group == 0 ? p.dk : p.dv) : p.dq;
-            T* out = static_cast<T*>(v.data) + b * v.batch + head * v.head + (int64_t)row * v.point;
+            const int64_t point = DKDV && apart && there ? sel.index[(int64_t)b * p.Nk + row] : row;
+            T* out = static_cast<T*>(v.data) + b * v.batch + head * v.head + point * v.point;
             for (int c = 32 * (DKDV ? half : 2 * half + group); c < p.C; c += DKDV ? 64 : 128) {
                 uint32_t o[32];
                 tm_ld32(o, tm + K::T_ACC + (DKDV ? group * D : 0) + c + lanes);
@@ -789,6 +807,7 @@ struct Join {
     Split cut;
     int64_t threads;
     int tiles, rows_per_tile, N, H;
+    const int *taken, *index;   // dk, dv: the selection's, or null
 };
 struct Joins {
     Join join[3];
@@ -803,9 +822,14 @@ __global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const _
     const int c = (int)(index - local * chunks) * 8;
     if (index >= j.threads) return;
     const int64_t tile = j.cut.full + local / j.rows_per_tile, bh = tile / j.tiles, b = bh / j.H, h = bh - b * j.H;
-    const int n = (int)(tile - bh * j.tiles) * j.rows_per_tile + (int)(local % j.rows_per_tile);
+    int n = (int)(tile - bh * j.tiles) * j.rows_per_tile + (int)(local % j.rows_per_tile);
     wait_for_previous();
     if (n >= j.N) return;
+    if (j.taken != nullptr) {
+        const int taken = j.taken[b];
+        if (n >= taken) return;
+        if (taken != j.N) n = j.index[b * j.N + n];
+    }
     const float* statistics = j.partials + parts * rest * C + local;
     float top = -INFINITY, total = 0.f;
     if (SOFTMAX)
@@ -833,9 +857,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const _
               j.rest.data == nullptr ? nullptr : static_cast<T*>(j.rest.data) + b * j.rest.batch + h * j.rest.head + n * j.rest.point + c, sum);
     if (SOFTMAX && c == 0 && a.lse != nullptr) a.lse[bh * j.N + n] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
 }
-Join join_of(const View& out, const View& rest, const Split& cut, int rows_per_tile, int N, int H, int C, const float* partials) {
+Join join_of(const View& out, const View& rest, const Split& cut, int rows_per_tile, int N, int H, int C, const float* partials, const Selection& sel) {
     const int64_t threads = cut.parts > 1 ? cut.rest() * rows_per_tile * (C / 8) : 0;
-    return Join{out, rest, partials, cut, threads, (N + rows_per_tile - 1) / rows_per_tile, rows_per_tile, N, H};
+    return Join{out, rest, partials, cut, threads, (N + rows_per_tile - 1) / rows_per_tile, rows_per_tile, N, H, sel.taken, sel.index};
 }
 template <typename T, bool SOFTMAX>
 cudaError_t launch_joins(const Joins& a, cudaStream_t stream) {
@@ -870,44 +894,57 @@ cudaError_t allow(K kernel, size_t bytes, std::atomic<uint64_t>& done) {
 }
 
 template <typename T, int D, bool WEIGHTS>
-cudaError_t forward_as(const Problem& p, const CUtensorMap (&maps)[3], const Split& cut, float* partials, cudaStream_t stream) {
+cudaError_t forward_as(const Problem& p, const Selection& sel, const CUtensorMap (&maps)[5], const Split& cut, float* partials, cudaStream_t stream) {
     const int tiles = (p.Nq + 2 * TILE - 1) / (2 * TILE);
     const auto kernel = attend_forward_tc_kernel<T, D, WEIGHTS>;
     static std::atomic<uint64_t> allowed{0};
     cudaError_t e = allow(kernel, Forward<D>::SMEM, allowed);
     if (e != cudaSuccess) return e;
-    kernel<<<(unsigned)cut.blocks(), FWD_THREADS, Forward<D>::SMEM, stream>>>(p, maps[0], maps[1], maps[2], tiles, cut, partials);
-    e = cudaGetLastError();
+    const bool selected = sel.taken != nullptr;
+    if (selected) e = launch_selection(p, sel, stream);
+    if (e != cudaSuccess) return e;
+    if (selected) {
+        e = launch_dependent(kernel, (unsigned)cut.blocks(), FWD_THREADS, Forward<D>::SMEM, stream, p, sel, maps[0], maps[1], maps[2], maps[3], maps[4], tiles, cut, partials);
+    } else {
+        kernel<<<(unsigned)cut.blocks(), FWD_THREADS, Forward<D>::SMEM, stream>>>(p, sel, maps[0], maps[1], maps[2], maps[3], maps[4], tiles, cut, partials);
+        e = cudaGetLastError();
+    }
     if (e != cudaSuccess) return e;
     Joins joins{};
-    joins.join[0] = join_of(p.out, p.rest, cut, 2 * TILE, p.Nq, p.Hq, p.C, partials);
+    joins.join[0] = join_of(p.out, p.rest, cut, 2 * TILE, p.Nq, p.Hq, p.C, partials, Selection{});
     joins.lse = p.lse;
     joins.C = p.C;
     return launch_joins<T, true>(joins, stream);
 }
 
 template <typename T, int D, bool DKDV, bool WEIGHTS>
-cudaError_t backward_as(const Problem& p, const Stats& s, const CUtensorMap (&maps)[4], const Split& cut, float* partials, cudaStream_t stream) {
+cudaError_t backward_as(const Problem& p, const Stats& s, const Selection& sel, const CUtensorMap (&maps)[6], const Split& cut, float* partials, cudaStream_t stream) {
     const int tiles = ((DKDV ? p.Nk : p.Nq) + TILE - 1) / TILE;
     const auto kernel = attend_backward_tc_kernel<T, D, DKDV, WEIGHTS>;
     static std::atomic<uint64_t> allowed{0};
     cudaError_t e = allow(kernel, Backward<D, DKDV>::SMEM, allowed);
     if (e != cudaSuccess) return e;
-    return launch_dependent(kernel, (unsigned)cut.blocks(), BWD_THREADS, Backward<D, DKDV>::SMEM, stream, p, s, maps[0], maps[1], maps[2], maps[3], tiles, cut, partials);
+    return launch_dependent(kernel, (unsigned)cut.blocks(), BWD_THREADS, Backward<D, DKDV>::SMEM, stream, p, s, sel, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], tiles, cut, partials);
+}
+// Maps of the selected keys and values (untouched and unread without a selection).
+bool make_selected(CUtensorMap* maps, const Problem& p, const Selection& sel, sna_dtype_t dtype, int rows) {
+    if (sel.taken == nullptr) return true;
+    return make_map(&maps[0], selected_view(p, sel.k), dtype, p.C, p.Nk, p.Hk, p.B, rows) && make_map(&maps[1], selected_view(p, sel.v), dtype, p.C, p.Nk, p.Hk, p.B, rows);
 }
 template <bool DKDV>
-bool backward_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
+bool backward_tc(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
     const Split cut = split_of(p, DKDV ? Kernel::DKDV : Kernel::DQ, sms);
-    CUtensorMap maps[4];        // A1, A2 (boxes of a tile), B1, B2 (of a block)
+    CUtensorMap maps[6];        // A1, A2 (boxes of a tile), B1, B2 (of a block), the selected keys and values
     const int q_rows = DKDV ? BLOCK : TILE, k_rows = DKDV ? TILE : BLOCK, q_at = DKDV ? 2 : 0, k_at = 2 - q_at;
     if (!make_map(&maps[q_at], p.q, dtype, p.C, p.Nq, p.Hq, p.B, q_rows) || !make_map(&maps[q_at + 1], p.dout, dtype, p.C, p.Nq, p.Hq, p.B, q_rows) ||
-        !make_map(&maps[k_at], p.k, dtype, p.C, p.Nk, p.Hk, p.B, k_rows) || !make_map(&maps[k_at + 1], p.v, dtype, p.C, p.Nk, p.Hk, p.B, k_rows))
+        !make_map(&maps[k_at], p.k, dtype, p.C, p.Nk, p.Hk, p.B, k_rows) || !make_map(&maps[k_at + 1], p.v, dtype, p.C, p.Nk, p.Hk, p.B, k_rows) ||
+        !make_selected(&maps[4], p, sel, dtype, k_rows))
         return false;
     const bool weights = p.log_weights != nullptr;
     auto run = [&](auto t, auto width) {
         using T = decltype(t);
         constexpr int D = decltype(width)::value;
-        return weights ? backward_as<T, D, DKDV, true>(p, s, maps, cut, partials, stream) : backward_as<T, D, DKDV, false>(p, s, maps, cut, partials, stream);
+        return weights ? backward_as<T, D, DKDV, true>(p, s, sel, maps, cut, partials, stream) : backward_as<T, D, DKDV, false>(p, s, sel, maps, cut, partials, stream);
     };
     using W64 = std::integral_constant<int, 64>;
     using W128 = std::integral_constant<int, 128>;
@@ -918,11 +955,11 @@ bool backward_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, f
 
 }  // namespace
 
-bool backward_dq_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
-    return backward_tc<false>(p, s, dtype, sms, partials, stream, e);
+bool backward_dq_tc(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
+    return backward_tc<false>(p, s, sel, dtype, sms, partials, stream, e);
 }
-bool backward_dkdv_tc(const Problem& p, const Stats& s, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
-    return backward_tc<true>(p, s, dtype, sms, partials, stream, e);
+bool backward_dkdv_tc(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
+    return backward_tc<true>(p, s, sel, dtype, sms, partials, stream, e);
 }
 
 // Pieces of each of `rest` tiles, where the SMs have a partial wave of them (see Split).
@@ -951,12 +988,12 @@ Split split_of(const Problem& p, Kernel kernel, int sms) {
     return cut;
 }
 
-cudaError_t join_backward(const Problem& p, sna_dtype_t dtype, int sms, const float* dq_partials, const float* dkdv_partials, cudaStream_t stream) {
+cudaError_t join_backward(const Problem& p, const Selection& sel, sna_dtype_t dtype, int sms, const float* dq_partials, const float* dkdv_partials, cudaStream_t stream) {
     const Split q = split_of(p, Kernel::DQ, sms), k = split_of(p, Kernel::DKDV, sms);
     Joins joins{};
-    joins.join[0] = join_of(p.dq, View{}, q, TILE, p.Nq, p.Hq, p.C, dq_partials);
-    joins.join[1] = join_of(p.dk, View{}, k, TILE, p.Nk, p.Hk, p.C, dkdv_partials);
-    joins.join[2] = join_of(p.dv, View{}, k, TILE, p.Nk, p.Hk, p.C, dkdv_partials + k.parts * k.rest() * TILE * p.C);
+    joins.join[0] = join_of(p.dq, View{}, q, TILE, p.Nq, p.Hq, p.C, dq_partials, Selection{});
+    joins.join[1] = join_of(p.dk, View{}, k, TILE, p.Nk, p.Hk, p.C, dkdv_partials, sel);
+    joins.join[2] = join_of(p.dv, View{}, k, TILE, p.Nk, p.Hk, p.C, dkdv_partials + k.parts * k.rest() * TILE * p.C, sel);
     joins.C = p.C;
     return dtype == SNA_BFLOAT16 ? launch_joins<__nv_bfloat16, false>(joins, stream) : launch_joins<__half, false>(joins, stream);
 }
@@ -979,17 +1016,17 @@ bool make_map(CUtensorMap* map, const View& v, sna_dtype_t dtype, int C, int N, 
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool forward_tc(const Problem& p, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
+bool forward_tc(const Problem& p, const Selection& sel, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
     const Split cut = split_of(p, Kernel::FORWARD, sms);
-    CUtensorMap maps[3];
+    CUtensorMap maps[5];        // queries, keys, values, the selected keys and values
     if (!make_map(&maps[0], p.q, dtype, p.C, p.Nq, p.Hq, p.B, TILE) || !make_map(&maps[1], p.k, dtype, p.C, p.Nk, p.Hk, p.B, TILE) ||
-        !make_map(&maps[2], p.v, dtype, p.C, p.Nk, p.Hk, p.B, TILE))
+        !make_map(&maps[2], p.v, dtype, p.C, p.Nk, p.Hk, p.B, TILE) || !make_selected(&maps[3], p, sel, dtype, TILE))
         return false;
     const bool weights = p.log_weights != nullptr;
     auto run = [&](auto t, auto width) {
         using T = decltype(t);
         constexpr int D = decltype(width)::value;
-        return weights ? forward_as<T, D, true>(p, maps, cut, partials, stream) : forward_as<T, D, false>(p, maps, cut, partials, stream);
+        return weights ? forward_as<T, D, true>(p, sel, maps, cut, partials, stream) : forward_as<T, D, false>(p, sel, maps, cut, partials, stream);
     };
     using W64 = std::integral_constant<int, 64>;
     using W128 = std::integral_constant<int, 128>;

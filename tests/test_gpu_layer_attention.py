@@ -462,3 +462,50 @@ def test_a_pending_negation_is_refused_and_that_of_a_gradient_taken():
     state = layer.dropout_state("cuda")
     for f in (lambda: layer.weighted_attention(q, k, v), lambda: layer.qk_norm_rotate(q, k, w)[0], lambda: layer.residual_dropout(q, state, 0.5)):
         assert torch.equal(torch.autograd.grad(f(), q, pending)[0], torch.autograd.grad(f(), q, -g)[0])
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=lambda d: str(d).split(".")[1])
+@pytest.mark.parametrize("shape", [(3, 8, 2, 5500, 1030, 40), (2, 16, 2, 2100, 2049, 64), (12, 8, 4, 2000, 700, 128), (1, 16, 1, 135, 62200, 24), (20, 10, 2, 10600, 64, 8)],
+                         ids=lambda s: "-".join(map(str, s)))
+@pytest.mark.parametrize("order", ["plain", "packed"])
+@pytest.mark.parametrize("shared", [False, True], ids=["per field", "shared"])
+def test_many_points_left_out(shape, dtype, order, shared):
+    # the points that take part are brought together where a sixteenth of a field's or more is left out, if there is work enough (2^27 pairs of a row and a point):
+    # fields on either side of that, without any points, with one, some or all of them
+    B, Hq, Hk, Nq, Nk, C = shape
+    torch.manual_seed(Nk)
+    q, k, v = heads(B, Hq, (1, Nq), C, dtype, order), heads(B, Hk, (1, Nk), C, dtype, order), heads(B, Hk, (1, Nk), C, dtype, order)
+    w = torch.randn(1 if shared else B, Nk, device="cuda")
+    left = [Nk // 2, 0, Nk - Nk // 16 + 1, 1, Nk, min(Nk, 128), min(Nk, 129), 64, 1 + Nk // 3, Nk - Nk // 16]
+    for case in range(0, len(left), 1 if shared else B):
+        out_of = torch.ones(w.shape, dtype=torch.bool, device="cuda")
+        for b in range(w.shape[0]):
+            out_of[b, torch.randperm(Nk, device="cuda")[:left[(case + b) % len(left)]]] = False
+        gone = out_of.expand(B, Nk)[:, None, None, :, None]
+        kk, vv = k.masked_fill(gone, math.nan), v.masked_fill(gone, math.inf)
+        out, lse, (dq, dk, dv) = check(q, kk, vv, w.masked_fill(out_of, -math.inf))
+        assert not bool(dk.masked_select(gone).any()) and not bool(dv.masked_select(gone).any())
+        none = out_of.all(1).expand(B)
+        assert not bool(out[none].any()) and not bool(dq[none].any())
+
+
+def test_rows_of_a_selection_in_a_captured_graph():
+    # the same graph with other masks: nothing of the selection is decided on the host
+    torch.manual_seed(21)
+    B, H, N, C = 2, 4, 4200, 32
+    ends = [heads(B, H, (1, N), C, torch.bfloat16).requires_grad_() for _ in range(3)]
+    g = heads(B, H, (1, N), C, torch.bfloat16)
+    w = torch.zeros(B, N, device="cuda")
+    step = lambda: (lambda out: (out.detach(), *torch.autograd.grad(out, ends, g)))(layer.weighted_attention(*ends, w))
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for share in (0.0, 0.5, 0.03, 1.0, 0.9):
+        w.copy_(torch.randn(B, N, device="cuda").masked_fill(torch.rand(B, N, device="cuda") < share, -math.inf))
+        graph.replay()
+        got = [t.clone() for t in captured]
+        assert all(torch.equal(a, b) for a, b in zip(got, step()))
