@@ -509,3 +509,28 @@ def test_rows_of_a_selection_in_a_captured_graph():
         graph.replay()
         got = [t.clone() for t in captured]
         assert all(torch.equal(a, b) for a, b in zip(got, step()))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=lambda d: str(d).split(".")[1])
+@pytest.mark.parametrize("shape", [(2, 4, 2, 800, 1203, 8), (1, 2, 2, 900, 1100, 16), (1, 1, 1, 33, 9800, 32), (2, 2, 1, 300, 406, 64), (1, 2, 2, 260, 1000, 128), (1, 3, 3, 10, 40, 40)],
+                         ids=lambda s: "-".join(map(str, s)))
+@pytest.mark.parametrize("weighted", [False, True])
+def test_gradients_of_narrow_heads_and_small_problems_round_once(shape, weighted, dtype):
+    # p and ds in two 16-bit parts: their second rounding is off by u^2 of the term (as is the product of the first's remainder and that), so that dv is off by half a
+    # step of the result and what 32-bit sums and exponentials lose
+    B, Hq, Hk, Nq, Nk, C = shape
+    torch.manual_seed(Nk)
+    q, k, v = heads(B, Hq, (1, Nq), C, dtype), heads(B, Hk, (1, Nk), C, dtype), heads(B, Hk, (1, Nk), C, dtype)
+    w = torch.randn(Nk, device="cuda") if weighted else None
+    check(q, k, v, w)
+    dout = heads(B, Hq, (1, Nq), C, dtype)
+    ends = [x.detach().requires_grad_() for x in (q, k, v)]
+    dv = torch.autograd.grad(layer.weighted_attention(*ends, w), ends[2], dout)[0]
+    values, _, _, d_lse = reference(q, k, v, w, C ** -0.5, dout)
+    u = torch.finfo(dtype).eps / 2
+    flat = lambda x: x.double().reshape(B, Hk, -1, C)
+    s = flat(q) @ flat(k).transpose(2, 3) * C ** -0.5 + (0 if w is None else w.double())
+    terms = (torch.softmax(s, -1).transpose(2, 3) @ flat(dout).abs()).reshape(dv.shape)
+    least = 2.0 ** -38 if dtype == torch.float16 else 2.0 ** -126
+    tol = terms * (2 * u * u + 2 * d_lse) + least * flat(dout).abs().sum(2, keepdim=True).reshape(B, Hk, 1, 1, C) + u * (1 + u) * values[3].abs()
+    close(dv, values[3], tol, "dv")
