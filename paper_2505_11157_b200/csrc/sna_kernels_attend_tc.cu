@@ -817,7 +817,8 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
 
 // ---- joins of tiles in pieces ---------------------------------------------------------------------------------------------------
 //
-// A thread takes eight channels of a row; the pieces are taken in their order.  forward: out = sum_s 2^(lse2_s - lse2) out_s; backward: plain sums, of dq, dk and dv
+// A thread takes eight channels of a row; many pieces are shared by up to 32 lanes, whose sums a tree joins: the order is fixed.  (One head of 32, 33 queries, 65536
+// points, bf16, 148 pieces: forward pass 60 us with one lane.)  forward: out = sum_s 2^(lse2_s - lse2) out_s; backward: plain sums, of dq, dk and dv
 // in one launch.
 constexpr int JOIN_THREADS = 256;
 struct Join {
@@ -825,6 +826,7 @@ struct Join {
     const float* partials;
     Split cut;
     int64_t threads;
+    int lanes;                  // a power of two
     int tiles, rows_per_tile, N, H;
     const int *taken, *index;   // dk, dv: the selection's, or null
 };
@@ -836,10 +838,12 @@ struct Joins {
 template <typename T, bool SOFTMAX>
 __global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const __grid_constant__ Joins a) {
     const Join& j = a.join[SOFTMAX ? 0 : blockIdx.y];
-    const int C = a.C, chunks = C / 8, parts = j.cut.parts;
-    const int64_t rest = j.cut.rest() * j.rows_per_tile, index = (int64_t)blockIdx.x * JOIN_THREADS + threadIdx.x, local = index / chunks;
+    const int C = a.C, chunks = C / 8, parts = j.cut.parts, lanes = j.lanes, lane = threadIdx.x & (lanes - 1);
+    const int64_t thread = (int64_t)blockIdx.x * JOIN_THREADS + threadIdx.x;
+    if (thread >= j.threads) return;        // (here and below: all lanes of an item)
+    const int64_t rest = j.cut.rest() * j.rows_per_tile, index = thread / lanes, local = index / chunks;
     const int c = (int)(index - local * chunks) * 8;
-    if (index >= j.threads) return;
+    const uint32_t mates = (lanes == 32 ? ~0u : (1u << lanes) - 1u) << (threadIdx.x & 31 & ~(lanes - 1));
     const int64_t tile = j.cut.full + local / j.rows_per_tile, bh = tile / j.tiles, b = bh / j.H, h = bh - b * j.H;
     int n = (int)(tile - bh * j.tiles) * j.rows_per_tile + (int)(local % j.rows_per_tile);
     wait_for_previous();
@@ -851,13 +855,15 @@ __global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const _
     }
     const float* statistics = j.partials + parts * rest * C + local;
     float top = -INFINITY, total = 0.f;
-    if (SOFTMAX)
+    if (SOFTMAX) {
 #pragma unroll 4
-        for (int s = 0; s < parts; ++s) top = fmaxf(top, statistics[s * rest]);
+        for (int s = lane; s < parts; s += lanes) top = fmaxf(top, statistics[s * rest]);
+        for (int o = lanes >> 1; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(mates, top, o));
+    }
     const float base = top == -INFINITY ? 0.f : top;
     float sum[8] = {};
 #pragma unroll 4
-    for (int s = 0; s < parts; ++s) {
+    for (int s = lane; s < parts; s += lanes) {
         float w = 1.f;
         if (SOFTMAX) {
             w = ex2(statistics[s * rest] - base);
@@ -869,6 +875,12 @@ __global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const _
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] = fmaf(w, v[i], sum[i]);
     }
+    for (int o = lanes >> 1; o > 0; o >>= 1) {
+        if (SOFTMAX) total += __shfl_xor_sync(mates, total, o);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += __shfl_xor_sync(mates, sum[i], o);
+    }
+    if (lane != 0) return;
     const float factor = !SOFTMAX ? 1.f : total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] *= factor;
@@ -877,8 +889,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) attend_join_tiles_kernel(const _
     if (SOFTMAX && c == 0 && a.lse != nullptr) a.lse[bh * j.N + n] = total == 0.f ? -INFINITY : (top + log2f(total)) * LN2;
 }
 Join join_of(const View& out, const View& rest, const Split& cut, int rows_per_tile, int N, int H, int C, const float* partials, const Selection& sel) {
-    const int64_t threads = cut.parts > 1 ? cut.rest() * rows_per_tile * (C / 8) : 0;
-    return Join{out, rest, partials, cut, threads, (N + rows_per_tile - 1) / rows_per_tile, rows_per_tile, N, H, sel.taken, sel.index};
+    int lanes = 1;
+    while (lanes < 32 && lanes * 4 < cut.parts) lanes *= 2;
+    const int64_t threads = cut.parts > 1 ? cut.rest() * rows_per_tile * (C / 8) * lanes : 0;
+    return Join{out, rest, partials, cut, threads, lanes, (N + rows_per_tile - 1) / rows_per_tile, rows_per_tile, N, H, sel.taken, sel.index};
 }
 template <typename T, bool SOFTMAX>
 cudaError_t launch_joins(const Joins& a, cudaStream_t stream) {
