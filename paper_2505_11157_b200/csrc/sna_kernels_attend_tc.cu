@@ -1022,6 +1022,17 @@ Split split_of(const Problem& p, Kernel kernel, int sms) {
     const int64_t keys = up(p.Nk, BLOCK), queries = p.G * up(p.Nq, BLOCK);
     // dq's and dk/dv's blocks run side by side, so theirs is one last wave, dk's and dv's; dq is cut only if both together are less than a wave
     const int64_t tiles = kernel == Kernel::FORWARD ? forward : kernel == Kernel::DQ ? dq : dkdv, all = kernel == Kernel::FORWARD ? forward : dq + dkdv;
+    if (kernel == Kernel::DQ || (kernel == Kernel::DKDV && all >= 8 * (int64_t)sms)) {
+        // Few queries and many points, or the reverse: what one side's tiles walk is longer than an SM's share of the work, in blocks (a tile's start and end take as long
+        // as about ten), dk's and dv's of what is left when they start.  Its tiles are cut to that (dk's and dv's in a few waves are cut below anyway).  (us, backward, bf16: 33
+        // queries, 9800 points, one head of 32, tiles whole 81, cut 12; B = 2, 17 queries, 60000 points, 8 and 2 heads of 64 498, 210; 60000 queries, 64 points, 16 heads of 64
+        // 852, 543.)
+        const bool is_dq = kernel == Kernel::DQ;
+        const int64_t length = is_dq ? keys : queries, other = is_dq ? queries : keys, ends = 10;
+        const int64_t share = std::max<int64_t>(1, ((is_dq ? dq * (keys + ends) : 0) + dkdv * (queries + ends)) / sms);
+        const int64_t parts = std::min(length / 4, up(length, std::max<int64_t>(4, share - ends)));
+        if (length > 2 * other && length + ends > 2 * share && parts > 1) return Split{tiles, 0, (int)parts};
+    }
     const int64_t rest = std::min(all % sms, tiles);
     Split cut{tiles, tiles, 1};
     if (rest == 0 || all >= 8 * (int64_t)sms || (kernel == Kernel::DQ && all >= sms)) return cut;

@@ -534,3 +534,17 @@ def test_gradients_of_narrow_heads_and_small_problems_round_once(shape, weighted
     least = 2.0 ** -38 if dtype == torch.float16 else 2.0 ** -126
     tol = terms * (2 * u * u + 2 * d_lse) + least * flat(dout).abs().sum(2, keepdim=True).reshape(B, Hk, 1, 1, C) + u * (1 + u) * values[3].abs()
     close(dv, values[3], tol, "dv")
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=lambda d: str(d).split(".")[1])
+@pytest.mark.parametrize("shape", [(1, 1, 1, 33, 9800, 32), (2, 4, 1, 17, 20011, 64), (1, 2, 2, 20011, 65, 40), (1, 4, 1, 9001, 130, 128), (2, 3, 3, 129, 5000, 96), (1, 16, 8, 9800, 64, 8)],
+                         ids=lambda s: "-".join(map(str, s)))
+@pytest.mark.parametrize("share", [0.0, 0.5])
+def test_long_and_narrow_problems(shape, share, dtype):
+    # one side's tiles are cut into pieces, over whole ranges of points left out too
+    B, Hq, Hk, Nq, Nk, C = shape
+    torch.manual_seed(Nk)
+    q, k, v = heads(B, Hq, (1, Nq), C, dtype), heads(B, Hk, (1, Nk), C, dtype), heads(B, Hk, (1, Nk), C, dtype)
+    w = torch.randn(B, Nk, device="cuda").masked_fill(torch.rand(B, Nk, device="cuda") < share, -math.inf)
+    w[0, Nk // 8: Nk // 8 + int(share * Nk)] = -math.inf
+    check(q, k, v, w)
