@@ -32,6 +32,7 @@ __device__ __forceinline__ float ex2(float x) { float y; asm("ex2.approx.ftz.f32
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, bool take) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(take ? 16 : 0) : "memory");
 }
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory"); }
 __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void ldsm(uint32_t (&r)[4], uint32_t addr) {
@@ -94,6 +95,20 @@ template <int CP> __device__ __forceinline__ void load_bt(uint32_t (&b)[4], uint
     ldsm_t(b, tile + piece<CP>(k0 + (lane & 7) + (((lane >> 3) & 1) << 3), n * 2 + (lane >> 4)));
 }
 
+// One warp's share of such a load: R rows, of which a lane's pieces lie fewer rows apart than the permutation's period.
+template <int CP, int R, typename T, typename Take>
+__device__ __forceinline__ void load_rows_by_warp(uint32_t tile, const T* head, int64_t point, int first, int C, int lane, Take take) {
+    constexpr int CH = CP / 8, RP = 32 / CH;
+    const int r0 = lane / CH, c = lane - r0 * CH;
+    const T* src = head + (first + r0) * point + c * 8;
+    const bool channel = c * 8 < C;
+#pragma unroll
+    for (int i = 0; i < R / RP; ++i) {
+        const bool there = channel && take(r0 + i * RP);
+        copy16(tile + piece<CP>(r0 + i * RP, c), there ? src : head, there);
+        src += RP * point;
+    }
+}
 // rows [first, first + R) of a head's points (stride `point`); a row that is not there, or for which take(row in tile) is false, is zero.
 // A thread's pieces lie RP rows apart, which is a multiple of the permutation's period: one address each way, and steps.  take also sees to rows
 // behind the last point.
@@ -151,7 +166,7 @@ template <typename T, int CP, int WM>
 __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_forward_kernel(const __grid_constant__ Problem p, int tiles, int splits, float* partials) {
     constexpr int STAGES = FORWARD_STAGES<WM>, WK = WARPS / WM, BM = 16 * WM, KW = BN / WK, NT = KW / 8, CN = CP / 8;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ __align__(16) float bias[4][BN];
+    __shared__ __align__(16) float bias[8][BN];
     const uint32_t tq = s32(smem), tkv = tq + BM * CP * 2;      // stages of (K, V)
     allow_dependents();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, wm = warp % WM, wk = warp / WM;
@@ -164,30 +179,47 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
     const int blocks = (p.Nk + BN - 1) / BN;
     const int first = (int)((int64_t)blocks * split / splits), last = (int)((int64_t)blocks * (split + 1) / splits);
 
-    // a weight is read one step before it is stored, so that no step waits for it
-    float weight = -INFINITY;
-    auto fetch_bias = [&](int j) {
-        if (tid < BN) {
-            const int n = j * BN + tid;
-            weight = j < last && n < p.Nk ? weight2(weights, n) : -INFINITY;
-        }
+    // few rows: a warp loads the 16 keys of a block that it takes itself, and waits for no other (one station as above, warps in step: 52 us without the join)
+    constexpr bool APART = WK == WARPS;
+    const int key0 = wk * KW, mine = APART ? (lane < KW ? key0 + lane : BN) : tid;
+    auto in_step = [&] {
+        if (APART) __syncwarp();
+        else __syncthreads();
     };
-    auto store_bias = [&](int j) {
-        if (tid < BN) bias[j & 3][tid] = weight;
+    // Weights come by asynchronous copies 2 STAGES blocks ahead, and are made ready (log2, -infinity for points left out) STAGES ahead, in place: the loads of a
+    // block's keys and values go by them.  (Read into a register one step ahead, they were what the steps waited for: one station over 361x720, B = 2, 2 key heads
+    // of 32, bf16: 47 us with weights, 35 without.)
+    auto ready = [&](int j, float raw) { return j >= last || j * BN + mine >= p.Nk ? -INFINITY : weights == nullptr ? 0.f : raw <= EXCLUDED ? -INFINITY : raw * LOG2E; };
+    auto copy_bias = [&](int j) {
+        if (weights != nullptr && mine < BN && j < last && j * BN + mine < p.Nk) copy4(s32(&bias[j & 7][mine]), weights + j * BN + mine);
+    };
+    auto ready_bias = [&](int j) {
+        if (mine < BN) bias[j & 7][mine] = ready(j, bias[j & 7][mine]);
     };
     auto load_block = [&](int j) {
         if (j < last) {
-            auto take = [&](int r) { return bias[j & 3][r] != -INFINITY; };
             const uint32_t stage = tkv + ((j - first) % STAGES) * 2 * BN * CP * 2;
-            load_rows<CP, BN>(stage, kh, p.k.point, j * BN, p.C, take);
-            load_rows<CP, BN>(stage + BN * CP * 2, vh, p.v.point, j * BN, p.C, take);
+            if constexpr (APART) {
+                auto take = [&](int r) { return bias[j & 7][key0 + r] != -INFINITY; };
+                const uint32_t to = stage + key0 * CP * 2;
+                load_rows_by_warp<CP, KW>(to, kh, p.k.point, j * BN + key0, p.C, lane, take);
+                load_rows_by_warp<CP, KW>(to + BN * CP * 2, vh, p.v.point, j * BN + key0, p.C, lane, take);
+            } else {
+                auto take = [&](int r) { return bias[j & 7][r] != -INFINITY; };
+                load_rows<CP, BN>(stage, kh, p.k.point, j * BN, p.C, take);
+                load_rows<CP, BN>(stage + BN * CP * 2, vh, p.v.point, j * BN, p.C, take);
+            }
         }
         commit();
     };
     load_stacked<CP>(tq, static_cast<const T*>(p.q.data) + b * p.q.batch + (int64_t)hk * p.G * p.q.head, p.q.head, p.q.point, row0, rows, p.Nq, BM, p.C);
 #pragma unroll
-    for (int i = 0; i < STAGES; ++i) { fetch_bias(first + i); store_bias(first + i); }
-    fetch_bias(first + STAGES);
+    for (int i = 0; i < 2 * STAGES; ++i)
+        if (mine < BN) {
+            const int j = first + i, n = j * BN + mine;
+            const float raw = weights != nullptr && j < last && n < p.Nk ? weights[n] : 0.f;
+            bias[j & 7][mine] = i < STAGES ? ready(j, raw) : raw;
+        }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) load_block(first + i);
@@ -206,13 +238,12 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
         for (int ks = 0; ks < CP / 16; ++ks) load_a<CP>(q[WM == 1 ? ks : 0], tq, 0, ks, lane);
     }
     for (int j = first; j < last; ++j) {
-        store_bias(j + STAGES);
-        fetch_bias(j + STAGES + 1);
+        ready_bias(j + STAGES);
+        copy_bias(j + 2 * STAGES);
         load_block(j + STAGES - 1);
         wait_group<STAGES - 1>();
-        __syncthreads();
+        in_step();
         const uint32_t tk = tkv + ((j - first) % STAGES) * 2 * BN * CP * 2, tv = tk + BN * CP * 2;
-        const int key0 = wk * KW;
         float s[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -233,7 +264,7 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
         float top[2] = {-INFINITY, -INFINITY};
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            const float2 w = *reinterpret_cast<const float2*>(&bias[j & 3][key0 + n * 8 + (lane & 3) * 2]);
+            const float2 w = *reinterpret_cast<const float2*>(&bias[j & 7][key0 + n * 8 + (lane & 3) * 2]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 s[n][i] = fmaf(s[n][i], p.scale_log2, (i & 1) ? w.y : w.x);
@@ -278,7 +309,7 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
                 mma<T>(o[n + 1], a, vb[2], vb[3]);
             }
         }
-        __syncthreads();        // before the stage is overwritten
+        in_step();        // before the stage is overwritten
     }
     wait_group<0>();
 #pragma unroll
