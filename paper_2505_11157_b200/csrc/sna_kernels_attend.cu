@@ -95,20 +95,6 @@ template <int CP> __device__ __forceinline__ void load_bt(uint32_t (&b)[4], uint
     ldsm_t(b, tile + piece<CP>(k0 + (lane & 7) + (((lane >> 3) & 1) << 3), n * 2 + (lane >> 4)));
 }
 
-// One warp's share of such a load: R rows, of which a lane's pieces lie fewer rows apart than the permutation's period.
-template <int CP, int R, typename T, typename Take>
-__device__ __forceinline__ void load_rows_by_warp(uint32_t tile, const T* head, int64_t point, int first, int C, int lane, Take take) {
-    constexpr int CH = CP / 8, RP = 32 / CH;
-    const int r0 = lane / CH, c = lane - r0 * CH;
-    const T* src = head + (first + r0) * point + c * 8;
-    const bool channel = c * 8 < C;
-#pragma unroll
-    for (int i = 0; i < R / RP; ++i) {
-        const bool there = channel && take(r0 + i * RP);
-        copy16(tile + piece<CP>(r0 + i * RP, c), there ? src : head, there);
-        src += RP * point;
-    }
-}
 // rows [first, first + R) of a head's points (stride `point`); a row that is not there, or for which take(row in tile) is false, is zero.
 // A thread's pieces lie RP rows apart, which is a multiple of the permutation's period: one address each way, and steps.  take also sees to rows
 // behind the last point.
@@ -156,15 +142,16 @@ __device__ __forceinline__ void store_out(const Problem& p, int64_t b, int64_t h
     if (p.rest.data != nullptr) static_cast<T*>(p.rest.data)[b * p.rest.batch + h * p.rest.head + n * p.rest.point + c] = from_float<T>(x - to_float(rounded));
 }
 
-// Stages of (K, V): a memory-bound walk wants two under way (one station over 361x720, B = 2, 2 key heads of 64, bf16: 71 us with one)
-template <int WM> constexpr int FORWARD_STAGES = WM == 1 ? 3 : 2;
-template <int CP, int WM> constexpr int forward_smem() { return WM * 16 * CP * 2 + FORWARD_STAGES<WM> * 2 * BN * CP * 2; }
+// Stages of (K, V).  One station over 361x720, B = 2, 8 and 2 heads of 64, bf16, four blocks per SM, with the join: 53 us; three stages 56, four 68; five blocks per SM
+// 54, six 61 (with fewer registers each).  A warp that loads and waits for its own keys alone gained nothing.
+constexpr int FORWARD_STAGES = 2;
+template <int CP, int WM> constexpr int forward_smem() { return WM * 16 * CP * 2 + FORWARD_STAGES * 2 * BN * CP * 2; }
 
 // WM warps along the rows, WK = 4 / WM along the keys of a block.  partials: null, or sums [splits][rows][C] (first, so that vectors stay aligned) and statistics
 // [splits][rows].
 template <typename T, int CP, int WM>
 __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_forward_kernel(const __grid_constant__ Problem p, int tiles, int splits, float* partials) {
-    constexpr int STAGES = FORWARD_STAGES<WM>, WK = WARPS / WM, BM = 16 * WM, KW = BN / WK, NT = KW / 8, CN = CP / 8;
+    constexpr int STAGES = FORWARD_STAGES, WK = WARPS / WM, BM = 16 * WM, KW = BN / WK, NT = KW / 8, CN = CP / 8;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(16) float bias[8][BN];
     const uint32_t tq = s32(smem), tkv = tq + BM * CP * 2;      // stages of (K, V)
@@ -179,46 +166,32 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
     const int blocks = (p.Nk + BN - 1) / BN;
     const int first = (int)((int64_t)blocks * split / splits), last = (int)((int64_t)blocks * (split + 1) / splits);
 
-    // few rows: a warp loads the 16 keys of a block that it takes itself, and waits for no other (one station as above, warps in step: 52 us without the join)
-    constexpr bool APART = WK == WARPS;
-    const int key0 = wk * KW, mine = APART ? (lane < KW ? key0 + lane : BN) : tid;
-    auto in_step = [&] {
-        if (APART) __syncwarp();
-        else __syncthreads();
-    };
     // Weights come by asynchronous copies 2 STAGES blocks ahead, and are made ready (log2, -infinity for points left out) STAGES ahead, in place: the loads of a
     // block's keys and values go by them.  (Read into a register one step ahead, they were what the steps waited for: one station over 361x720, B = 2, 2 key heads
     // of 32, bf16: 47 us with weights, 35 without.)
-    auto ready = [&](int j, float raw) { return j >= last || j * BN + mine >= p.Nk ? -INFINITY : weights == nullptr ? 0.f : raw <= EXCLUDED ? -INFINITY : raw * LOG2E; };
+    auto ready = [&](int j, float raw) { return j >= last || j * BN + tid >= p.Nk ? -INFINITY : weights == nullptr ? 0.f : raw <= EXCLUDED ? -INFINITY : raw * LOG2E; };
     auto copy_bias = [&](int j) {
-        if (weights != nullptr && mine < BN && j < last && j * BN + mine < p.Nk) copy4(s32(&bias[j & 7][mine]), weights + j * BN + mine);
+        if (weights != nullptr && tid < BN && j < last && j * BN + tid < p.Nk) copy4(s32(&bias[j & 7][tid]), weights + j * BN + tid);
     };
     auto ready_bias = [&](int j) {
-        if (mine < BN) bias[j & 7][mine] = ready(j, bias[j & 7][mine]);
+        if (tid < BN) bias[j & 7][tid] = ready(j, bias[j & 7][tid]);
     };
     auto load_block = [&](int j) {
         if (j < last) {
             const uint32_t stage = tkv + ((j - first) % STAGES) * 2 * BN * CP * 2;
-            if constexpr (APART) {
-                auto take = [&](int r) { return bias[j & 7][key0 + r] != -INFINITY; };
-                const uint32_t to = stage + key0 * CP * 2;
-                load_rows_by_warp<CP, KW>(to, kh, p.k.point, j * BN + key0, p.C, lane, take);
-                load_rows_by_warp<CP, KW>(to + BN * CP * 2, vh, p.v.point, j * BN + key0, p.C, lane, take);
-            } else {
-                auto take = [&](int r) { return bias[j & 7][r] != -INFINITY; };
-                load_rows<CP, BN>(stage, kh, p.k.point, j * BN, p.C, take);
-                load_rows<CP, BN>(stage + BN * CP * 2, vh, p.v.point, j * BN, p.C, take);
-            }
+            auto take = [&](int r) { return bias[j & 7][r] != -INFINITY; };
+            load_rows<CP, BN>(stage, kh, p.k.point, j * BN, p.C, take);
+            load_rows<CP, BN>(stage + BN * CP * 2, vh, p.v.point, j * BN, p.C, take);
         }
         commit();
     };
     load_stacked<CP>(tq, static_cast<const T*>(p.q.data) + b * p.q.batch + (int64_t)hk * p.G * p.q.head, p.q.head, p.q.point, row0, rows, p.Nq, BM, p.C);
 #pragma unroll
     for (int i = 0; i < 2 * STAGES; ++i)
-        if (mine < BN) {
-            const int j = first + i, n = j * BN + mine;
+        if (tid < BN) {
+            const int j = first + i, n = j * BN + tid;
             const float raw = weights != nullptr && j < last && n < p.Nk ? weights[n] : 0.f;
-            bias[j & 7][mine] = i < STAGES ? ready(j, raw) : raw;
+            bias[j & 7][tid] = i < STAGES ? ready(j, raw) : raw;
         }
     __syncthreads();
 #pragma unroll
@@ -242,8 +215,9 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
         copy_bias(j + 2 * STAGES);
         load_block(j + STAGES - 1);
         wait_group<STAGES - 1>();
-        in_step();
+        __syncthreads();
         const uint32_t tk = tkv + ((j - first) % STAGES) * 2 * BN * CP * 2, tv = tk + BN * CP * 2;
+        const int key0 = wk * KW;
         float s[NT][4];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -309,7 +283,7 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
                 mma<T>(o[n + 1], a, vb[2], vb[3]);
             }
         }
-        in_step();        // before the stage is overwritten
+        __syncthreads();        // before the stage is overwritten
     }
     wait_group<0>();
 #pragma unroll
