@@ -59,9 +59,12 @@ struct Walk {
 // Instructions are what costs: with fp32 values exchanged, weights multiplied per vector and addresses computed per slice the kernels took 310 (forward)
 // instructions per vector of eight channels and were bound by issue (256x512 -> 128x256, B = 2, eight heads of 32, bf16: forward 129 us, backward 208).
 // So a lane exchanges its words as they are, weights and angles are one factor per channel and point, and arithmetic is on packed pairs.
-template <typename T, int V, Pairs PAIRS, bool BACKWARD>
+// LANES: the lanes of a vector where the compiler knows them (0: a.lanes), which saves the loop of the sums and some addresses (forward and backward, us: the case above
+// 185 -> 174, 128x256, B = 4, four heads of 32, fp32 125 -> 120).
+template <typename T, int V, Pairs PAIRS, bool BACKWARD, int LANES>
 __global__ void __launch_bounds__(ROTATE_THREADS, BACKWARD ? 3 : 4) norm_rotate_kernel(const __grid_constant__ RotateArgs a) {
     using W = Words<T, V>;
+    const int lanes = LANES > 0 ? LANES : a.lanes;
     constexpr int VP = V / 2, U = 2;        // pairs per lane; vectors of a group under way
     // (the last sum over threads needs room for a block's partial dw, the exchange for a block's vectors)
     __shared__ __align__(16) float shared[BACKWARD || PAIRS == Pairs::BY_SHARED ? ROTATE_THREADS * V : 4];
@@ -69,7 +72,7 @@ __global__ void __launch_bounds__(ROTATE_THREADS, BACKWARD ? 3 : 4) norm_rotate_
     const int which = (int)blockIdx.x >= a.first_blocks;
     const Part& p = a.part[which];
     const int block = (int)blockIdx.x - (which ? a.first_blocks : 0);
-    const int lane = threadIdx.x & (a.lanes - 1), group = threadIdx.x / a.lanes, groups = ROTATE_THREADS / a.lanes;
+    const int lane = threadIdx.x & (lanes - 1), group = threadIdx.x / lanes, groups = ROTATE_THREADS / lanes;
     const int c0 = lane * V, C = a.C, P = p.pairs;
     const bool mine = c0 < C;
     // where the partners of the lane's channels are: a lane (itself if they are not turned), or the other half of each word
@@ -82,14 +85,14 @@ __global__ void __launch_bounds__(ROTATE_THREADS, BACKWARD ? 3 : 4) norm_rotate_
         W y;
         if constexpr (PAIRS == Pairs::BY_SHUFFLE) {
 #pragma unroll
-            for (int i = 0; i < W::N; ++i) y.w[i] = __shfl_sync(0xffffffffu, x.w[i], other, a.lanes);
+            for (int i = 0; i < W::N; ++i) y.w[i] = __shfl_sync(0xffffffffu, x.w[i], other, lanes);
         } else if constexpr (PAIRS == Pairs::IN_LANE) {
 #pragma unroll
             for (int i = 0; i < W::N; ++i)
                 if constexpr (sizeof(T) == 2) y.w[i] = __byte_perm(x.w[i], 0, swap[i]);
                 else y.w[i] = c0 + (i & ~1) < 2 * P ? x.w[i ^ 1] : x.w[i];
         } else {
-            T* row = reinterpret_cast<T*>(shared) + group * a.lanes * V;
+            T* row = reinterpret_cast<T*>(shared) + group * lanes * V;
             T own[V], got[V];
             *reinterpret_cast<W*>(own) = x;
 #pragma unroll
@@ -190,7 +193,8 @@ __global__ void __launch_bounds__(ROTATE_THREADS, BACKWARD ? 3 : 4) norm_rotate_
                 square += upper;
                 unpack2(product2, product, upper);
                 product += upper;
-                for (int o = a.lanes >> 1; o > 0; o >>= 1) {
+#pragma unroll (LANES > 0 ? 4 : 1)
+                for (int o = lanes >> 1; o > 0; o >>= 1) {
                     square += __shfl_xor_sync(0xffffffffu, square, o);
                     if (BACKWARD) product += __shfl_xor_sync(0xffffffffu, product, o);
                 }
@@ -218,11 +222,11 @@ __global__ void __launch_bounds__(ROTATE_THREADS, BACKWARD ? 3 : 4) norm_rotate_
     if (BACKWARD && p.partials != nullptr) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < VP; ++i) unpack2(dw2[i], shared[(group * a.lanes + lane) * V + 2 * i], shared[(group * a.lanes + lane) * V + 2 * i + 1]);
+        for (int i = 0; i < VP; ++i) unpack2(dw2[i], shared[(group * lanes + lane) * V + 2 * i], shared[(group * lanes + lane) * V + 2 * i + 1]);
         __syncthreads();
         for (int c = threadIdx.x; c < C; c += ROTATE_THREADS) {
             float sum = 0.f;
-            for (int g = 0; g < groups; ++g) sum += shared[g * a.lanes * V + c];
+            for (int g = 0; g < groups; ++g) sum += shared[g * lanes * V + c];
             p.partials[(int64_t)block * C + c] = sum;
         }
     }
@@ -255,12 +259,25 @@ __global__ void __launch_bounds__(1024) sum_partials_kernel(const __grid_constan
     if (threadIdx.y == 0 && c < a.C) a.dweight[which][c] = sums[0][threadIdx.x];
 }
 
+template <typename T, int V, Pairs PAIRS, bool BACKWARD>
+cudaError_t launch_lanes(const RotateArgs& a, int blocks, cudaStream_t stream) {
+    auto run = [&](auto lanes) {
+        norm_rotate_kernel<T, V, PAIRS, BACKWARD, decltype(lanes)::value><<<blocks, ROTATE_THREADS, 0, stream>>>(a);
+        return cudaGetLastError();
+    };
+    // (vectors of 16 bytes: heads of 17 to 128 channels in 16 bits, of 9 to 64 in 32; the others are left to one kernel)
+    if constexpr (V * sizeof(T) == 16 && PAIRS != Pairs::BY_SHARED) {
+        if (a.lanes == 4) return run(std::integral_constant<int, 4>());
+        if (a.lanes == 8) return run(std::integral_constant<int, 8>());
+        if (a.lanes == 16) return run(std::integral_constant<int, 16>());
+    }
+    return run(std::integral_constant<int, 0>());
+}
 template <typename T, int V, bool BACKWARD>
 cudaError_t launch_pairs(const RotateArgs& a, Pairs pairs, int blocks, cudaStream_t stream) {
-    if (pairs == Pairs::IN_LANE) norm_rotate_kernel<T, V, Pairs::IN_LANE, BACKWARD><<<blocks, ROTATE_THREADS, 0, stream>>>(a);
-    else if (pairs == Pairs::BY_SHUFFLE) norm_rotate_kernel<T, V, Pairs::BY_SHUFFLE, BACKWARD><<<blocks, ROTATE_THREADS, 0, stream>>>(a);
-    else norm_rotate_kernel<T, V, Pairs::BY_SHARED, BACKWARD><<<blocks, ROTATE_THREADS, 0, stream>>>(a);
-    return cudaGetLastError();
+    if (pairs == Pairs::IN_LANE) return launch_lanes<T, V, Pairs::IN_LANE, BACKWARD>(a, blocks, stream);
+    if (pairs == Pairs::BY_SHUFFLE) return launch_lanes<T, V, Pairs::BY_SHUFFLE, BACKWARD>(a, blocks, stream);
+    return launch_lanes<T, V, Pairs::BY_SHARED, BACKWARD>(a, blocks, stream);
 }
 template <typename T>
 cudaError_t launch_width(const RotateArgs& a, int V, Pairs pairs, bool backward, int blocks, cudaStream_t stream) {
