@@ -55,7 +55,7 @@ struct Walk {
     }
 };
 
-// Measured, 256x512 -> 128x256, B = 2, eight heads of 32, bf16: forward 70 us (73 % of the measured bandwidth), backward 117 (66 %); issue slots 78 and 69 % busy.
+// Measured, 256x512 -> 128x256, B = 2, eight heads of 32, bf16: forward 67 us (76 % of the measured bandwidth), backward 105 (73 %); issue slots 74 and 67 % busy.
 // Instructions are what costs: with fp32 values exchanged, weights multiplied per vector and addresses computed per slice the kernels took 310 (forward)
 // instructions per vector of eight channels and were bound by issue (256x512 -> 128x256, B = 2, eight heads of 32, bf16: forward 129 us, backward 208).
 // So a lane exchanges its words as they are, weights and angles are one factor per channel and point, and arithmetic is on packed pairs.
