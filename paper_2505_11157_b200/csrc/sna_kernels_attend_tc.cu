@@ -1020,7 +1020,7 @@ Split split_of(const Problem& p, Kernel kernel, int sms) {
     auto up = [](int64_t n, int64_t d) { return (n + d - 1) / d; };
     const int64_t forward = (int64_t)p.B * p.Hq * up(p.Nq, 2 * TILE), dq = (int64_t)p.B * p.Hq * up(p.Nq, TILE), dkdv = (int64_t)p.B * p.Hk * up(p.Nk, TILE);
     const int64_t keys = up(p.Nk, BLOCK), queries = p.G * up(p.Nq, BLOCK);
-    // dq's and dk/dv's blocks run side by side, so theirs is one last wave, dk's and dv's; dq is cut only if both together are less than a wave
+    // dq's and dk/dv's blocks run side by side, so theirs is one last wave, dk's and dv's; dq is cut if both together are less than a wave, or for its length (below)
     const int64_t tiles = kernel == Kernel::FORWARD ? forward : kernel == Kernel::DQ ? dq : dkdv, all = kernel == Kernel::FORWARD ? forward : dq + dkdv;
     if (kernel == Kernel::DQ || (kernel == Kernel::DKDV && all >= 8 * (int64_t)sms)) {
         // Few queries and many points, or the reverse: what one side's tiles walk is longer than an SM's share of the work, in blocks (a tile's start and end take as long
