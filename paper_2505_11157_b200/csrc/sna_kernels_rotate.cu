@@ -198,7 +198,8 @@ __global__ void __launch_bounds__(ROTATE_THREADS, BACKWARD ? 3 : 4) norm_rotate_
                     square += __shfl_xor_sync(0xffffffffu, square, o);
                     if (BACKWARD) product += __shfl_xor_sync(0xffffffffu, product, o);
                 }
-                const float r = rsqrtf(square * inverse_C + a.eps);
+                // (groups behind the last point hold zeros: with eps = 0 theirs would be infinite, and their part of dw NaN)
+                const float r = BACKWARD && !here ? 0.f : rsqrtf(square * inverse_C + a.eps);
                 const uint64_t r2 = pack2(r, r);
                 if (BACKWARD) {
                     // dx = r (g w) - n (r sum(g w n) / C) with n = x r

@@ -300,3 +300,50 @@ def test_saved_tensors_that_hooks_return_are_checked(saved, change, says):
             torch.autograd.grad(total, (q, k, *w))
     else:
         assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(total, (q, k, *w)), ref))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=lambda d: str(d).split(".")[1])
+@pytest.mark.parametrize("eps", [0.0, 1e-50])
+@pytest.mark.parametrize("grid, C, interleaved", [((7, 13), 32, False), ((7, 13), 32, True), ((45, 90), 24, False), ((3, 5), 100, True), ((1, 1), 4, False), ((91, 180), 128, False)])
+def test_gradients_without_eps(grid, C, interleaved, eps, dtype):
+    """eps = 0, or below what 32 bits hold, on grids whose last block of points is not full."""
+    torch.manual_seed(C)
+    q, k = heads(2, 3, *grid, C, dtype).requires_grad_(), heads(2, 1, *grid, C, dtype).requires_grad_()
+    weights = [torch.randn(C, device="cuda").requires_grad_() for _ in range(2)]
+    pairs = (1, 1) if C == 100 else (C // 4, C // 4)        # (24 and 100 channels: pairs at a distance that is no multiple of a lane's, channels of no pair)
+    rotation = tables(*grid, *pairs)
+    out = layer.qk_norm_rotate(q, k, *weights, rotation, rotation, eps=eps, interleaved=interleaved)
+    grads_out = [torch.randn(o.shape, device="cuda").to(dtype) for o in out]
+    got = torch.autograd.grad(out, (q, k, *weights), grads_out)
+    for i, (x, weight, g) in enumerate(zip((q, k), weights, grads_out)):
+        ends = [x.detach().double().requires_grad_(), weight.detach().double().requires_grad_()]
+        ref, size = definition(*ends, rotation, 0.0, interleaved)
+        near(out[i].detach(), ref.detach(), size.detach(), C + 16, dtype, f"out {i}")
+        ref_x, ref_w = torch.autograd.grad(ref, ends, g.double())
+        xd = x.detach().double()
+        r = 1 / xd.square().mean(-1, keepdim=True).sqrt()
+        turned = definition_transposed_size(g.double(), rotation, interleaved)
+        gw = turned * weight.detach().double().abs()
+        near(got[i], ref_x, r * (gw + xd.abs() * r * (gw * xd.abs() * r).mean(-1, keepdim=True)), 3 * C + 32, dtype, f"dx {i}")
+        near(got[2 + i], ref_w, (turned * xd.abs() * r).sum((0, 1, 2, 3)), C + 16 + x.numel() // C, torch.float32, f"dw {i}")
+
+
+@pytest.mark.parametrize("C, pairs, interleaved", [(32, (8, 8), False), (64, (16, 16), True), (24, (5, 6), False)], ids=["by shuffle", "within a lane", "by shared memory"])
+def test_results_in_place_of_inputs_for_all_pairs(C, pairs, interleaved):
+    torch.manual_seed(12)
+    x, w, g = heads(3, 5, 7, 9, C, torch.float16), torch.randn(C, device="cuda"), heads(3, 5, 7, 9, C, torch.float16)
+    rotation = tables(7, 9, *pairs)
+    xr, wr = x.clone().requires_grad_(), w.clone().requires_grad_()
+    y = layer.qk_norm_rotate(xr, xr.detach(), wr, w, rotation, rotation, interleaved=interleaved)[0]
+    dx, dw = torch.autograd.grad(y, (xr, wr), g)
+    t = lambda a: sna.SnaTensor(a.data_ptr(), a.stride(0), a.stride(1), a.stride(2), a.stride(3))
+    stream = torch.cuda.current_stream().cuda_stream
+    a, b, dw2 = x.clone(), g.clone(), torch.empty_like(w)
+    part = sna.SnaRotate(nlat=7, nlon=9, H=5, x=t(a), y=t(a), weight=w.data_ptr(), lat_table=rotation[0].data_ptr(), lon_table=rotation[1].data_ptr(), pairs_lat=pairs[0], pairs_lon=pairs[1])
+    assert sna._lib.sna_norm_rotate_forward(part, 1, sna.SNA_FLOAT16, 3, C, 1e-6, interleaved, stream) == 0
+    assert torch.equal(a, y)
+    part.x, part.dy, part.dx, part.dweight = t(x), t(b), t(b), dw2.data_ptr()
+    need = sna._lib.sna_norm_rotate_workspace_bytes(C)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    assert sna._lib.sna_norm_rotate_backward(part, 1, sna.SNA_FLOAT16, 3, C, 1e-6, interleaved, ws.data_ptr(), need, stream) == 0
+    assert torch.equal(b, dx) and torch.equal(dw2, dw)
