@@ -1,5 +1,6 @@
 // The operators around the attention of a layer as native autograd functions over the C ABI (include/sna.h): checks of arguments,
 // allocations and what is kept for the backward pass.  Nothing is computed here.
+#include <c10/core/AutogradState.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/extension.h>
@@ -25,9 +26,14 @@ sna_dtype_t dtype_of(const at::Tensor& t, const char* name) {
     }
 }
 
+// Forward-mode differentiation: the kernels compute no tangents, and a result without one would pass for a derivative of zero.
+void check_no_tangent(const at::Tensor& t, const char* name) {
+    TORCH_CHECK(!c10::AutogradState::get_tls_state().get_fw_grad_mode() || !t._fw_grad(0).defined(), name, " carries a tangent: forward-mode differentiation is not supported");
+}
 void check_cuda(const at::Tensor& t, const char* name, const at::Tensor& first, const char* first_name) {
     TORCH_CHECK_VALUE(t.is_cuda() && t.device() == first.device(), name, " must be a CUDA tensor on the device of ", first_name, " (", first.device(), "), got ", t.device());
     TORCH_CHECK_VALUE(t.layout() == at::kStrided && !t.is_neg(), name, " must be a dense tensor without a pending negation");
+    check_no_tangent(t, name);
 }
 void check_like(const at::Tensor& t, const char* name, const at::Tensor& first, const char* first_name) {
     TORCH_CHECK_VALUE(t.defined(), name, " is missing");
@@ -68,6 +74,7 @@ at::Tensor result_like(const at::Tensor& t, int64_t grain) {
 // What autograd hands over, as the kernels read it.  One row for all points (the gradient of a mean over them) is spread out first: read in place, the blocks of
 // a kernel queue for the same few lines (attention's gradient, B = 2, 4 heads of 64, 4096 points, bf16: 199 us instead of 149).
 at::Tensor gradient(const at::Tensor& g, const at::Tensor& like) {
+    check_no_tangent(g, "the gradient");
     const at::Tensor t = g.to(like.scalar_type()).resolve_neg();
     return (t.size(2) > 1 && t.stride(2) == 0) || (t.size(3) > 1 && t.stride(3) == 0) ? t.contiguous() : t;
 }
@@ -366,6 +373,7 @@ public:
     static variable_list backward(AutogradContext* ctx, variable_list grads) {
         check_once_differentiable("residual_dropout");
         const at::Tensor state = ctx->get_saved_variables()[0];
+        check_no_tangent(grads[0], "the gradient");
         const at::Tensor dout = grads[0].resolve_neg();
         check_state(state, dout);
         variable_list result(4);

@@ -3,7 +3,8 @@
 Nothing is computed here: the calls go to native autograd functions (csrc_torch/sna_layer.cpp) over the C ABI.  Tensors of grids are
 [B, H, nlat, nlon, C] (heads leading, as everywhere in this package) with any strides over contiguous channels: a packed projection, or
 one that left the channels last, is read in place.  Every call takes its tensors' device and that device's current stream; gradients are
-computed once (``create_graph`` is refused), in a fixed order of sums: the same call gives the same bits.
+computed once (``create_graph`` is refused, and so are tensors with a tangent of forward-mode differentiation), in a fixed order of sums: the
+same call gives the same bits.
 """
 from __future__ import annotations
 
