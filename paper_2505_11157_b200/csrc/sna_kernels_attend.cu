@@ -173,8 +173,12 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
     auto copy_bias = [&](int j) {
         if (weights != nullptr && tid < BN && j < last && j * BN + tid < p.Nk) copy4(s32(&bias[j & 7][tid]), weights + j * BN + tid);
     };
+    bool present = false;       // whether any point of this thread's takes part
     auto ready_bias = [&](int j) {
-        if (tid < BN) bias[j & 7][tid] = ready(j, bias[j & 7][tid]);
+        if (tid >= BN) return;
+        const float weight = ready(j, bias[j & 7][tid]);
+        bias[j & 7][tid] = weight;
+        present |= weight != -INFINITY;
     };
     auto load_block = [&](int j) {
         if (j < last) {
@@ -191,7 +195,8 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
         if (tid < BN) {
             const int j = first + i, n = j * BN + tid;
             const float raw = weights != nullptr && j < last && n < p.Nk ? weights[n] : 0.f;
-            bias[j & 7][tid] = i < STAGES ? ready(j, raw) : raw;
+            bias[j & 7][tid] = raw;
+            if (i < STAGES) ready_bias(j);
         }
     __syncthreads();
 #pragma unroll
@@ -286,6 +291,15 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
         __syncthreads();        // before the stage is overwritten
     }
     wait_group<0>();
+    if (weights != nullptr && __syncthreads_or(present) == 0) {
+        // nothing takes part: not even a query of infinities or NaN, whose products with rows of zeros are NaN
+        m[0] = m[1] = -INFINITY;
+        l[0] = l[1] = 0.f;
+#pragma unroll
+        for (int n = 0; n < CN; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[n][i] = 0.f;
+    }
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
         l[r] += __shfl_xor_sync(0xffffffffu, l[r], 1);

@@ -379,6 +379,16 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
             if (ok && count > 0) ok = all_lanes(mb_wait(bar(F::O_DONE + t), (count - 1) & 1, ok));
             if (ok) {
                 tm_after();
+                bool nothing = count == 0;
+                if (WEIGHTS && !apart && __any_sync(0xffffffffu, l != l)) {
+                    // A query of infinities or NaN makes S NaN against the zeros of points left out, too: with those alone its row is one without points.
+                    const float* weights = p.log_weights + b * p.log_weights_batch;
+                    const int end = min(Nk, (first + count) * TILE);
+                    nothing = true;
+                    for (int n = first * TILE; n < end && nothing; n += 32)
+                        nothing = __all_sync(0xffffffffu, n + lane >= end || weights[n + lane] <= EXCLUDED);
+                    if (nothing) { ref = -INFINITY; l = 0.f; }
+                }
                 const int row = row0 + t * TILE + (warp & 3) * 32 + lane;
                 const int64_t at = ((int64_t)b * p.Hq + h) * p.Nq + row;
                 const int64_t rest = cut.rest() * 2 * TILE, local = piece.local * 2 * TILE + t * TILE + (warp & 3) * 32 + lane;
@@ -392,7 +402,7 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
                 }
                 for (int c = 0; c < p.C; c += 32) {
                     uint32_t o[32];
-                    if (count > 0) {
+                    if (!nothing) {
                         tm_ld32(o, to + c);
                         tm_ld_wait();
                     } else {

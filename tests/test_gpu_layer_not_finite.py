@@ -1,0 +1,51 @@
+"""16-bit attention: infinities and NaN in queries and gradients stay where the definition leaves them; a row without points has zeros and no gradient whatever its
+query holds, and a point left out has no gradient."""
+import math
+
+import pytest
+import torch
+
+from paper_2505_11157_b200 import layer
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = [torch.bfloat16, torch.float16]
+# queries, points: few queries, keys split over blocks, tiles of 64 stacked rows, tcgen05 (one tile, pieces, points brought together)
+SIZES = [(1, 20), (3, 20000), (40, 40), (200, 300), (33, 9000), (4500, 4000)]
+
+
+def tensors(Nq, Nk, dtype, C=32):
+    torch.manual_seed(Nq + Nk)
+    B, Hq, Hk = 3, 8, 4
+    q, g = (torch.randn(B, Hq, 1, Nq, C, device="cuda").to(dtype) for _ in range(2))
+    k, v = (torch.randn(B, Hk, 1, Nk, C, device="cuda").to(dtype) for _ in range(2))
+    w = torch.randn(B, Nk, device="cuda")
+    w[1] = -math.inf                                        # a field without points
+    w[2, torch.rand(Nk, device="cuda") < 0.3] = -math.inf   # one with some
+    w[2, 0] = 0.0
+    return q, k, v, w, g
+
+
+def run(q, k, v, w, g):
+    ends = [x.detach().requires_grad_() for x in (q, k, v)]
+    out, lse = layer.weighted_attention(*ends, w, return_lse=True)
+    return (out.detach(), lse, *torch.autograd.grad(out, ends, g))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=lambda d: str(d).split(".")[1])
+@pytest.mark.parametrize("Nq, Nk", SIZES)
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_rows_without_points_whatever_their_query_holds(Nq, Nk, bad, dtype):
+    q, k, v, w, g = tensors(Nq, Nk, dtype)
+    with torch.no_grad():
+        ref = layer.weighted_attention(q, k, v, w, return_lse=True)
+        q[1, 0, 0, 0, 3] = q[1, 5, 0, Nq // 2, 0] = q[1, 7, 0, Nq - 1] = bad
+        out, lse = layer.weighted_attention(q, k, v, w, return_lse=True)
+        assert not bool(out[1].any()) and bool((lse[1] == -math.inf).all())
+        assert torch.equal(out, ref[0]) and torch.equal(lse, ref[1])
+        # points that take part: the row is NaN, and no other
+        q[2, 6, 0, Nq - 1, 3] = bad
+        out, lse = layer.weighted_attention(q, k, v, w, return_lse=True)
+        assert bool(out[2, 6, 0, Nq - 1].isnan().all())
+        out[2, 6, 0, Nq - 1], lse[2, 6, 0, Nq - 1] = ref[0][2, 6, 0, Nq - 1], ref[1][2, 6, 0, Nq - 1]
+        assert torch.equal(out, ref[0]) and torch.equal(lse, ref[1])
