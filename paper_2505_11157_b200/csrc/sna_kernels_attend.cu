@@ -628,8 +628,11 @@ __global__ void __launch_bounds__(THREADS) attend_dq_kernel(const __grid_constan
             weight = j < last && n < p.Nk ? weight2(weights, n) : -INFINITY;
         }
     };
+    bool present = false;       // whether any point of this thread's takes part
     auto store_bias = [&](int j) {
-        if (tid < BN) bias[j & 3][tid] = weight;
+        if (tid >= BN) return;
+        bias[j & 3][tid] = weight;
+        present |= weight != -INFINITY;
     };
     auto load_block = [&](int j) {
         if (j < last) {
@@ -719,6 +722,8 @@ __global__ void __launch_bounds__(THREADS) attend_dq_kernel(const __grid_constan
         __syncthreads();
     }
     wait_group<0>();
+    // (where nothing takes part there is no gradient, not even of a query or for a gradient of infinities or NaN)
+    const bool nothing = weights != nullptr && __syncthreads_or(present) == 0;
     const float back = p.scale * ex2(-SHIFT<T>) / factor;
 #pragma unroll
     for (int r = 0; r < 2; ++r) {
@@ -729,7 +734,7 @@ __global__ void __launch_bounds__(THREADS) attend_dq_kernel(const __grid_constan
 #pragma unroll
         for (int n = 0; n < CN; ++n) {
             const int c = n * 8 + (lane & 3) * 2;
-            if (c < p.C) *reinterpret_cast<uint32_t*>(out + c) = pack<T>(dq[n][2 * r] * back, dq[n][2 * r + 1] * back);
+            if (c < p.C) *reinterpret_cast<uint32_t*>(out + c) = nothing ? 0u : pack<T>(dq[n][2 * r] * back, dq[n][2 * r + 1] * back);
         }
     }
 }
@@ -848,14 +853,15 @@ __global__ void __launch_bounds__(THREADS) attend_dkdv_kernel(const __grid_const
     for (int r = 0; r < 2; ++r) {
         const int n_key = key0 + warp * 16 + (lane >> 2) + 8 * r;
         if (n_key >= p.Nk) continue;
+        const bool left_out = w2[r] == -INFINITY;       // (its sums are NaN if a query or a gradient is infinite or NaN)
         T* k_out = static_cast<T*>(p.dk.data) + b * p.dk.batch + hk * p.dk.head + (int64_t)n_key * p.dk.point;
         T* v_out = static_cast<T*>(p.dv.data) + b * p.dv.batch + hk * p.dv.head + (int64_t)n_key * p.dv.point;
 #pragma unroll
         for (int n = 0; n < CN; ++n) {
             const int c = n * 8 + (lane & 3) * 2;
             if (c >= p.C) continue;
-            *reinterpret_cast<uint32_t*>(k_out + c) = pack<T>(dk[n][2 * r] * back, dk[n][2 * r + 1] * back);
-            *reinterpret_cast<uint32_t*>(v_out + c) = pack<T>(dv[n][2 * r] * unshift, dv[n][2 * r + 1] * unshift);
+            *reinterpret_cast<uint32_t*>(k_out + c) = left_out ? 0u : pack<T>(dk[n][2 * r] * back, dk[n][2 * r + 1] * back);
+            *reinterpret_cast<uint32_t*>(v_out + c) = left_out ? 0u : pack<T>(dv[n][2 * r] * unshift, dv[n][2 * r + 1] * unshift);
         }
     }
 }

@@ -49,3 +49,25 @@ def test_rows_without_points_whatever_their_query_holds(Nq, Nk, bad, dtype):
         assert bool(out[2, 6, 0, Nq - 1].isnan().all())
         out[2, 6, 0, Nq - 1], lse[2, 6, 0, Nq - 1] = ref[0][2, 6, 0, Nq - 1], ref[1][2, 6, 0, Nq - 1]
         assert torch.equal(out, ref[0]) and torch.equal(lse, ref[1])
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=lambda d: str(d).split(".")[1])
+@pytest.mark.parametrize("Nq, Nk", SIZES)
+@pytest.mark.parametrize("which", ["query", "gradient", "both"])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_points_left_out_have_no_gradient_whatever_queries_and_gradients_hold(Nq, Nk, bad, which, dtype):
+    q, k, v, w, g = tensors(Nq, Nk, dtype)
+    clean = run(q, k, v, w, g)
+    for x in [q] * (which != "gradient") + [g] * (which != "query"):
+        x[1, 0, 0, 0, 3] = x[1, 5, 0, Nq // 2, 0] = x[1, 7, 0, Nq - 1] = bad      # in the field without points
+    for got, ref in zip(run(q, k, v, w, g), clean):
+        assert torch.equal(got, ref)
+    for x in [q] * (which != "gradient") + [g] * (which != "query"):
+        x[2, 6, 0, Nq - 1, 3] = bad         # and in one with some: key head 3 of that field has no gradient that is a number, the others have theirs
+    _, _, dq, dk, dv = run(q, k, v, w, g)
+    gone = w[2] == -math.inf
+    assert not bool(dk[2, :, 0, gone].any()) and not bool(dv[2, :, 0, gone].any())
+    assert bool(dq[2, 6, 0, Nq - 1].isnan().any()) and bool((~dk[2, 3, 0, ~gone].isfinite()).any())
+    for got, ref in zip((dk, dv), clean[3:]):
+        assert torch.equal(got[:2], ref[:2]) and torch.equal(got[2, :3], ref[2, :3])
+    assert torch.equal(dq[:2], clean[2][:2]) and torch.equal(dq[2, :6], clean[2][2, :6])
