@@ -596,7 +596,8 @@ __global__ void __launch_bounds__(256) attend_statistics_kernel(const __grid_con
     if (SCALED) {
         if (threadIdx.x == 0) most = 0;
         __syncthreads();
-        if (there && part == 0) atomicMax(&most, __float_as_uint(sqrtf(square)));
+        // (rows of infinities or NaN, whose own gradients are no numbers, do not count: the others are to be scaled as without them)
+        if (there && part == 0 && square < INFINITY) atomicMax(&most, __float_as_uint(sqrtf(square)));
         __syncthreads();
         if (threadIdx.x == 0 && most != 0) atomicMax(s.norms + (b * p.Hk + (queries ? h / p.G : h)) * 2 + (queries ? 0 : 1), most);
     }

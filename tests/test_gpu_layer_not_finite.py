@@ -71,3 +71,21 @@ def test_points_left_out_have_no_gradient_whatever_queries_and_gradients_hold(Nq
     for got, ref in zip((dk, dv), clean[3:]):
         assert torch.equal(got[:2], ref[:2]) and torch.equal(got[2, :3], ref[2, :3])
     assert torch.equal(dq[:2], clean[2][:2]) and torch.equal(dq[2, :6], clean[2][2, :6])
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=lambda d: str(d).split(".")[1])
+@pytest.mark.parametrize("Nq, Nk", [(5, 20), (40, 40), (200, 300), (33, 9000), (4500, 4000)])
+@pytest.mark.parametrize("bad", [math.nan, -math.nan, math.inf])
+def test_a_gradient_that_is_not_finite_leaves_the_other_rows_theirs(Nq, Nk, bad, dtype):
+    """float16: ds is held times a power of two from the largest rows of dout and v, without which values of this size overflow."""
+    q, k, v, w, g = tensors(Nq, Nk, dtype)
+    v *= 8
+    g *= 64
+    g[0, 2, 0, 1] = g[2, 6, 0, Nq - 1] = 0
+    clean = run(q, k, v, w, g)[2]
+    assert bool(clean.isfinite().all())
+    g[0, 2, 0, 1, 5] = g[2, 6, 0, Nq - 1] = bad
+    dq = run(q, k, v, w, g)[2]
+    assert bool((~dq[0, 2, 0, 1].isfinite()).any()) and bool((~dq[2, 6, 0, Nq - 1].isfinite()).any())
+    dq[0, 2, 0, 1], dq[2, 6, 0, Nq - 1] = clean[0, 2, 0, 1], clean[2, 6, 0, Nq - 1]
+    assert torch.equal(dq, clean)
