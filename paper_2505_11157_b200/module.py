@@ -102,7 +102,9 @@ class SphericalNeighborhoodAttention(torch.nn.Module):
         if self.training and self.dropout > 0.0:
             if residual is not None:        # (of other types, under autocast say: as the plain sum takes them)
                 dtype = torch.promote_types(y.dtype, residual.dtype)
-                residual = residual.to(dtype).expand_as(y)
-                y = y.to(dtype)
+                y, residual = y.to(dtype), residual.to(dtype)
+                if torch.broadcast_shapes(y.shape, residual.shape) != y.shape:      # (several residuals of one result, dropped once)
+                    return residual + layer.residual_dropout(y, layer.dropout_state(y.device), self.dropout)
+                residual = residual.expand_as(y)
             return layer.residual_dropout(y, layer.dropout_state(y.device), self.dropout, residual)
         return y if residual is None else residual + y

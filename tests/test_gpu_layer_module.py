@@ -203,3 +203,21 @@ def test_residuals_of_another_type_or_shape_with_dropout(shape):
     assert bool((dropped | ((y - quotient).abs() <= room)).all()) and 0.2 < float(dropped.double().mean()) < 0.3
     kept.sum().backward()
     assert torch.equal(residual.grad, torch.full(shape, 2 * 8 * 12 * 24 / residual.numel(), device="cuda"))
+
+
+def test_more_residuals_than_results_with_dropout():
+    """One result and a batch of residuals, as the plain sum takes them: the result is dropped once."""
+    torch.manual_seed(8)
+    plan = sna.Plan(6, 12, 6, 12, 0, 0, global_attention=True)
+    m = SphericalNeighborhoodAttention(plan, 8, 2, 16, half_attention=True, dropout=0.25).cuda()
+    x, residual = torch.randn(1, 8, 6, 12, device="cuda"), torch.randn(3, 8, 6, 12, device="cuda", requires_grad=True)
+    assert m.eval()(x, residual=residual).shape == residual.shape
+    m.train()
+    torch.manual_seed(9)
+    kept = m(x, residual=residual)
+    torch.manual_seed(9)
+    assert torch.equal(kept, residual + m(x))
+    kept.sum().backward()
+    assert torch.equal(residual.grad, torch.ones_like(residual)) and bool(torch.isfinite(m.wo.grad).all())
+    with pytest.raises(RuntimeError, match="broadcast|must match|not match"):
+        m(x, residual=residual[:, :, :5])
