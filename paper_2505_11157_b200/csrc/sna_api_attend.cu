@@ -182,8 +182,7 @@ sna_status_t sna_attention_backward(const sna_attention_t* a, sna_dtype_t dtype,
     const Stats& s = w.stats;
     cudaError_t e = launch_statistics(p, s, w.selection, dtype, stream);
     // (on_tensor_memory: there are queries and keys)
-    if (e == cudaSuccess && on_tensor_memory(p) && backward_dq_tc(p, s, w.selection, dtype, sms, w.dq_partials, stream, e)) {
-        if (e == cudaSuccess && !backward_dkdv_tc(p, s, w.selection, dtype, sms, w.dkdv_partials, stream, e)) e = cudaErrorInvalidValue;      // (the same tensors, in other boxes)
+    if (e == cudaSuccess && on_tensor_memory(p) && backward_tc(p, s, w.selection, dtype, sms, w.dq_partials, w.dkdv_partials, stream, e)) {
         if (e == cudaSuccess) e = join_backward(p, w.selection, dtype, sms, w.dq_partials, w.dkdv_partials, stream);
     } else {
         if (e == cudaSuccess && queries) e = launch_backward_dq(p, s, dtype, stream);

@@ -108,8 +108,7 @@ enum class Kernel { FORWARD, DQ, DKDV };
 Split split_of(const Problem& p, Kernel kernel, int sms);
 size_t partial_floats(const Problem& p, Kernel kernel, int sms);
 bool forward_tc(const Problem& p, const Selection& sel, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
-bool backward_dq_tc(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
-bool backward_dkdv_tc(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e);
+bool backward_tc(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, int sms, float* dq_partials, float* dkdv_partials, cudaStream_t stream, cudaError_t& e);
 cudaError_t join_backward(const Problem& p, const Selection& sel, sna_dtype_t dtype, int sms, const float* dq_partials, const float* dkdv_partials, cudaStream_t stream);
 cudaError_t read_status(int* status);
 cudaError_t launch_wait_probe(cudaStream_t stream);

@@ -21,12 +21,12 @@ __device__ int g_status;        // non-zero: a bounded wait has run out since th
 struct Piece {
     int tile, bh, part, parts;
     int64_t local;          // of a tile in pieces: its number among them
-    __device__ __forceinline__ Piece(const Split& cut, int tiles) {
-        const int64_t over = (int64_t)blockIdx.x - cut.full;
+    __device__ __forceinline__ Piece(const Split& cut, int tiles, int64_t block) {
+        const int64_t over = block - cut.full;
         parts = over < 0 ? 1 : cut.parts;
         local = over < 0 ? 0 : over / parts;
         part = over < 0 ? 0 : (int)(over - local * parts);
-        const int64_t index = over < 0 ? (int64_t)blockIdx.x : cut.full + local;
+        const int64_t index = over < 0 ? block : cut.full + local;
         bh = (int)(index / tiles);
         tile = (int)(index - (int64_t)bh * tiles);
     }
@@ -121,7 +121,7 @@ attend_forward_tc_kernel(const __grid_constant__ Problem p, const __grid_constan
     __shared__ uint32_t tmem_s;
     __shared__ int fail_s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const Piece piece(cut, tiles);
+    const Piece piece(cut, tiles, blockIdx.x);
     const int part = piece.part, parts = piece.parts, tile = piece.tile, bh = piece.bh;
     const int b = bh / p.Hq, h = bh - b * p.Hq, hk = h / p.G;
     const int row0 = tile * 2 * TILE, halves = row0 + TILE < p.Nq ? 2 : 1;
@@ -476,12 +476,23 @@ template <int D, bool DKDV> struct Backward {
            S_DONE = T_FULL + 2 /* S read (dq) or P ready (dk, dv) */, D_READY = S_DONE + 2, ACC_DONE = D_READY + 2, COUNT };
 };
 
+// dq's tiles, or dk's and dv's
+struct Side {
+    Split cut;
+    int tiles;          // of a head
+    float* partials;
+};
+// In boxes of a streamed block: queries and their gradients (for dk, dv), keys and values (for dq).  In boxes of a tile: keys and values, where dk, dv has them in
+// shared memory.  The selected ones are there if there is a selection.
+struct BackwardMaps {
+    CUtensorMap q, dout, k, v, k_sel, v_sel, k_tile, v_tile, k_sel_tile, v_sel_tile;
+};
+
 template <typename T, int D, bool DKDV, bool WEIGHTS, bool FINE>
-__global__ void __launch_bounds__(BWD_THREADS, 1)
-attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats stats, const __grid_constant__ Selection sel, const __grid_constant__ CUtensorMap map_a1,
-                          const __grid_constant__ CUtensorMap map_a2, const __grid_constant__ CUtensorMap map_b1, const __grid_constant__ CUtensorMap map_b2,
-                          const __grid_constant__ CUtensorMap map_k_sel, const __grid_constant__ CUtensorMap map_v_sel, int tiles, const __grid_constant__ Split cut, float* partials) {
+__device__ __forceinline__ void backward_block(const Problem& p, const Stats& stats, const Selection& sel, const BackwardMaps& maps, const Side& side, int64_t block) {
     using K = Backward<D, DKDV>;
+    const Split& cut = side.cut;
+    float* const partials = side.partials;
     constexpr bool EXTRA = DKDV || WEIGHTS;
     static_assert(BLOCK == STATS_BLOCK, "the statistics kernel's blocks");
     extern __shared__ unsigned char raw[];
@@ -490,15 +501,9 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     __shared__ uint32_t tmem_s;
     __shared__ int fail_s;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const Piece piece(cut, tiles);
+    const Piece piece(cut, side.tiles, block);
     const int tile = piece.tile, bh = piece.bh;
     const int heads = DKDV ? p.Hk : p.Hq, b = bh / heads, head = bh - b * heads, hk = DKDV ? head : head / p.G;
-    // The order on the stream is statistics, dq, dk and dv, joins.  dk and dv need nothing of dq: their blocks fill the SMs that its last blocks leave idle, and wait
-    // for them at their end alone; by the time that they may start, every block of dq has seen the statistics complete.
-    if (!DKDV) {
-        wait_for_previous();
-        allow_dependents();
-    }
     const int Nk = WEIGHTS && sel.taken != nullptr ? sel.taken[b] : p.Nk;
     const bool apart = WEIGHTS && Nk != p.Nk;
     const int row0 = tile * TILE, N = DKDV ? Nk : p.Nq, M = DKDV ? p.Nq : Nk;       // rows, streamed points
@@ -544,7 +549,6 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
                     }
                 }
             }
-            if (DKDV) wait_for_previous();
             return;
         }
     }
@@ -575,8 +579,8 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     if (warp >= 16) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
         if (warp == 16 && elect_one()) {
-            const CUtensorMap *a1 = DKDV && apart ? &map_k_sel : &map_a1, *a2 = DKDV && apart ? &map_v_sel : &map_a2;
-            const CUtensorMap *b1 = !DKDV && apart ? &map_k_sel : &map_b1, *b2 = !DKDV && apart ? &map_v_sel : &map_b2;
+            const CUtensorMap *a1 = apart ? &maps.k_sel_tile : &maps.k_tile, *a2 = apart ? &maps.v_sel_tile : &maps.v_tile;       // (dk, dv)
+            const CUtensorMap *b1 = DKDV ? &maps.q : apart ? &maps.k_sel : &maps.k, *b2 = DKDV ? &maps.dout : apart ? &maps.v_sel : &maps.v;
             // ---------------------------------------------------------------- TMA
             if (!K::A_IN_TMEM) {
                 mb_expect(bar(K::A_FULL), 2 * slabs * SLAB);
@@ -822,7 +826,17 @@ attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_consta
     __syncthreads();
     if (fail_s && tid == 0) atomicExch(&g_status, 1);
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tm), "r"(512));
-    if (DKDV) wait_for_previous();
+}
+
+// One launch for dq and for dk and dv, which need nothing of each other: dq's blocks come first, and the others fill the SMs that its last ones leave idle.
+template <typename T, int D, bool WEIGHTS, bool FINE>
+__global__ void __launch_bounds__(BWD_THREADS, 1)
+attend_backward_tc_kernel(const __grid_constant__ Problem p, const __grid_constant__ Stats stats, const __grid_constant__ Selection sel, const __grid_constant__ BackwardMaps maps,
+                          const __grid_constant__ Side dq, const __grid_constant__ Side dkdv) {
+    wait_for_previous();        // the statistics
+    const int64_t dq_blocks = dq.cut.blocks();
+    if (blockIdx.x < dq_blocks) backward_block<T, D, false, WEIGHTS, FINE>(p, stats, sel, maps, dq, blockIdx.x);
+    else backward_block<T, D, true, WEIGHTS, FINE>(p, stats, sel, maps, dkdv, blockIdx.x - dq_blocks);
 }
 
 // ---- joins of tiles in pieces ---------------------------------------------------------------------------------------------------
@@ -960,58 +974,53 @@ cudaError_t forward_as(const Problem& p, const Selection& sel, const CUtensorMap
     return launch_joins<T, true>(joins, stream);
 }
 
-template <typename T, int D, bool DKDV, bool WEIGHTS, bool FINE>
-cudaError_t backward_as(const Problem& p, const Stats& s, const Selection& sel, const CUtensorMap (&maps)[6], const Split& cut, float* partials, cudaStream_t stream) {
-    const int tiles = ((DKDV ? p.Nk : p.Nq) + TILE - 1) / TILE;
-    const auto kernel = attend_backward_tc_kernel<T, D, DKDV, WEIGHTS, FINE>;
+template <typename T, int D, bool WEIGHTS, bool FINE>
+cudaError_t backward_as(const Problem& p, const Stats& s, const Selection& sel, const BackwardMaps& maps, const Side& dq, const Side& dkdv, cudaStream_t stream) {
+    constexpr size_t smem = std::max(Backward<D, false>::SMEM, Backward<D, true>::SMEM);
+    const auto kernel = attend_backward_tc_kernel<T, D, WEIGHTS, FINE>;
     static std::atomic<uint64_t> allowed{0};
-    cudaError_t e = allow(kernel, Backward<D, DKDV>::SMEM, allowed);
+    cudaError_t e = allow(kernel, smem, allowed);
     if (e != cudaSuccess) return e;
-    return launch_dependent(kernel, (unsigned)cut.blocks(), BWD_THREADS, Backward<D, DKDV>::SMEM, stream, p, s, sel, maps[0], maps[1], maps[2], maps[3], maps[4], maps[5], tiles, cut, partials);
+    return launch_dependent(kernel, (unsigned)(dq.cut.blocks() + dkdv.cut.blocks()), BWD_THREADS, smem, stream, p, s, sel, maps, dq, dkdv);
 }
 // Maps of the selected keys and values (untouched and unread without a selection).
-bool make_selected(CUtensorMap* maps, const Problem& p, const Selection& sel, sna_dtype_t dtype, int rows) {
+bool make_selected(CUtensorMap& k, CUtensorMap& v, const Problem& p, const Selection& sel, sna_dtype_t dtype, int rows) {
     if (sel.taken == nullptr) return true;
-    return make_map(&maps[0], selected_view(p, sel.k), dtype, p.C, p.Nk, p.Hk, p.B, rows) && make_map(&maps[1], selected_view(p, sel.v), dtype, p.C, p.Nk, p.Hk, p.B, rows);
+    return make_map(&k, selected_view(p, sel.k), dtype, p.C, p.Nk, p.Hk, p.B, rows) && make_map(&v, selected_view(p, sel.v), dtype, p.C, p.Nk, p.Hk, p.B, rows);
 }
 // Whether p and ds are held in two 16-bit parts: where their rounding is less averaged out than elsewhere.  With one part the gradients' relative errors (norms) are 1.41 to
 // 1.47 times those of rounding the result alone, which is what single roundings of as many terms give; narrow heads reach 1.6, and so do a few rows.  The second part
 // costs a forward and backward pass 20 % there (us, B = 2, 4 heads of 8, 8192 queries and points, bf16: 596 with one part, 717 with two), small problems less (1024 queries
 // and points, B = 1, 4 heads of 32: 31, 33; 33 queries, 9800 points, one head of 32: 94, 108).
 bool in_two_parts(const Problem& p) { return p.C <= 16 || rows_of(p) * p.Nk <= (int64_t)1 << 22; }
-template <bool DKDV>
-bool backward_tc(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
-    const Split cut = split_of(p, DKDV ? Kernel::DKDV : Kernel::DQ, sms);
-    CUtensorMap maps[6];        // A1, A2 (boxes of a tile), B1, B2 (of a block), the selected keys and values
-    const int q_rows = DKDV ? BLOCK : TILE, k_rows = DKDV ? TILE : BLOCK, q_at = DKDV ? 2 : 0, k_at = 2 - q_at;
-    if (!make_map(&maps[q_at], p.q, dtype, p.C, p.Nq, p.Hq, p.B, q_rows) || !make_map(&maps[q_at + 1], p.dout, dtype, p.C, p.Nq, p.Hq, p.B, q_rows) ||
-        !make_map(&maps[k_at], p.k, dtype, p.C, p.Nk, p.Hk, p.B, k_rows) || !make_map(&maps[k_at + 1], p.v, dtype, p.C, p.Nk, p.Hk, p.B, k_rows) ||
-        !make_selected(&maps[4], p, sel, dtype, k_rows))
+}  // namespace
+
+bool backward_tc(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, int sms, float* dq_partials, float* dkdv_partials, cudaStream_t stream, cudaError_t& e) {
+    BackwardMaps maps;
+    const bool wide = p.C > 64;
+    if (!make_map(&maps.q, p.q, dtype, p.C, p.Nq, p.Hq, p.B, BLOCK) || !make_map(&maps.dout, p.dout, dtype, p.C, p.Nq, p.Hq, p.B, BLOCK) ||
+        !make_map(&maps.k, p.k, dtype, p.C, p.Nk, p.Hk, p.B, BLOCK) || !make_map(&maps.v, p.v, dtype, p.C, p.Nk, p.Hk, p.B, BLOCK) ||
+        !make_selected(maps.k_sel, maps.v_sel, p, sel, dtype, BLOCK))
         return false;
+    if (wide && (!make_map(&maps.k_tile, p.k, dtype, p.C, p.Nk, p.Hk, p.B, TILE) || !make_map(&maps.v_tile, p.v, dtype, p.C, p.Nk, p.Hk, p.B, TILE) ||
+                 !make_selected(maps.k_sel_tile, maps.v_sel_tile, p, sel, dtype, TILE)))
+        return false;
+    const Side dq{split_of(p, Kernel::DQ, sms), (p.Nq + TILE - 1) / TILE, dq_partials}, dkdv{split_of(p, Kernel::DKDV, sms), (p.Nk + TILE - 1) / TILE, dkdv_partials};
     const bool weights = p.log_weights != nullptr;
     auto run = [&](auto t, auto width) {
         using T = decltype(t);
         constexpr int D = decltype(width)::value;
         auto go = [&](auto fine) {
             constexpr bool FINE = decltype(fine)::value;
-            return weights ? backward_as<T, D, DKDV, true, FINE>(p, s, sel, maps, cut, partials, stream) : backward_as<T, D, DKDV, false, FINE>(p, s, sel, maps, cut, partials, stream);
+            return weights ? backward_as<T, D, true, FINE>(p, s, sel, maps, dq, dkdv, stream) : backward_as<T, D, false, FINE>(p, s, sel, maps, dq, dkdv, stream);
         };
         return in_two_parts(p) ? go(std::true_type()) : go(std::false_type());
     };
     using W64 = std::integral_constant<int, 64>;
     using W128 = std::integral_constant<int, 128>;
-    if (dtype == SNA_BFLOAT16) e = p.C <= 64 ? run(__nv_bfloat16(), W64()) : run(__nv_bfloat16(), W128());
-    else e = p.C <= 64 ? run(__half(), W64()) : run(__half(), W128());
+    if (dtype == SNA_BFLOAT16) e = wide ? run(__nv_bfloat16(), W128()) : run(__nv_bfloat16(), W64());
+    else e = wide ? run(__half(), W128()) : run(__half(), W64());
     return true;
-}
-
-}  // namespace
-
-bool backward_dq_tc(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
-    return backward_tc<false>(p, s, sel, dtype, sms, partials, stream, e);
-}
-bool backward_dkdv_tc(const Problem& p, const Stats& s, const Selection& sel, sna_dtype_t dtype, int sms, float* partials, cudaStream_t stream, cudaError_t& e) {
-    return backward_tc<true>(p, s, sel, dtype, sms, partials, stream, e);
 }
 
 // Pieces of each of `rest` tiles, where the SMs have a partial wave of them (see Split).
@@ -1083,7 +1092,7 @@ bool forward_tc(const Problem& p, const Selection& sel, sna_dtype_t dtype, int s
     const Split cut = split_of(p, Kernel::FORWARD, sms);
     CUtensorMap maps[5];        // queries, keys, values, the selected keys and values
     if (!make_map(&maps[0], p.q, dtype, p.C, p.Nq, p.Hq, p.B, TILE) || !make_map(&maps[1], p.k, dtype, p.C, p.Nk, p.Hk, p.B, TILE) ||
-        !make_map(&maps[2], p.v, dtype, p.C, p.Nk, p.Hk, p.B, TILE) || !make_selected(&maps[3], p, sel, dtype, TILE))
+        !make_map(&maps[2], p.v, dtype, p.C, p.Nk, p.Hk, p.B, TILE) || !make_selected(maps[3], maps[4], p, sel, dtype, TILE))
         return false;
     const bool weights = p.log_weights != nullptr;
     auto run = [&](auto t, auto width) {
