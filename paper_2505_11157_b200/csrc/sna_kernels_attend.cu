@@ -173,12 +173,8 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
     auto copy_bias = [&](int j) {
         if (weights != nullptr && tid < BN && j < last && j * BN + tid < p.Nk) copy4(s32(&bias[j & 7][tid]), weights + j * BN + tid);
     };
-    bool present = false;       // whether any point of this thread's takes part
     auto ready_bias = [&](int j) {
-        if (tid >= BN) return;
-        const float weight = ready(j, bias[j & 7][tid]);
-        bias[j & 7][tid] = weight;
-        present |= weight != -INFINITY;
+        if (tid < BN) bias[j & 7][tid] = ready(j, bias[j & 7][tid]);
     };
     auto load_block = [&](int j) {
         if (j < last) {
@@ -195,8 +191,7 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
         if (tid < BN) {
             const int j = first + i, n = j * BN + tid;
             const float raw = weights != nullptr && j < last && n < p.Nk ? weights[n] : 0.f;
-            bias[j & 7][tid] = raw;
-            if (i < STAGES) ready_bias(j);
+            bias[j & 7][tid] = i < STAGES ? ready(j, raw) : raw;
         }
     __syncthreads();
 #pragma unroll
@@ -291,8 +286,14 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
         __syncthreads();        // before the stage is overwritten
     }
     wait_group<0>();
-    if (weights != nullptr && __syncthreads_or(present) == 0) {
-        // nothing takes part: not even a query of infinities or NaN, whose products with rows of zeros are NaN
+    // A query of infinities or NaN makes scores NaN against the zeros of points left out, too: with those alone its row is one without points.
+    bool nothing = false;
+    if (weights != nullptr && __syncthreads_or(l[0] != l[0] || l[1] != l[1])) {
+        bool present = false;
+        for (int n = first * BN + tid; n < p.Nk && n < last * BN; n += THREADS) present |= !(weights[n] <= EXCLUDED);
+        nothing = __syncthreads_or(present) == 0;
+    }
+    if (nothing) {
         m[0] = m[1] = -INFINITY;
         l[0] = l[1] = 0.f;
 #pragma unroll
