@@ -316,7 +316,7 @@ typedef struct {
  * latitude and longitude.  Tables are [nlat][pairs_lat][2] and [nlon][pairs_lon][2] (cos, sin), device, fp32.
  *
  * The backward pass takes x and dy and writes dx and dweight (summed in a fixed order: reproducible bit for bit).
- * Sums are in fp32; results are rounded once.  y may be x, and dx may be dy (same strides); other overlaps are not allowed.
+ * Sums are in fp32; results are rounded once.  eps >= 0; with eps = 0 a vector of zeros is NaN.  y may be x, and dx may be dy (same strides); other overlaps are not allowed.
  */
 typedef struct {
     int nlat, nlon, H;
@@ -357,8 +357,8 @@ sna_status_t sna_dropout(const void* x, const void* residual, void* out, sna_dty
  *   s_ij = scale q_i . k_j + log_weights_j,   out_i = sum_j exp(s_ij) v_j / sum_j exp(s_ij),   lse_i = log sum_j exp(s_ij)
  *
  * With the logarithms of quadrature weights this is global spherical attention (Eq. s2_attention_discrete).  A point whose
- * logarithmic weight is -1e30 or less is left out, whatever its k and v hold (infinities and NaN too), the others must be below 1e30; a row all of whose points are left
- * out has out = 0, lse = -infinity and no gradient.  Hk key heads serve Hq = G Hk query heads, G each: head h reads key head h / G.
+ * logarithmic weight is -1e30 or less is left out, whatever its k and v hold (infinities and NaN too), and has no gradient; the others must be below 1e30.  A row all of
+ * whose points are left out has out = 0, lse = -infinity and no gradient, whatever its q and dout hold.  Hk key heads serve Hq = G Hk query heads, G each: head h reads key head h / G.
  *
  * q, out, out_rest, dout, dq: [B][Hq][nlat_q][nlon_q][C]; k, v, dk, dv: [B][Hk][nlat_k][nlon_k][C]; bfloat16 or float16, C a multiple of 8 between
  * 8 and 128.  Pointers and strides must be multiples of 8 elements, and a tensor's points in one line (lat = nlon * lon where both

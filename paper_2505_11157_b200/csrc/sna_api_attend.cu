@@ -57,6 +57,9 @@ sna_status_t check_workspace(const void* workspace, size_t bytes, size_t need) {
 // the heads of a group) or few points.  us, mma.sync : tcgen05, bf16, C = 64, forward and (in brackets) with the backward pass: 32 heads, 32 x 1024
 // 15.8 : 12.1 (56 : 41), 17 x 8192 41.8 : 27.0 (280 : 148), 65 x 128 7.7 : 6.9 (27 : 26); 128 heads, 512 x 64 20 : 16 (77 : 61), 128 x 64 7.5 : 7.9 (28 : 27);
 // 4 heads, 64 x 8192 14.6 : 20.2 (193 : 57).
+// On the other side of both limits the gradients are slow: the mma.sync kernels do not cut a walk over many keys (dq) or many queries (dk, dv) into pieces as their
+// forward pass and the tcgen05 kernels do.  us, forward (and with the backward pass), B = 2, 8 and 2 heads of 64: 16 queries, 361x720 points 121 (6780), 17 queries
+// 250 (926); 361x720 queries, 63 points 921 (60500), 64 points 743 (3100).
 // The tcgen05 kernels find a row's maximum before the scores are scaled, and hold weights divided by the scale: it has to be positive, and not so small that
 // a point left out could be taken for one with a low weight.
 bool on_tensor_memory(const Problem& p) { return p.Nq > 16 && p.Nk >= 64 && p.scale >= 0x1p-20f && p.scale <= 0x1p20f; }

@@ -15,7 +15,7 @@
 // over blocks whose partial results a second kernel joins.
 //
 // A point whose weight leaves it out is read as zeros, whatever it holds, and has a weight of exactly zero.  A row without any point has
-// out = 0, lse = -infinity, and no gradient.
+// out = 0, lse = -infinity, and no gradient.  Both hold for queries and gradients of infinities and NaN, too, whose products with those zeros are NaN.
 #include <algorithm>
 
 #include "sna_attend.cuh"
@@ -63,7 +63,8 @@ template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi)
 }
 
 // The A operand of a second product from 16 x 16 numbers in a product's layout (two 16 x 8 accumulators), rounded to 16 bits, and what rounding leaves: with
-// both, p and ds count with twice the digits.  These kernels take the small problems, whose time is not the tensor cores'; the tcgen05 kernels round once.
+// both, p and ds count with twice the digits.  These kernels take the small problems, whose time is not the tensor cores'; of the tcgen05 kernels
+// the forward one rounds once, and so does the backward one except for narrow heads and small problems (in_two_parts).
 template <typename T>
 __device__ __forceinline__ void operands(const float (&x)[4], const float (&y)[4], uint32_t (&hi)[4], uint32_t (&lo)[4]) {
     const float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};

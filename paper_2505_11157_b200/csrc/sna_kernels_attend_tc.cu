@@ -53,8 +53,8 @@ __device__ __forceinline__ void warp_arrive(uint32_t bar, int lane) {
 //                only when its maximum has grown by 2^8: then the sums are still far from overflow, and most blocks skip the correction.
 // Narrow heads leave TMEM columns for P beside S: S of the next block is then computed during this block's softmax.  Wide ones keep P
 // in S's columns; while one tile's products run, the other tile's softmax does.
-// What bounds them: latencies.  Eight softmax warps keep the special-function unit 57 %, the tensor pipe 43 % and the issue slots 54 % busy (heads of 64); with heads of
-// 128 it is the chain of a tile's softmax and products, 3200 cycles per block and pair of tiles, of which the tensor pipe works 2200.  Tried and not kept (64x128, B = 2,
+// What bounds them: latencies.  Eight softmax warps keep the special-function unit 52 %, the tensor pipe 34 % and the issue slots 50 % busy (heads of 64); with heads of
+// 128 it is the chain of a tile's softmax and products, 3200 cycles per block and pair of tiles, of which the tensor pipe works 2000.  Tried and not kept (64x128, B = 2,
 // four heads of 32, 193 us): the two tiles taking turns with their exponentials 225; four groups with half a row per thread, whose scores do not fit
 // their 104 registers, 240; the next block's scores loaded and their maxima found between this block's exponentials 213.
 // A point's weight is one more step of the first product: its parts against ones.  (Added per element, with the weights read from shared memory, it

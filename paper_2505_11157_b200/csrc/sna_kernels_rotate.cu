@@ -353,8 +353,9 @@ sna_status_t norm_rotate(const sna_rotate_t* parts, int n_parts, sna_dtype_t dty
         if (backward) sum.dweight[i] = r.dweight;
         if (p.points == 0 || p.slices == 0) continue;
         // A block's groups take neighbouring points.  Slices are spread over blocks until the GPU has one full wave of them, as long as each still takes
-        // sixteen with the angles that it has read (four: forward 73 instead of 70 us, two waves of blocks 78, in the case above); the backward pass also
-        // bounds its blocks, each of which leaves a row of partial sums.
+        // sixteen with the angles that it has read, or two where the points give less than a block per SM; the backward pass also bounds its blocks, each of which
+        // leaves a row of partial sums.  Sixteen was measured on the case above alone (four: forward 73 instead of 70 us, two waves of blocks 78).  For middle
+        // sizes it leaves SMs idle: 91x180, B = 2, 8 and 2 heads of 24, fp16 takes 14 us, with 512 blocks for 592 places and eight trips of two vectors in a row.
         const int groups = ROTATE_THREADS / a.lanes;
         p.point_blocks = (p.points + groups - 1) / groups;
         const int want = std::max(1, (4 * sms + p.point_blocks - 1) / p.point_blocks);

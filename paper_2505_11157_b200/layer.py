@@ -57,7 +57,7 @@ def qk_norm_rotate(q, k, q_weight=None, k_weight=None, q_rotation=None, k_rotati
     q [B, Hq, nlat, nlon, C], k [B, Hk, nlat', nlon', C], float32, bfloat16 or float16, C a multiple of 4 up to 128; their grids and
     heads may differ.  ``*_weight``: float32 [C], or None for ones.  ``*_rotation``: a pair (lat_table [nlat, pairs_lat, 2], lon_table
     [nlon, pairs_lon, 2]) of cos and sin (:func:`rotation_tables`), or None for no rotation; pairs are the channels (2p, 2p + 1) if
-    ``interleaved``, else (p, p + pairs).  Differentiable in q, k and the weights."""
+    ``interleaved``, else (p, p + pairs).  ``eps`` may be zero for vectors that are not.  Differentiable in q, k and the weights."""
     q_lat, q_lon = (None, None) if q_rotation is None else q_rotation
     k_lat, k_lon = (None, None) if k_rotation is None else k_rotation
     _check_plain(q, k, q_weight, k_weight, q_lat, q_lon, k_lat, k_lon)
@@ -70,9 +70,11 @@ def weighted_attention(q, k, v, log_weights=None, scale: float | None = None, re
     q [B, Hq, nlat, nlon, C], k and v [B, Hk, nlat', nlon', C], bfloat16 or float16, C a multiple of 8 up to 128, Hq a multiple of Hk:
     query head h reads key head h // (Hq // Hk).  ``log_weights``: float32, [nlat' * nlon'] or one such row per batch; with the logarithms of
     quadrature weights (:func:`log_quadrature_weights`) this is global spherical attention.  A point at -1e30 or below (-inf, the lowest number of any
-    type) is left out, whatever k and v hold there (others must be below 1e30); a row without points gives zeros, and no gradient.  ``scale``: 1 / sqrt(C) if None.
+    type) is left out, whatever k and v hold there (others must be below 1e30); a row without points gives zeros, and no gradient, whatever q holds.  ``scale``: 1 / sqrt(C) if None.
     Returns out, or with ``return_lse`` (out, lse): the logarithm of each row's sum, float32 [B, Hq, nlat, nlon], not differentiable.
-    Differentiable in q, k and v: what is kept for the backward pass is lse, and out with what its rounding took; the probabilities are recomputed."""
+    Differentiable in q, k and v: what is kept for the backward pass is lse, and out with what its rounding took (a second tensor of out's size); the probabilities are
+    recomputed, and all three gradients computed, also where one is wanted.  The backward pass is slow for up to 16 queries, or less than 64 points, against very many of
+    the other: it walks those without cutting them."""
     _check_plain(q, k, v, log_weights)
     if scale is None:
         scale = q.shape[-1] ** -0.5 if q.dim() and q.shape[-1] else 1.0
