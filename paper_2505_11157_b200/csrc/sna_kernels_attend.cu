@@ -7,8 +7,8 @@
 //
 // These are the kernels for any size, on mma.sync (m16n8k16): a warp owns 16 rows, scores stay in registers and become the next product's
 // operand there.  Products are accumulated in 32 bits, the softmax and all statistics are in 32 bits.  p and ds are operands of
-// the second products in two 16-bit parts, except for few rows in the forward pass, where p is rounded once, to nearest, so that the roundings of a
-// sum's terms cancel on average (one station over 361x720: 55 us with two parts, 51 with one).
+// the second products in two 16-bit parts (one station over 361x720, B = 2, 8 and 2 heads of 64, bf16: 53.3 us and a relative error of 0.0017, that of rounding the result;
+// with p rounded once 52.9 us and 0.0020).
 //
 // A key head serves G query heads: their rows are stacked, so that the head's keys are read once for all of them, and so that its
 // gradients are summed within one block.  Few rows: a tile of 16 rows, the block's four warps sharing each 64 keys, and the keys split
@@ -143,7 +143,7 @@ __device__ __forceinline__ void store_out(const Problem& p, int64_t b, int64_t h
     if (p.rest.data != nullptr) static_cast<T*>(p.rest.data)[b * p.rest.batch + h * p.rest.head + n * p.rest.point + c] = from_float<T>(x - to_float(rounded));
 }
 
-// Stages of (K, V).  One station over 361x720, B = 2, 8 and 2 heads of 64, bf16, four blocks per SM, with the join: 53 us; three stages 56, four 68; five blocks per SM
+// Stages of (K, V).  One station over 361x720, B = 2, 8 and 2 heads of 64, bf16, four blocks per SM, with the join: 53 us (these with p rounded once); three stages 56, four 68; five blocks per SM
 // 54, six 61 (with fewer registers each).  A warp that loads and waits for its own keys alone gained nothing.
 constexpr int FORWARD_STAGES = 2;
 template <int CP, int WM> constexpr int forward_smem() { return WM * 16 * CP * 2 + FORWARD_STAGES * 2 * BN * CP * 2; }
@@ -276,10 +276,8 @@ __global__ void __launch_bounds__(THREADS, WM == 1 && CP <= 64 ? 4 : 1) attend_f
             for (int n = 0; n < CN; n += 2) {
                 uint32_t vb[4];
                 load_bt<CP>(vb, tv, key0 + ks * 16, n / 2, lane);
-                if (WM != 1) {
-                    mma<T>(o[n], a_lo, vb[0], vb[1]);
-                    mma<T>(o[n + 1], a_lo, vb[2], vb[3]);
-                }
+                mma<T>(o[n], a_lo, vb[0], vb[1]);
+                mma<T>(o[n + 1], a_lo, vb[2], vb[3]);
                 mma<T>(o[n], a, vb[0], vb[1]);
                 mma<T>(o[n + 1], a, vb[2], vb[3]);
             }

@@ -58,3 +58,18 @@ def test_errors_of_whole_results(shape, share, dtype):
         size = float(ref.norm())
         assert block > 4 * bound * size, (name, block / size)
         assert float((x.double() - ref).norm()) <= bound * size, (name, float((x.double() - ref).norm()) / size)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=lambda d: str(d).split(".")[1])
+@pytest.mark.parametrize("shape", [(2, 8, 2, 1, 361 * 720, 64), (1, 2, 2, 1, 30011, 128), (2, 8, 1, 2, 9000, 32), (4, 8, 2, 2, 16200, 40), (1, 4, 4, 16, 8192, 32), (2, 4, 2, 60, 50, 24)],
+                         ids=lambda s: "-".join(map(str, s)))
+def test_few_queries_or_points_are_off_by_the_rounding_of_the_result_alone(shape, dtype):
+    """p in two 16-bit parts is off by u^2, exponentials by 2^-22, sums in 32 bits by less than a thousandth of u on average; an error d before the result's rounding moves
+    the result by at most 2 d more than that rounding, so that a twentieth of it is ample."""
+    B, Hq, Hk, Nq, Nk, C = shape
+    torch.manual_seed(Nk)
+    q, k, v = (torch.randn(B, h, 1, n, C, device="cuda").to(dtype) for h, n in ((Hq, Nq), (Hk, Nk), (Hk, Nk)))
+    w = torch.randn(B, Nk, device="cuda")
+    ref = definition(q, k, v, w, torch.zeros_like(q))[0][0]
+    alone = float((ref.to(dtype).double() - ref).norm())
+    assert float((layer.weighted_attention(q, k, v, w).double() - ref).norm()) < 1.05 * alone
