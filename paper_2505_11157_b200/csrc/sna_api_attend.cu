@@ -62,7 +62,8 @@ sna_status_t check_workspace(const void* workspace, size_t bytes, size_t need) {
 // 250 (926); 361x720 queries, 63 points 921 (60500), 64 points 743 (3100).
 // The tcgen05 kernels find a row's maximum before the scores are scaled, and hold weights divided by the scale: it has to be positive, and not so small that
 // a point left out could be taken for one with a low weight.
-bool on_tensor_memory(const Problem& p) { return p.Nq > 16 && p.Nk >= 64 && p.scale >= 0x1p-20f && p.scale <= 0x1p20f; }
+// (Without query heads there is no tile of queries, and dk and dv are zeros.)
+bool on_tensor_memory(const Problem& p) { return p.G > 0 && p.Nq > 16 && p.Nk >= 64 && p.scale >= 0x1p-20f && p.scale <= 0x1p20f; }
 // Pieces of a workspace, or with a null pointer their sizes alone.
 struct Pieces {
     char* at;

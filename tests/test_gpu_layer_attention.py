@@ -548,3 +548,15 @@ def test_long_and_narrow_problems(shape, share, dtype):
     w = torch.randn(B, Nk, device="cuda").masked_fill(torch.rand(B, Nk, device="cuda") < share, -math.inf)
     w[0, Nk // 8: Nk // 8 + int(share * Nk)] = -math.inf
     check(q, k, v, w)
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=lambda d: str(d).split(".")[1])
+@pytest.mark.parametrize("weighted", [False, True])
+def test_no_query_heads(weighted, dtype):
+    q = torch.randn(2, 0, 3, 100, 32, device="cuda").to(dtype).requires_grad_()
+    k, v = (torch.randn(2, 2, 20, 30, 32, device="cuda").to(dtype).requires_grad_() for _ in range(2))
+    out = layer.weighted_attention(q, k, v, torch.randn(600, device="cuda") if weighted else None)
+    assert out.shape == q.shape
+    spoil = torch.full((2, 2, 20, 30, 32), math.nan, device="cuda", dtype=dtype)        # (what the next results' memory may hold)
+    del spoil
+    assert not any(bool(g.any()) for g in torch.autograd.grad(out.sum(), (q, k, v)))
